@@ -55,6 +55,9 @@ extern "C" {
 #define SEMMOE_MAX_E 512 /* experts */
 #define SEMMOE_MAX_K 16  /* experts per token */
 #define SEMMOE_MAX_D 64  /* logical ranks */
+#define SEMMOE_MAX_ADAPTERS 1024    /* low-rank adapters of one call */
+#define SEMMOE_MAX_RANK 128         /* their rank */
+#define SEMMOE_MAX_REQUESTS 65536   /* requests of one adapter_index */
 
 typedef struct semmoe_config {
   int32_t T, d, E, k, F, D;
@@ -71,7 +74,7 @@ typedef struct semmoe_config {
 int32_t semmoe_version(void);
 /* hipError_t of the last failed HIP call on this thread (0 if none). */
 int32_t semmoe_last_hip_error(void);
-/* Workspace size that covers every device call below for this config. */
+/* Workspace size that covers every device call below for this config, but for those that name a size of their own. */
 int32_t semmoe_workspace_bytes(const semmoe_config* cfg, size_t* bytes_out /*host*/);
 
 /*
@@ -453,6 +456,111 @@ int32_t semmoe_shared_ffn(const semmoe_config* cfg, void* stream, const void* X,
  */
 int32_t semmoe_combine(const semmoe_config* cfg, void* stream, const void* Y, const int32_t* slot_of_pair,
                        const float* topk_w, const void* Y_shared, void* Out);
+
+/*
+ * The gradient of the layer's steps, for training what lies before and beside it (adapters, attention) with the experts'
+ * and the router's weights standing still.  In the order of a backward pass:
+ *   combine_grad -> expert_ffn_grad, shared_ffn_grad -> dispatch_grad
+ * (the router's weights' gradient begins at dtopk_w; towards Y_shared combine's gradient is dOut itself).
+ */
+
+/*
+ * combine_grad - the gradient of semmoe_combine towards the experts' rows and the weights:
+ *   dY[slot_of_pair[i*k+j]] = topk_w[i,j] * dOut[i]  (rounded once to the act type);
+ *   dtopk_w[i,j] = <dOut[i], Y[slot_of_pair[i*k+j]]>  (fp32, summed in a fixed order).
+ * A pair whose slot lies outside [0,P) has no row and dtopk_w = 0; rows of dY that no pair names are not written.
+ * dev in : dOut[T,d] act; Y[P,d] act (NULL where dtopk_w is); slot_of_pair[P], no slot twice; topk_w[T,k] f32 (NULL
+ *          where dY is).  dev out: dY[P,d] act or NULL (may be Y itself); dtopk_w[T,k] f32 or NULL; not both NULL.
+ */
+int32_t semmoe_combine_grad(const semmoe_config* cfg, void* stream, const void* dOut, const void* Y,
+                            const int32_t* slot_of_pair, const float* topk_w, void* dY, float* dtopk_w);
+
+/*
+ * dispatch_grad - the gradient of dispatch_rows towards X: dX[i] = sum_j dX_perm[slot_of_pair[i*k+j]] (+ dX_add[i]),
+ * accumulated in fp32 in ascending j, rounded once to the act type.  dX_add: what reaches X on other ways (the shared
+ * expert's gradient, the residual's).  A slot outside [0,P) adds nothing.
+ * dev in : dX_perm[P,d] act; slot_of_pair[P]; dX_add[T,d] act or NULL.  dev out: dX[T,d] act (may be dX_add itself).
+ */
+int32_t semmoe_dispatch_grad(const semmoe_config* cfg, void* stream, const void* dX_perm, const int32_t* slot_of_pair,
+                             const void* dX_add, void* dX);
+
+/*
+ * expert_ffn_grad - the gradient of semmoe_expert_ffn towards its rows, the experts' weights standing still.  With
+ * g = W_gate[e] x, u = W_up[e] x (computed again from X_perm) and sig = 1/(1+exp(-g)):
+ *   dh = W_down[e]^T dy;  dg = dh * u * sig * (1 + g (1 - sig));  du = dh * g * sig;
+ *   dx = W_gate[e]^T dg + W_up[e]^T du.
+ * fp32 accumulate; g, u, dg and du are rounded to the act type.  rank, offsets and weights as in semmoe_expert_ffn; rows of
+ * other ranks in dX_perm are not written.
+ * dev in : X_perm[P,d] act; dY[P,d] act.  dev out: dX_perm[P,d] act (may be X_perm or dY itself).
+ * ws: T*k*2F activations + 512 bytes (not covered by semmoe_workspace_bytes).
+ */
+int32_t semmoe_expert_ffn_grad(const semmoe_config* cfg, void* stream, int32_t rank, const void* X_perm, const void* dY,
+                               const int32_t* expert_offsets, const int32_t* expert_of_phys, const void* W_gu,
+                               const void* W_down, void* dX_perm, void* ws, size_t ws_bytes);
+
+/*
+ * shared_ffn_grad - the same for semmoe_shared_ffn: X[n_tokens,d], dY[n_tokens,d] -> dX[n_tokens,d] (may be X or dY
+ * itself).  n_tokens <= T*k.  ws: n_tokens*2F activations + 512 bytes.
+ */
+int32_t semmoe_shared_ffn_grad(const semmoe_config* cfg, void* stream, const void* X, const void* dY, int32_t n_tokens,
+                               const void* W_gu_sh, const void* W_down_sh, void* dX, void* ws, size_t ws_bytes);
+
+/*
+ * Low-rank adapters of many requests at once, beside a projection that all requests share (the shared expert, an attention
+ * projection): token i of a request with adapter a gets  s_a B_a (A_a x_i)  added to the projection's output.
+ *   A[n_adapters, rank, d_in], B[n_adapters, d_out, rank] act; scale s[n_adapters] f32 or NULL (1).
+ * Rows may lie further apart than they are wide: ld* in elements, 0 = packed, multiples of 8, at least the row's width.  So X
+ * and Y may be column ranges of wider tensors (one projection of a fused one); pointers are 16-byte aligned.
+ * rank, d_in and d_out are multiples of 8.  cfg: T (tokens of the batch) and dtype are used.
+ */
+typedef struct semmoe_adapter_shape {
+  int32_t n_adapters, rank, d_in, d_out;
+  int64_t ldx;     /* X[T,d_in] */
+  int64_t ldy;     /* dY[T,d_out] (adapters_grad) */
+  int64_t ld_base; /* Y_base[T,d_out] / dX_base[T,d_in] */
+  int64_t ld_out;  /* Y[T,d_out] / dX[T,d_in] */
+} semmoe_adapter_shape;
+
+/*
+ * adapter_index - the tokens of a batch of requests in the order the adapter calls read them.  Request q owns the tokens
+ * [req_offsets[q], req_offsets[q+1]) (as in semmoe_request_schedule; empty requests are allowed) and asks for adapter
+ * adapter_of_req[q]; a value outside [0,n_adapters) is no adapter.  order = tokens sorted by adapter, ascending inside one;
+ * then those without an adapter, ascending; then -1 for each of the cfg->T rows behind the last request (padding, which
+ * the adapter calls leave alone).  adapter_offsets[a] = first place of a's tokens, [n_adapters] = tokens with an adapter.
+ * One index serves every projection of every layer of a step.  One launch, no workspace.
+ * req_offsets[0] = 0, ascending, at most T (they are clamped when read; the result is defined for ascending ones only).
+ * dev in : req_offsets[n_req+1], adapter_of_req[n_req] i32.  dev out: order[T], adapter_offsets[n_adapters+1] i32.
+ */
+int32_t semmoe_adapter_index(const semmoe_config* cfg, void* stream, const int32_t* req_offsets, int32_t n_req,
+                             const int32_t* adapter_of_req, int32_t n_adapters, int32_t* order, int32_t* adapter_offsets);
+
+/* Workspace of semmoe_adapters and semmoe_adapters_grad for this config and shape (its ld* do not matter). */
+int32_t semmoe_adapter_workspace_bytes(const semmoe_config* cfg, const semmoe_adapter_shape* shape,
+                                       size_t* bytes_out /*host*/);
+
+/*
+ * adapters - Y[i] = Y_base[i] + s_a B_a (A_a X[i]) for the tokens with an adapter, Y[i] = Y_base[i] for those without.
+ * Sums in fp32; s_a A_a x is rounded to the act type once (an operand of the second product), Y once.
+ * dev in : X[T,d_in]; order, adapter_offsets of semmoe_adapter_index; A, B, scale; Y_base[T,d_out] act or NULL (zero).
+ * dev out: Y[T,d_out] act; may be Y_base itself (with the same ld), then rows without an adapter are not touched.
+ */
+int32_t semmoe_adapters(const semmoe_config* cfg, void* stream, const semmoe_adapter_shape* shape, const void* X,
+                        const int32_t* order, const int32_t* adapter_offsets, const void* A, const void* B,
+                        const float* scale, const void* Y_base, void* Y, void* ws, size_t ws_bytes);
+
+/*
+ * adapters_grad - the gradient of semmoe_adapters (towards Y_base it is dY itself).  With v_i = s_a B_a^T dY[i] and
+ * u_i = s_a A_a X[i]:
+ *   dX[i] = dX_base[i] + A_a^T v_i (dX_base[i] alone without an adapter);
+ *   dA_a = sum over a's tokens of v_i X[i]^T;   dB_a = sum of dY[i] u_i^T  (zero for an adapter without tokens).
+ * Sums in fp32 in a fixed order; u and v are rounded to the act type once, the results once.
+ * dev in : X[T,d_in], dY[T,d_out]; order, adapter_offsets; A, B, scale; dX_base[T,d_in] act or NULL (zero).
+ * dev out: dX[T,d_in] (may be dX_base itself, with the same ld), dA and dB (as A and B) act; each may be NULL, not all.
+ */
+int32_t semmoe_adapters_grad(const semmoe_config* cfg, void* stream, const semmoe_adapter_shape* shape, const void* X,
+                             const void* dY, const int32_t* order, const int32_t* adapter_offsets, const void* A,
+                             const void* B, const float* scale, const void* dX_base, void* dX, void* dA, void* dB,
+                             void* ws, size_t ws_bytes);
 
 /*
  * Probes of what the chip sustains, for reading roofline fractions against (not part of the layer; no passage of

@@ -45,6 +45,12 @@ class CoschedParams(C.Structure):
                 ("n_steps", C.c_int32)]
 
 
+class _CAdapterShape(C.Structure):
+    """semmoe_adapter_shape of the C header, field for field"""
+    _fields_ = [("n_adapters", C.c_int32), ("rank", C.c_int32), ("d_in", C.c_int32), ("d_out", C.c_int32),
+                ("ldx", C.c_int64), ("ldy", C.c_int64), ("ld_base", C.c_int64), ("ld_out", C.c_int64)]
+
+
 @dataclass
 class Config:
     T: int
@@ -121,6 +127,14 @@ _SIGS = {
     "semmoe_expert_ffn": ([_P, _P, C.c_int32] + [_P] * 7 + [C.c_size_t], C.c_int32),
     "semmoe_shared_ffn": ([_P, _P, _P, C.c_int32, _P, _P, _P, _P, C.c_size_t], C.c_int32),
     "semmoe_combine": ([_P] * 7, C.c_int32),
+    "semmoe_combine_grad": ([_P] * 8, C.c_int32),
+    "semmoe_dispatch_grad": ([_P] * 6, C.c_int32),
+    "semmoe_expert_ffn_grad": ([_P, _P, C.c_int32] + [_P] * 8 + [C.c_size_t], C.c_int32),
+    "semmoe_shared_ffn_grad": ([_P] * 4 + [C.c_int32] + [_P] * 4 + [C.c_size_t], C.c_int32),
+    "semmoe_adapter_index": ([_P, _P, _P, C.c_int32, _P, C.c_int32, _P, _P], C.c_int32),
+    "semmoe_adapter_workspace_bytes": ([_P, _P, C.POINTER(C.c_size_t)], C.c_int32),
+    "semmoe_adapters": ([_P] * 12 + [C.c_size_t], C.c_int32),
+    "semmoe_adapters_grad": ([_P] * 15 + [C.c_size_t], C.c_int32),
     "semmoe_probe_copy": ([_P, _P, _P, C.c_size_t], C.c_int32),
     "semmoe_probe_stream": ([_P, _P, C.c_size_t, C.c_int32, _P], C.c_int32),
     "semmoe_probe_mfma": ([_P, _P, C.c_int32, _P, C.POINTER(C.c_double)], C.c_int32),
@@ -158,6 +172,17 @@ def _ptr(t):
     return t.ctypes.data
 
 
+def _rows(t, n_cols: int, name: str):
+    """(pointer, distance of rows in elements) of a matrix whose rows are runs of n_cols numbers, however far apart"""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or t.shape[1] != n_cols or t.stride(1) != 1:
+        raise ValueError("%s must be a matrix of rows of %d numbers, each row one run of memory" % (name, n_cols))
+    if t.shape[0] > 1 and t.stride(0) < n_cols:  # a broadcast row, too: the library takes a distance of 0 as packed
+        raise ValueError("rows of %s overlap" % name)
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else n_cols)
+
+
 def _stream():
     """handle of torch's current stream on the current device.  A call costs the host a few microseconds, as much as a
     small kernel; once torch has initialised the GPU the handle comes without the availability check and the stream
@@ -178,6 +203,8 @@ class SemMoE:
         self.ws = None
         self.ws_bytes = 0
         self.ws_shared = None
+        self._own_ws = {}   # workspaces of the calls that name a size of their own, by call
+        self._old_ws = []   # smaller ones before them: a captured graph may still hold their addresses
         self._c_config = None  # (values, C struct of them)
         if allocate_workspace:
             import torch
@@ -202,6 +229,16 @@ class SemMoE:
         for k_, v in over.items():
             setattr(c, k_, v)
         return c
+
+    def _workspace(self, call: str, need: int):
+        """(pointer, bytes) of a workspace that only `call` uses, of at least `need` bytes: kept from call to call"""
+        t = self._own_ws.get(call)
+        if t is None or t.numel() < need:
+            import torch
+            if t is not None:
+                self._old_ws.append(t)
+            self._own_ws[call] = t = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+        return t.data_ptr(), t.numel()
 
     def workspace_bytes(self) -> int:
         n = C.c_size_t(0)
@@ -423,3 +460,89 @@ class SemMoE:
         c = self._cfg()
         self._check("semmoe_combine", self.lib.semmoe_combine(
             C.byref(c), _stream(), _ptr(Y), _ptr(slot_of_pair), _ptr(topk_w), _ptr(Y_shared), _ptr(Out)))
+
+    # -- gradients of the layer's steps
+    def combine_grad(self, dOut, Y, slot_of_pair, topk_w, dY, dtopk_w):
+        """dY or dtopk_w may be None (then topk_w or Y may be, too); dY may be Y itself"""
+        c = self._cfg()
+        self._check("semmoe_combine_grad", self.lib.semmoe_combine_grad(
+            C.byref(c), _stream(), _ptr(dOut), _ptr(Y), _ptr(slot_of_pair), _ptr(topk_w), _ptr(dY), _ptr(dtopk_w)))
+
+    def dispatch_grad(self, dX_perm, slot_of_pair, dX, dX_add=None):
+        c = self._cfg()
+        self._check("semmoe_dispatch_grad", self.lib.semmoe_dispatch_grad(
+            C.byref(c), _stream(), _ptr(dX_perm), _ptr(slot_of_pair), _ptr(dX_add), _ptr(dX)))
+
+    def _ffn_grad_bytes(self, rows: int) -> int:
+        return rows * 2 * self.cfg.F * (2 if self.cfg.dtype == BF16 else 4) + 512
+
+    def expert_ffn_grad(self, rank, X_perm, dY, expert_offsets, expert_of_phys, W_gu, W_down, dX_perm):
+        c = self._cfg()
+        ws, n = self._workspace("expert_ffn_grad", self._ffn_grad_bytes(self.cfg.T * self.cfg.k))
+        self._check("semmoe_expert_ffn_grad", self.lib.semmoe_expert_ffn_grad(
+            C.byref(c), _stream(), int(rank), _ptr(X_perm), _ptr(dY), _ptr(expert_offsets), _ptr(expert_of_phys),
+            _ptr(W_gu), _ptr(W_down), _ptr(dX_perm), ws, n))
+
+    def shared_ffn_grad(self, X, dY, n_tokens, W_gu_sh, W_down_sh, dX):
+        """has a workspace of its own, as shared_ffn does, so that it may run on another stream beside the routed path's"""
+        c = self._cfg()
+        ws, n = self._workspace("shared_ffn_grad", self._ffn_grad_bytes(max(int(n_tokens), 0)))
+        self._check("semmoe_shared_ffn_grad", self.lib.semmoe_shared_ffn_grad(
+            C.byref(c), _stream(), _ptr(X), _ptr(dY), int(n_tokens), _ptr(W_gu_sh), _ptr(W_down_sh), _ptr(dX), ws, n))
+
+    # -- low-rank adapters
+    def adapter_index(self, req_offsets, adapter_of_req, n_adapters, order, adapter_offsets):
+        """the batch is order's length; requests are adapter_of_req's"""
+        c = self._cfg(T=order.shape[0])
+        n_req = adapter_of_req.shape[0]
+        if req_offsets.shape[0] != n_req + 1 or adapter_offsets.shape[0] != int(n_adapters) + 1:
+            raise SemMoEError("adapter_index: shapes must be req_offsets[n_req+1], adapter_of_req[n_req], "
+                              "adapter_offsets[n_adapters+1]", -2)
+        self._check("semmoe_adapter_index", self.lib.semmoe_adapter_index(
+            C.byref(c), _stream(), _ptr(req_offsets), int(n_req), _ptr(adapter_of_req), int(n_adapters), _ptr(order),
+            _ptr(adapter_offsets)))
+
+    def _adapter_shape(self, call, X, order, adapter_offsets, A, B, scale):
+        n_ad, rank, d_in = A.shape
+        if B.dim() != 3 or B.shape[0] != n_ad or B.shape[2] != rank or adapter_offsets.shape[0] != n_ad + 1 \
+                or order.shape[0] != X.shape[0] or (scale is not None and tuple(scale.shape) != (n_ad,)):
+            raise SemMoEError("%s: shapes must be A[n,r,d_in], B[n,d_out,r], adapter_offsets[n+1], order[T], scale[n]" % call, -2)
+        return self._cfg(T=X.shape[0]), _CAdapterShape(n_ad, rank, d_in, B.shape[1], 0, 0, 0, 0)
+
+    def _adapter_workspace(self, c, s):
+        n = C.c_size_t(0)
+        self._check("semmoe_adapter_workspace_bytes",
+                    self.lib.semmoe_adapter_workspace_bytes(C.byref(c), C.byref(s), C.byref(n)))
+        return self._workspace("adapters", int(n.value))
+
+    def adapters(self, X, order, adapter_offsets, A, B, Y, Y_base=None, scale=None):
+        """Y = Y_base + scale * B (A x) by each token's adapter; Y_base=None adds to nothing, Y_base=Y adds in place"""
+        c, s = self._adapter_shape("adapters", X, order, adapter_offsets, A, B, scale)
+        x, s.ldx = _rows(X, s.d_in, "X")
+        base, s.ld_base = _rows(Y_base, s.d_out, "Y_base")
+        y, s.ld_out = _rows(Y, s.d_out, "Y")
+        self._same_rows("adapters", X, Y_base, Y)
+        ws, n = self._adapter_workspace(c, s)
+        self._check("semmoe_adapters", self.lib.semmoe_adapters(
+            C.byref(c), _stream(), C.byref(s), x, _ptr(order), _ptr(adapter_offsets), _ptr(A), _ptr(B), _ptr(scale), base, y,
+            ws, n))
+
+    def adapters_grad(self, X, dY, order, adapter_offsets, A, B, dX=None, dA=None, dB=None, dX_base=None, scale=None):
+        """each of dX, dA, dB may be left out; dX_base=dX adds in place"""
+        c, s = self._adapter_shape("adapters_grad", X, order, adapter_offsets, A, B, scale)
+        x, s.ldx = _rows(X, s.d_in, "X")
+        dy, s.ldy = _rows(dY, s.d_out, "dY")
+        base, s.ld_base = _rows(dX_base, s.d_in, "dX_base")
+        dx, s.ld_out = _rows(dX, s.d_in, "dX")
+        self._same_rows("adapters_grad", X, dY, dX_base, dX)
+        if (dA is not None and dA.shape != A.shape) or (dB is not None and dB.shape != B.shape):
+            raise SemMoEError("adapters_grad: dA and dB have the shapes of A and B", -2)
+        ws, n = self._adapter_workspace(c, s)
+        self._check("semmoe_adapters_grad", self.lib.semmoe_adapters_grad(
+            C.byref(c), _stream(), C.byref(s), x, dy, _ptr(order), _ptr(adapter_offsets), _ptr(A), _ptr(B), _ptr(scale), base,
+            dx, _ptr(dA), _ptr(dB), ws, n))
+
+    @staticmethod
+    def _same_rows(call, first, *others):
+        if any(t is not None and t.shape[0] != first.shape[0] for t in others):
+            raise SemMoEError("%s: all row tensors have X's rows" % call, -2)

@@ -18,7 +18,8 @@ __device__ __forceinline__ uint4 load_stream16(const uint4* p) {
 // lose a third of their rate (16384 tokens of 7168, 8 rows each: 277 us without the stores, 412 with them): written
 // back in the order they leave the L2, they interrupt the read stream.  Past the caches: 388 us; 32768 tokens of 2880,
 // 4 rows each: 179 -> 164.  A result that the memory-side cache can hold for its reader is stored as before.
-template <bool BF16, int KU, bool NTOUT>
+// WEIGHTED = false: weights of one, topk_w is not read (the gradient of dispatch).
+template <bool BF16, int KU, bool NTOUT, bool WEIGHTED>
 __global__ __launch_bounds__(512) void combine_kernel(int k, int row_chunks, int P, const uint4* __restrict__ Y,
                                                       const int32_t* __restrict__ slot_of_pair,
                                                       const float* __restrict__ topk_w,
@@ -42,7 +43,8 @@ __global__ __launch_bounds__(512) void combine_kernel(int k, int row_chunks, int
     if (j < k) {
       const int s = slot_of_pair[size_t(tok) * k + j];
       if ((unsigned)s < (unsigned)P) sl[j] = s;
-      wt[j] = topk_w[size_t(tok) * k + j];
+      if constexpr (WEIGHTED) wt[j] = topk_w[size_t(tok) * k + j];
+      else wt[j] = 1.0f;
     }
   }
   for (int c = threadIdx.x; c < row_chunks; c += blockDim.x) {
@@ -105,14 +107,14 @@ __global__ __launch_bounds__(512) void combine_kernel(int k, int row_chunks, int
   }
 }
 
-template <bool BF16, bool NTOUT>
+template <bool BF16, bool NTOUT, bool WEIGHTED>
 static void launch_combine(int k, int T, int row_chunks, hipStream_t s, const uint4* Y, const int32_t* slot,
                            const float* w, const uint4* Ysh, uint4* Out) {
   const int P = T * k;
   const int threads = row_walk_threads(row_chunks);
   // k rounded up to the next unrolled width; the kernel skips the slots beyond k
 #define SEMMOE_COMBINE(KU_)                                                                                          \
-  hipLaunchKernelGGL((combine_kernel<BF16, KU_, NTOUT>), dim3(T), dim3(threads), 0, s, k, row_chunks, P, Y, slot, w, \
+  hipLaunchKernelGGL((combine_kernel<BF16, KU_, NTOUT, WEIGHTED>), dim3(T), dim3(threads), 0, s, k, row_chunks, P, Y, slot, w, \
                      Ysh, Out)
   if (k <= 1) SEMMOE_COMBINE(1);
   else if (k <= 2) SEMMOE_COMBINE(2);
@@ -129,20 +131,32 @@ constexpr size_t kCachedResult = size_t(128) << 20;
 
 using namespace semmoe;
 
-extern "C" int32_t semmoe_combine(const semmoe_config* cfg, void* stream, const void* Y, const int32_t* slot_of_pair,
-                                  const float* topk_w, const void* Y_shared, void* Out) {
+// Out[i] = sum_j w[i,j] Rows[slot(i,j)] (+ Add[i]); w = 1 where topk_w is not wanted
+template <bool WEIGHTED>
+static int32_t run_combine(const semmoe_config* cfg, void* stream, const void* Rows, const int32_t* slot_of_pair,
+                           const float* topk_w, const void* Add, void* Out) {
   int32_t st = validate_config(cfg, true, true, false);
   if (st != SEMMOE_OK) return st;
-  if (!Y || !slot_of_pair || !topk_w || !Out) return SEMMOE_EINVAL;
-  if (!aligned16(Y) || !aligned16(Out) || (Y_shared && !aligned16(Y_shared))) return SEMMOE_EINVAL;
+  if (!Rows || !slot_of_pair || (WEIGHTED && !topk_w) || !Out) return SEMMOE_EINVAL;
+  if (!aligned16(Rows) || !aligned16(Out) || (Add && !aligned16(Add))) return SEMMOE_EINVAL;
   if (cfg->T == 0) return SEMMOE_OK;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int row_chunks = int(size_t(cfg->d) * act_bytes(cfg) / 16);
   const bool nt = size_t(cfg->T) * row_chunks * 16 > kCachedResult;
-  auto* const launch = cfg->dtype == SEMMOE_BF16 ? (nt ? launch_combine<true, true> : launch_combine<true, false>)
-                                                 : (nt ? launch_combine<false, true> : launch_combine<false, false>);
-  launch(cfg->k, cfg->T, row_chunks, s, static_cast<const uint4*>(Y), slot_of_pair, topk_w,
-         static_cast<const uint4*>(Y_shared), static_cast<uint4*>(Out));
+  auto* const launch = cfg->dtype == SEMMOE_BF16 ? (nt ? launch_combine<true, true, WEIGHTED> : launch_combine<true, false, WEIGHTED>)
+                                                 : (nt ? launch_combine<false, true, WEIGHTED> : launch_combine<false, false, WEIGHTED>);
+  launch(cfg->k, cfg->T, row_chunks, s, static_cast<const uint4*>(Rows), slot_of_pair, topk_w,
+         static_cast<const uint4*>(Add), static_cast<uint4*>(Out));
   SEMMOE_LAUNCH_CHECK();
   return SEMMOE_OK;
+}
+
+extern "C" int32_t semmoe_combine(const semmoe_config* cfg, void* stream, const void* Y, const int32_t* slot_of_pair,
+                                  const float* topk_w, const void* Y_shared, void* Out) {
+  return run_combine<true>(cfg, stream, Y, slot_of_pair, topk_w, Y_shared, Out);
+}
+
+extern "C" int32_t semmoe_dispatch_grad(const semmoe_config* cfg, void* stream, const void* dX_perm,
+                                        const int32_t* slot_of_pair, const void* dX_add, void* dX) {
+  return run_combine<false>(cfg, stream, dX_perm, slot_of_pair, nullptr, dX_add, dX);
 }

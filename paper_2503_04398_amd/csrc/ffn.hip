@@ -1,6 +1,7 @@
 // expert_ffn / shared_ffn: the expert FFN (Sec. 2) in SwiGLU form as two grouped GEMMs over the rows
 // that dispatch made contiguous per expert:  H = silu(X_perm W_gate^T) * (X_perm W_up^T),  Y = H W_down^T.
 #include "gemm_core.hpp"
+#include "gemm_nn.hpp"
 
 namespace semmoe {
 
@@ -22,6 +23,34 @@ static int32_t run_ffn(const semmoe_config* cfg, hipStream_t s, const void* X, c
   b.N = cfg->d; b.K = cfg->F;
   b.out = Y; b.ldo = cfg->d;
   return launch_gemm(kModeStore, cfg->dtype, b, max_rows, est_rows, s);
+}
+
+// The gradient towards the rows, the weights standing still:  [g | u] = X W_gu^T again,  dh = dY W_down,
+// dg = dh u silu'(g),  du = dh silu(g),  dX = [dg | du] W_gu.  GU: rows x 2F of the workspace, [g | u] and then [dg | du].
+// g, u, dg and du are rounded to the act type (as operands of the products they have to be); dh is not.
+static int32_t run_ffn_grad(const semmoe_config* cfg, hipStream_t s, const void* X, const void* dY, const int32_t* offsets,
+                            int q_lo, int nq, int n_rows_single, int max_rows, int est_rows, const int32_t* group_to_weight,
+                            const void* W_gu, const void* W_down, void* dX, void* GU) {
+  GemmArgs a{};
+  a.X = X; a.ldx = cfg->d;
+  a.W = W_gu; a.w_group_stride = size_t(2) * cfg->F * cfg->d; a.ldw = cfg->d;
+  a.N = 2 * cfg->F; a.K = cfg->d;
+  a.offsets = offsets; a.q_lo = q_lo; a.nq = nq; a.n_rows_single = n_rows_single;
+  a.group_to_weight = group_to_weight;
+  a.out = GU; a.ldo = 2 * cfg->F;
+  int32_t st = launch_gemm(kModeStore, cfg->dtype, a, max_rows, est_rows, s);
+  if (st != SEMMOE_OK) return st;
+  GemmArgs h = a;
+  h.X = dY;
+  h.W = W_down; h.w_group_stride = size_t(cfg->d) * cfg->F; h.ldw = cfg->F;
+  h.N = cfg->F;
+  st = launch_gemm_nn(kNnSwigluGrad, cfg->dtype, h, max_rows, est_rows, s);
+  if (st != SEMMOE_OK) return st;
+  GemmArgs b = a;
+  b.X = GU; b.ldx = 2 * cfg->F;
+  b.N = cfg->d; b.K = 2 * cfg->F;
+  b.out = dX; b.ldo = cfg->d;
+  return launch_gemm_nn(kNnStore, cfg->dtype, b, max_rows, est_rows, s);
 }
 
 size_t ws_ffn(const semmoe_config* cfg) {
@@ -64,4 +93,38 @@ extern "C" int32_t semmoe_shared_ffn(const semmoe_config* cfg, void* stream, con
   if (n_tokens == 0) return SEMMOE_OK;
   return run_ffn(cfg, static_cast<hipStream_t>(stream), X, nullptr, 0, 1, n_tokens, n_tokens, n_tokens, nullptr, W_gu_sh,
                  W_down_sh, Y_shared, H);
+}
+
+extern "C" int32_t semmoe_expert_ffn_grad(const semmoe_config* cfg, void* stream, int32_t rank, const void* X_perm,
+                                          const void* dY, const int32_t* expert_offsets, const int32_t* expert_of_phys,
+                                          const void* W_gu, const void* W_down, void* dX_perm, void* ws, size_t ws_bytes) {
+  int32_t st = validate_config(cfg, true, true, true);
+  if (st != SEMMOE_OK) return st;
+  if (!X_perm || !dY || !expert_offsets || !expert_of_phys || !W_gu || !W_down || !dX_perm) return SEMMOE_EINVAL;
+  if (rank < -1 || rank >= cfg->D) return SEMMOE_EINVAL;
+  if (!aligned16(X_perm) || !aligned16(dY) || !aligned16(W_gu) || !aligned16(W_down) || !aligned16(dX_perm)) return SEMMOE_EINVAL;
+  Carver c(ws, ws_bytes);
+  void* GU = c.take<char>(size_t(cfg->T) * cfg->k * 2 * cfg->F * act_bytes(cfg));
+  if (!c.ok) return SEMMOE_EWORKSPACE;
+  const int m = cfg->E / cfg->D;
+  const int q_lo = rank < 0 ? 0 : rank * m;
+  const int nq = rank < 0 ? cfg->E : m;
+  return run_ffn_grad(cfg, static_cast<hipStream_t>(stream), X_perm, dY, expert_offsets, q_lo, nq, 0, cfg->T * cfg->k,
+                      cfg->T * cfg->k / cfg->E, expert_of_phys, W_gu, W_down, dX_perm, GU);
+}
+
+extern "C" int32_t semmoe_shared_ffn_grad(const semmoe_config* cfg, void* stream, const void* X, const void* dY,
+                                          int32_t n_tokens, const void* W_gu_sh, const void* W_down_sh, void* dX, void* ws,
+                                          size_t ws_bytes) {
+  int32_t st = validate_config(cfg, true, true, true);
+  if (st != SEMMOE_OK) return st;
+  if (!X || !dY || !W_gu_sh || !W_down_sh || !dX || n_tokens < 0) return SEMMOE_EINVAL;
+  if ((long long)n_tokens > (long long)cfg->T * cfg->k) return SEMMOE_ESHAPE;
+  if (!aligned16(X) || !aligned16(dY) || !aligned16(W_gu_sh) || !aligned16(W_down_sh) || !aligned16(dX)) return SEMMOE_EINVAL;
+  Carver c(ws, ws_bytes);
+  void* GU = c.take<char>(size_t(n_tokens) * 2 * cfg->F * act_bytes(cfg));
+  if (!c.ok) return SEMMOE_EWORKSPACE;
+  if (n_tokens == 0) return SEMMOE_OK;
+  return run_ffn_grad(cfg, static_cast<hipStream_t>(stream), X, dY, nullptr, 0, 1, n_tokens, n_tokens, n_tokens, nullptr,
+                      W_gu_sh, W_down_sh, dX, GU);
 }

@@ -1,0 +1,148 @@
+"""CPU-only: the adapter and gradient calls check their arguments before they touch a GPU."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2503_04398_amd as S
+from paper_2503_04398_amd import binding as B
+
+EINVAL, ESHAPE, EWORKSPACE, EUNSUPPORTED = -1, -2, -3, -5
+
+
+def _lib():
+    m = S.SemMoE(S.Config(T=64, d=64, E=16, k=2, F=32, D=4, cap=16), allocate_workspace=False)
+    buf = np.zeros(4096 + 16, dtype=np.int32)
+    p = buf.ctypes.data + (-buf.ctypes.data) % 16
+    return m.lib, m.cfg.c(), p, buf
+
+
+def test_row_gradients_refuse():
+    lib, c, p, _keep = _lib()
+    r = C.byref(c)
+    assert lib.semmoe_combine_grad(r, None, None, p, p, p, p, p) == EINVAL   # no dOut
+    assert lib.semmoe_combine_grad(r, None, p, p, None, p, p, p) == EINVAL   # no slots
+    assert lib.semmoe_combine_grad(r, None, p, p, p, p, None, None) == EINVAL  # nothing asked for
+    assert lib.semmoe_combine_grad(r, None, p, None, p, p, p, p) == EINVAL   # dtopk_w needs Y
+    assert lib.semmoe_combine_grad(r, None, p, p, p, None, p, p) == EINVAL   # dY needs topk_w
+    assert lib.semmoe_combine_grad(r, None, p + 4, p, p, p, p, p) == EINVAL  # rows on 16 bytes
+    assert lib.semmoe_combine_grad(r, None, p, p, p, p, p + 8, p) == EINVAL
+    assert lib.semmoe_dispatch_grad(r, None, None, p, None, p) == EINVAL
+    assert lib.semmoe_dispatch_grad(r, None, p, p, None, None) == EINVAL
+    assert lib.semmoe_dispatch_grad(r, None, p, p, p + 4, p) == EINVAL
+    c.d = 60
+    assert lib.semmoe_combine_grad(r, None, p, p, p, p, p, p) == ESHAPE
+    assert lib.semmoe_dispatch_grad(r, None, p, p, None, p) == ESHAPE
+    c.d, c.T = 64, 0
+    assert lib.semmoe_combine_grad(r, None, p, p, p, p, p, p) == 0  # nothing to do
+    assert lib.semmoe_dispatch_grad(r, None, p, p, None, p) == 0
+
+
+def test_ffn_gradients_refuse():
+    lib, c, p, _keep = _lib()
+    r, big = C.byref(c), 1 << 30
+    args = [p] * 7
+    assert lib.semmoe_expert_ffn_grad(r, None, 4, *args, p, big) == EINVAL  # rank >= D
+    assert lib.semmoe_expert_ffn_grad(r, None, -2, *args, p, big) == EINVAL
+    for i in range(7):
+        bad = list(args)
+        bad[i] = None
+        assert lib.semmoe_expert_ffn_grad(r, None, 0, *bad, p, big) == EINVAL
+    assert lib.semmoe_expert_ffn_grad(r, None, 0, p, p + 4, p, p, p, p, p, p, big) == EINVAL
+    need = 64 * 2 * 2 * 32 * 2
+    assert lib.semmoe_expert_ffn_grad(r, None, 0, *args, None, big) == EWORKSPACE
+    assert lib.semmoe_expert_ffn_grad(r, None, 0, *args, p, need - 1) == EWORKSPACE
+    assert lib.semmoe_shared_ffn_grad(r, None, p, p, 129, p, p, p, p, big) == ESHAPE  # more tokens than pairs
+    assert lib.semmoe_shared_ffn_grad(r, None, p, p, -1, p, p, p, p, big) == EINVAL
+    assert lib.semmoe_shared_ffn_grad(r, None, p, None, 4, p, p, p, p, big) == EINVAL
+    assert lib.semmoe_shared_ffn_grad(r, None, p, p, 4, p, p, p, p, 4 * 2 * 32 * 2 - 1) == EWORKSPACE
+    assert lib.semmoe_shared_ffn_grad(r, None, p, p, 0, p, p, p, p, 256) == 0
+
+
+def _shape(**kw):
+    v = dict(n_adapters=4, rank=8, d_in=64, d_out=32, ldx=0, ldy=0, ld_base=0, ld_out=0)
+    v.update(kw)
+    return B._CAdapterShape(*v.values())
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n_adapters=0), EINVAL), (dict(rank=0), EINVAL), (dict(d_in=-8), EINVAL), (dict(ldx=-8), EINVAL),
+    (dict(rank=12), ESHAPE), (dict(d_in=60), ESHAPE), (dict(d_out=12), ESHAPE), (dict(ld_out=36), ESHAPE),
+    (dict(rank=136), EUNSUPPORTED), (dict(n_adapters=1025), EUNSUPPORTED), (dict(d_in=(1 << 20) + 8), EUNSUPPORTED),
+])
+def test_adapter_shapes_are_refused(kw, status):
+    lib, c, p, _keep = _lib()
+    s, n = _shape(**kw), C.c_size_t(0)
+    assert lib.semmoe_adapter_workspace_bytes(C.byref(c), C.byref(s), C.byref(n)) == status
+    big = 1 << 30
+    assert lib.semmoe_adapters(C.byref(c), None, C.byref(s), p, p, p, p, p, None, None, p, p, big) == status
+    assert lib.semmoe_adapters_grad(C.byref(c), None, C.byref(s), p, p, p, p, p, p, None, None, p, None, None, p, big) == status
+
+
+def test_adapter_calls_refuse():
+    lib, c, p, _keep = _lib()
+    r, s, big = C.byref(c), _shape(), 1 << 30
+    sr = C.byref(s)
+    n = C.c_size_t(0)
+    assert lib.semmoe_adapter_workspace_bytes(r, sr, None) == EINVAL
+    assert lib.semmoe_adapter_workspace_bytes(r, None, C.byref(n)) == EINVAL
+    assert lib.semmoe_adapter_workspace_bytes(r, sr, C.byref(n)) == 0 and n.value >= 64 * 8 * 4
+    # X, order, offsets, A, B, (scale), (Y_base), Y
+    full = [p, p, p, p, p, None, None, p]
+    for i in (0, 1, 2, 3, 4, 7):
+        bad = list(full)
+        bad[i] = None
+        assert lib.semmoe_adapters(r, None, sr, *bad, p, big) == EINVAL, i
+    for i in (0, 3, 4, 6, 7):
+        bad = list(full)
+        bad[i] = p + 4
+        assert lib.semmoe_adapters(r, None, sr, *bad, p, big) == EINVAL, i
+    assert lib.semmoe_adapters(r, None, sr, *full, None, 0) == EWORKSPACE
+    assert lib.semmoe_adapters(r, None, sr, *full, p, 64 * 8 * 4 - 1) == EWORKSPACE
+    for kw in (dict(ldx=56), dict(ld_base=24), dict(ld_out=24)):
+        assert lib.semmoe_adapters(r, None, C.byref(_shape(**kw)), *full, p, big) == ESHAPE, kw
+    # in place needs one distance of rows
+    assert lib.semmoe_adapters(r, None, C.byref(_shape(ld_out=40)), p, p, p, p, p, None, p, p, p, big) == ESHAPE
+    # X, dY, order, offsets, A, B, (scale), (dX_base), dX, dA, dB
+    grad = [p, p, p, p, p, p, None, None, p, p, p]
+    for i in range(6):
+        bad = list(grad)
+        bad[i] = None
+        assert lib.semmoe_adapters_grad(r, None, sr, *bad, p, big) == EINVAL, i
+    assert lib.semmoe_adapters_grad(r, None, sr, *grad[:8], None, None, None, p, big) == EINVAL  # nothing asked for
+    assert lib.semmoe_adapters_grad(r, None, sr, *grad, p, 64) == EWORKSPACE
+    for kw in (dict(ldx=56), dict(ldy=24), dict(ld_base=56), dict(ld_out=56)):
+        assert lib.semmoe_adapters_grad(r, None, C.byref(_shape(**kw)), *grad, p, big) == ESHAPE, kw
+    assert lib.semmoe_adapter_index(r, None, p, 4, p, 0, p, p) == EINVAL
+    assert lib.semmoe_adapter_index(r, None, p, -1, p, 4, p, p) == EINVAL
+    assert lib.semmoe_adapter_index(r, None, None, 4, p, 4, p, p) == EINVAL
+    assert lib.semmoe_adapter_index(r, None, p, 4, p, 4, None, p) == EINVAL
+    assert lib.semmoe_adapter_index(r, None, p, 4, p, 1025, p, p) == EUNSUPPORTED
+    assert lib.semmoe_adapter_index(r, None, p, 65537, p, 4, p, p) == EUNSUPPORTED
+
+
+def test_binding_refuses_shapes_that_do_not_fit():
+    m = S.SemMoE(S.Config(T=8, d=16, E=1, k=1, F=8, D=1, cap=8, dtype="fp32"), allocate_workspace=False)
+    m.device = "cpu"
+    T, X, Y = 8, torch.zeros(8, 16), torch.zeros(8, 24)
+    A, Bm = torch.zeros(2, 8, 16), torch.zeros(2, 24, 8)
+    order, off = torch.zeros(T, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(S.SemMoEError):
+        m.adapters(X, order[:7], off, A, Bm, Y)
+    with pytest.raises(S.SemMoEError):
+        m.adapters(X, order, off[:2], A, Bm, Y)
+    with pytest.raises(S.SemMoEError):
+        m.adapters(X, order, off, A, Bm.transpose(1, 2), Y)
+    with pytest.raises(S.SemMoEError):
+        m.adapters(X, order, off, A, Bm, torch.zeros(7, 24))
+    with pytest.raises(ValueError):
+        m.adapters(X, order, off, A, Bm, torch.zeros(8, 25))
+    with pytest.raises(ValueError):
+        m.adapters(torch.zeros(16, 8).t(), order, off, A, Bm, Y)           # columns and not rows in one run
+    with pytest.raises(ValueError):
+        m.adapters_grad(X, torch.zeros(1, 24).expand(8, 24), order, off, A, Bm, dX=X.clone())  # a broadcast row
+    with pytest.raises(S.SemMoEError):
+        m.adapters_grad(X, Y, order, off, A, Bm, dA=torch.zeros(2, 8, 8))
+    with pytest.raises(S.SemMoEError):
+        m.adapter_index(torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), 2, order, off)
