@@ -489,10 +489,10 @@ int32_t semmoe_dispatch_grad(const semmoe_config* cfg, void* stream, const void*
  * g = W_gate[e] x, u = W_up[e] x (computed again from X_perm) and sig = 1/(1+exp(-g)):
  *   dh = W_down[e]^T dy;  dg = dh * u * sig * (1 + g (1 - sig));  du = dh * g * sig;
  *   dx = W_gate[e]^T dg + W_up[e]^T du.
- * fp32 accumulate; g, u, dg and du are rounded to the act type.  rank, offsets and weights as in semmoe_expert_ffn; rows of
+ * fp32 accumulate; dg and du are rounded to the act type.  rank, offsets and weights as in semmoe_expert_ffn; rows of
  * other ranks in dX_perm are not written.
  * dev in : X_perm[P,d] act; dY[P,d] act.  dev out: dX_perm[P,d] act (may be X_perm or dY itself).
- * ws: T*k*2F activations + 512 bytes (not covered by semmoe_workspace_bytes).
+ * ws: T*k, rounded up to a multiple of 32, rows of F floats, and T*k of 2F activations, + 768 bytes (not covered by semmoe_workspace_bytes).
  */
 int32_t semmoe_expert_ffn_grad(const semmoe_config* cfg, void* stream, int32_t rank, const void* X_perm, const void* dY,
                                const int32_t* expert_offsets, const int32_t* expert_of_phys, const void* W_gu,
@@ -500,7 +500,8 @@ int32_t semmoe_expert_ffn_grad(const semmoe_config* cfg, void* stream, int32_t r
 
 /*
  * shared_ffn_grad - the same for semmoe_shared_ffn: X[n_tokens,d], dY[n_tokens,d] -> dX[n_tokens,d] (may be X or dY
- * itself).  n_tokens <= T*k.  ws: n_tokens*2F activations + 512 bytes.
+ * itself).  n_tokens <= T*k.  ws: n_tokens, rounded up to a multiple of 32, rows of F floats, and n_tokens of 2F
+ * activations, + 768 bytes.
  */
 int32_t semmoe_shared_ffn_grad(const semmoe_config* cfg, void* stream, const void* X, const void* dY, int32_t n_tokens,
                                const void* W_gu_sh, const void* W_down_sh, void* dX, void* ws, size_t ws_bytes);

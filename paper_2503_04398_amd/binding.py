@@ -474,7 +474,7 @@ class SemMoE:
             C.byref(c), _stream(), _ptr(dX_perm), _ptr(slot_of_pair), _ptr(dX_add), _ptr(dX)))
 
     def _ffn_grad_bytes(self, rows: int) -> int:
-        return rows * 2 * self.cfg.F * (2 if self.cfg.dtype == BF16 else 4) + 512
+        return self.cfg.F * ((rows + 31) // 32 * 128 + rows * (4 if self.cfg.dtype == BF16 else 8)) + 768
 
     def expert_ffn_grad(self, rank, X_perm, dY, expert_offsets, expert_of_phys, W_gu, W_down, dX_perm):
         c = self._cfg()

@@ -72,7 +72,7 @@ static int32_t launch_dma(const GemmArgs& a, int max_rows, int blocks_per_cu, hi
 template <int MODE, int BK, int NSTAGE, int DMA_EVERY, int TJ = 4>
 static int32_t launch_w4(const GemmArgs& a, int max_rows, hipStream_t stream) {
   using C = W4Cfg<MODE, BK, NSTAGE, DMA_EVERY, TJ>;
-  const int w_rows = (MODE == kModeSwiglu) ? 2 * a.N : a.N;
+  const int w_rows = kPaired<MODE> ? 2 * a.N : a.N;
   if (a.K % BK != 0 || a.K / BK < NSTAGE) return SEMMOE_EUNSUPPORTED;
   if ((unsigned long long)w_rows * a.ldw * 2 >= (1ull << 32) || (unsigned long long)C::BT * a.ldx * 2 >= (1ull << 32))
     return SEMMOE_EUNSUPPORTED;  // per-lane row offsets are 32-bit
@@ -128,7 +128,7 @@ static int32_t launch_tail_as(GemmArgs a, int max_rows, int head_grid, hipStream
 template <int MODE, int NSTAGE>
 static int32_t launch_tail_pieces(GemmArgs a, int max_rows, int head_grid, hipStream_t stream) {
   using C = DmaCfg<MODE, 2, 2, 2, 2, 64, NSTAGE>;
-  const int w_rows = (MODE == kModeSwiglu) ? 2 * a.N : a.N;
+  const int w_rows = kPaired<MODE> ? 2 * a.N : a.N;
   if (a.K % 64 != 0 || a.K / 64 < NSTAGE) return SEMMOE_EUNSUPPORTED;
   if ((unsigned long long)w_rows * a.ldw * 2 >= (1ull << 32) || (unsigned long long)C::BT * a.ldx * 2 >= (1ull << 32))
     return SEMMOE_EUNSUPPORTED;  // per-lane row offsets are 32-bit
@@ -160,7 +160,7 @@ static int32_t launch_tail_pieces(GemmArgs a, int max_rows, int head_grid, hipSt
 template <int MODE>
 static int32_t launch_all_pieces(GemmArgs a, int max_rows, hipStream_t stream) {
   using C = DmaCfg<MODE, 2, 2, 2, 2, 64, 3>;
-  const int w_rows = (MODE == kModeSwiglu) ? 2 * a.N : a.N;
+  const int w_rows = kPaired<MODE> ? 2 * a.N : a.N;
   if (a.K % 64 != 0 || a.K / 64 < 3) return SEMMOE_EUNSUPPORTED;
   if ((unsigned long long)w_rows * a.ldw * 2 >= (1ull << 32) || (unsigned long long)C::BT * a.ldx * 2 >= (1ull << 32))
     return SEMMOE_EUNSUPPORTED;  // per-lane row offsets are 32-bit
@@ -191,7 +191,7 @@ template <int MODE, int NSTAGE = 2, int TJ = 4>
 static int32_t launch_w4_split(const GemmArgs& h, int max_rows, hipStream_t stream) {
   using CH = W4Cfg<MODE, 64, NSTAGE, 2, TJ>;
   using CP = DmaCfg<MODE, 2, 2, 2, 2, 64, 3>;
-  const int w_rows = (MODE == kModeSwiglu) ? 2 * h.N : h.N;
+  const int w_rows = kPaired<MODE> ? 2 * h.N : h.N;
   if (h.K % 64 != 0 || h.K / 64 < 3) return SEMMOE_EUNSUPPORTED;
   if ((unsigned long long)w_rows * h.ldw * 2 >= (1ull << 32) || (unsigned long long)CH::BT * h.ldx * 2 >= (1ull << 32))
     return SEMMOE_EUNSUPPORTED;  // per-lane row offsets are 32-bit
@@ -259,7 +259,7 @@ static int32_t launch_stream_as(const GemmArgs& a, int max_rows, int per_cu, hip
 template <int MODE, bool F32, int TW, int TT, int NW = 4>
 static int32_t launch_stream(const GemmArgs& a, int max_rows, int per_cu, hipStream_t stream) {
   const unsigned long long es = F32 ? 4 : 2, row_bytes = a.K * es;
-  const unsigned long long w_rows = (MODE == kModeSwiglu) ? 2ull * a.N : a.N, x_rows = StreamCfg<MODE, TW, TT>::BT;
+  const unsigned long long w_rows = kPaired<MODE> ? 2ull * a.N : a.N, x_rows = StreamCfg<MODE, TW, TT>::BT;
   if (w_rows * a.ldw * es >= (1ull << 31) || x_rows * a.ldx * es >= (1ull << 31)) return SEMMOE_EUNSUPPORTED;
   if (row_bytes % 128 == 0 && row_bytes >= 128 * NW)
     return launch_stream_as<MODE, F32, TW, TT, false, false, NW>(a, max_rows, per_cu, stream);
@@ -293,7 +293,7 @@ static int32_t launch_stream_ring_as(const GemmArgs& a, int max_rows, int few_ro
 
 template <int MODE, int TW, int TT>
 static int32_t launch_stream_ring(const GemmArgs& a, int max_rows, int few_rows, int per_cu, hipStream_t stream) {
-  const unsigned long long row_bytes = a.K * 2ull, w_rows = (MODE == kModeSwiglu) ? 2ull * a.N : a.N;
+  const unsigned long long row_bytes = a.K * 2ull, w_rows = kPaired<MODE> ? 2ull * a.N : a.N;
   if (w_rows * a.ldw * 2 >= (1ull << 31) || StreamCfg<MODE, TW, TT>::BT * 2ull * a.ldx >= (1ull << 31))
     return SEMMOE_EUNSUPPORTED;  // 32-bit offsets do not reach every row
   if (row_bytes % 128 == 0 && row_bytes >= 512) return launch_stream_ring_as<MODE, TW, TT, false>(a, max_rows, few_rows, per_cu, stream);
@@ -340,7 +340,7 @@ static int32_t launch_f32(int id, const GemmArgs& a, int max_rows, int est_rows_
   }
   const int est = est_rows_per_group < 1 ? 1 : est_rows_per_group;
   auto items = [&](int tw, int tt) {
-    return (long long)a.nq * cdiv(est, 16 * tt) * cdiv(a.N, (MODE == kModeSwiglu) ? 8 * tw : 16 * tw);
+    return (long long)a.nq * cdiv(est, 16 * tt) * cdiv(a.N, kPaired<MODE> ? 8 * tw : 16 * tw);
   };
   const long long cus = num_cu();
   int32_t st;
@@ -585,6 +585,25 @@ int32_t launch_ksplit_gemm(const void* X, const void* W, int T, int N, int d, in
   return launch_w4<kModeLogits, 64, 2, 2>(a, T * n_parts, stream);
 }
 
+// the products with gate and up rows in pairs
+template <int MODE>
+static int32_t launch_gate_up(const GemmArgs& a, int max_rows, int est_rows_per_group, int bpc, hipStream_t stream) {
+  const int id = tuning_value(SEMMOE_TUNE_GATEUP_TILE) >= 0
+                     ? tuning_value(SEMMOE_TUNE_GATEUP_TILE)
+                     : default_tile(a, max_rows, est_rows_per_group, 2 * a.N);
+  if (!split_launch(id)) return launch_bf16_tile<MODE>(id, a, max_rows, bpc, stream);
+  GemmArgs h = a;
+  h.sched_mode = 1;
+  h.sched_thr = split_threshold();
+  if (id == 22 && (tuning_value(SEMMOE_TUNE_TAIL_RING) < 0 || tuning_value(SEMMOE_TUNE_TAIL_RING) == 2)) {  // both halves in one launch
+    const int32_t sm = launch_w4_split<MODE>(h, max_rows, stream);
+    if (sm != SEMMOE_EUNSUPPORTED) return sm;
+  }
+  const int32_t st = launch_bf16_tile<MODE>(id, h, max_rows, 1, stream);
+  if (st != SEMMOE_OK) return st;
+  return launch_tail<MODE>(h, max_rows, big_tile_grid(a, max_rows, 128), stream);
+}
+
 int32_t launch_gemm(int mode, int dtype, const GemmArgs& a, int max_rows, int est_rows_per_group,
                     hipStream_t stream) {
   if (a.nq <= 0 || max_rows <= 0) return SEMMOE_OK;
@@ -593,22 +612,8 @@ int32_t launch_gemm(int mode, int dtype, const GemmArgs& a, int max_rows, int es
     const int bpc = tuning_value(SEMMOE_TUNE_BLOCKS_PER_CU);
     switch (mode) {
       case kModeLogits: return launch_bf16<kModeLogits, 2, 2, 2, 1, 64>(a, max_rows, 2, stream);  // 128 experts x 64 tokens
-      case kModeSwiglu: {
-        const int id = tuning_value(SEMMOE_TUNE_GATEUP_TILE) >= 0
-                           ? tuning_value(SEMMOE_TUNE_GATEUP_TILE)
-                           : default_tile(a, max_rows, est_rows_per_group, 2 * a.N);
-        if (!split_launch(id)) return launch_bf16_tile<kModeSwiglu>(id, a, max_rows, bpc, stream);
-        GemmArgs h = a;
-        h.sched_mode = 1;
-        h.sched_thr = split_threshold();
-        if (id == 22 && (tuning_value(SEMMOE_TUNE_TAIL_RING) < 0 || tuning_value(SEMMOE_TUNE_TAIL_RING) == 2)) {  // both halves in one launch
-          const int32_t sm = launch_w4_split<kModeSwiglu>(h, max_rows, stream);
-          if (sm != SEMMOE_EUNSUPPORTED) return sm;
-        }
-        const int32_t st = launch_bf16_tile<kModeSwiglu>(id, h, max_rows, 1, stream);
-        if (st != SEMMOE_OK) return st;
-        return launch_tail<kModeSwiglu>(h, max_rows, big_tile_grid(a, max_rows, 128), stream);
-      }
+      case kModeSwiglu: return launch_gate_up<kModeSwiglu>(a, max_rows, est_rows_per_group, bpc, stream);
+      case kModeSwigluGrad: return launch_gate_up<kModeSwigluGrad>(a, max_rows, est_rows_per_group, bpc, stream);
       default: {
         const int id = tuning_value(SEMMOE_TUNE_DOWN_TILE) >= 0
                            ? tuning_value(SEMMOE_TUNE_DOWN_TILE)
@@ -631,6 +636,7 @@ int32_t launch_gemm(int mode, int dtype, const GemmArgs& a, int max_rows, int es
   switch (mode) {
     case kModeLogits: return launch_f32<kModeLogits>(gate_id, a, max_rows, est_rows_per_group, stream);
     case kModeSwiglu: return launch_f32<kModeSwiglu>(gate_id, a, max_rows, est_rows_per_group, stream);
+    case kModeSwigluGrad: return launch_f32<kModeSwigluGrad>(gate_id, a, max_rows, est_rows_per_group, stream);
     default: return launch_f32<kModeStore>(down_id, a, max_rows, est_rows_per_group, stream);
   }
 }

@@ -1,7 +1,7 @@
 // Grouped "NT" GEMM core for gfx950:  OUT[row, n] = sum_c X[row, c] * W[g][n, c]
 // X rows (tokens / slots) are split into contiguous groups (one per expert) by an offsets array that
 // lives on the device, so the tile list is built inside the kernel and no host sync is needed.
-// Three epilogues: router logits (fp32 + bias terms), SwiGLU (gate/up pair -> hidden), plain store.
+// Epilogues: router logits (fp32 + bias terms), SwiGLU (gate/up pair -> hidden), its gradient, plain store.
 //
 // bf16 path: v_mfma_f32_32x32x16_bf16, 256 threads = 4 waves, weights as the MFMA "A" operand so a
 // lane ends up with 4 consecutive output features of one row (8-byte stores).
@@ -12,7 +12,11 @@
 
 namespace semmoe {
 
-enum GemmMode { kModeLogits = 0, kModeSwiglu = 1, kModeStore = 2 };
+// kModeSwigluGrad: the sums are gate and up as in kModeSwiglu; with dh, the gradient of silu(gate) * up, out[row] gets
+// [dgate | dup], 2N numbers.
+enum GemmMode { kModeLogits = 0, kModeSwiglu = 1, kModeStore = 2, kModeSwigluGrad = 3 };
+template <int MODE>
+constexpr bool kPaired = MODE == kModeSwiglu || MODE == kModeSwigluGrad;  // weight rows are N gate and N up rows
 
 struct GemmArgs {
   const void* X;          // [rows, K] act
@@ -20,7 +24,7 @@ struct GemmArgs {
   const void* W;          // [groups, w_rows, K] act
   size_t w_group_stride;  // elements between groups
   int ldw;
-  int N;                  // output features per row (Swiglu: F; W then has 2N rows, gate rows first)
+  int N;                  // output features per row (Swiglu, SwigluGrad: F; W then has 2N rows, gate rows first)
   int K;
   const int32_t* offsets; // device [>= q_lo+nq+1] row offsets per physical group, or nullptr
   int q_lo, nq;           // groups handled
@@ -28,7 +32,7 @@ struct GemmArgs {
   const int32_t* group_to_weight;  // physical group -> weight index (nullptr: identity)
   void* out;              // Logits: f32 [rows, N]; else act [rows, ldo]
   int ldo;
-  const float* b_g;       // Logits only (nullable)
+  const float* b_g;       // Logits: bias (nullable); SwigluGrad: dh in fours (quad_at)
   const int32_t* token_class;
   const float* class_bias;
   int n_classes;
@@ -49,6 +53,7 @@ struct GemmArgs {
   // Groups of more than rows_min rows, and of at most rows_max where that is set, make up the tile list (a launch whose
   // workgroups run two kernels one after the other, one for the small groups and one for the large).
   int rows_min, rows_max;
+  int sched_reverse;      // the tile list from its end (gemm_nn.hpp): the weights that the product before read last come first
 };
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
@@ -56,6 +61,24 @@ typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 
 __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+
+// fp32 sums between two products: blocks of 32 rows, in a block the rows of four consecutive features behind one another
+// ([rows / 32][N / 4][32][4]).  A lane's four of an accumulator are 16 bytes, the next lanes' rows follow, where the sums are
+// written and where they are read, whatever the tiles of the two are.  As rows of N floats the reads of the gradient's
+// epilogue touch 32 rows each (16 experts of 1300 rows, d 2048, F 768: 180 us, 155 without the reads).
+__device__ __forceinline__ size_t quad_at(int N, int row, int feat) {
+  return (size_t(row >> 5) * N + feat) * 32 + (row & 31) * 4;
+}
+
+// y = silu(g) u:  dg = dh u sig (1 + g (1 - sig)),  du = dh g sig,  sig = 1 / (1 + exp(-g)).  With one exp2 and one reciprocal;
+// where exp2 overflows sig is 0, and so are both (F32: with expf and a division).
+template <bool F32 = false>
+__device__ __forceinline__ void swiglu_grad(float dh, float g, float u, float* dg, float* du) {
+  const float sig = F32 ? 1.0f / (1.0f + expf(-g))
+                        : __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * g));
+  *dg = dh * u * sig * (1.0f + g * (1.0f - sig));
+  *du = dh * g * sig;
+}
 
 // SIZED: the list is cut by rows_min / rows_max.  Kernels that take every group don't read the two: they stand at the
 // end of the arguments, and a short launch waits for them (gate/up on 300 rows of d 2048, F 768: 18.9 us with the two
@@ -210,52 +233,82 @@ template <int MODE, int NWF, int NWT, int TF, int TT>
 __device__ __forceinline__ void store_tile_via_lds(f32x16_t (&acc)[TF][TT], unsigned char* lds, const GemmArgs& a,
                                                    int row_lo, int n_tok, int f0, int wf, int wt) {
   constexpr int BT = NWT * TT * 32;
-  constexpr int FEAT = (MODE == kModeSwiglu) ? NWF * TF * 16 : NWF * TF * 32;
+  constexpr int FEAT = kPaired<MODE> ? NWF * TF * 16 : NWF * TF * 32;
   constexpr int CPR = FEAT / 8;                   // 16-byte chunks per output row
   constexpr int MASK = (CPR < 32 ? CPR : 32) - 1; // swizzle range
   constexpr int RB = FEAT * 2;
   constexpr int kThreads = 64 * NWF * NWT;
   const int lane = threadIdx.x & 63;
   const int tok_in = lane & 31, half = lane >> 5;
+  bf16_t* out = static_cast<bf16_t*>(a.out);
+  if constexpr (MODE == kModeSwigluGrad) {
+    // gate and up give way to their gradients; a lane's four features of a token are 16 bytes of dh
 #pragma unroll
-  for (int j = 0; j < TT; ++j) {
-    const int t = (wt * TT + j) * 32 + tok_in;
-    unsigned char* rowp = lds + t * RB + half * 8;
-    if constexpr (MODE == kModeSwiglu) {
+    for (int j = 0; j < TT; ++j) {
+      const int t = (wt * TT + j) * 32 + tok_in;
+      const int row = row_lo + min(t, n_tok - 1);
 #pragma unroll
       for (int i = 0; i < TF; i += 2) {
+        f32x4_t dh[4];
 #pragma unroll
         for (int g4 = 0; g4 < 4; ++g4) {
-          const int chunk = (wf * (TF / 2) + i / 2) * 4 + g4;
-          const float h0 = silu_mul(acc[i][j][g4 * 4 + 0], acc[i + 1][j][g4 * 4 + 0]);
-          const float h1 = silu_mul(acc[i][j][g4 * 4 + 1], acc[i + 1][j][g4 * 4 + 1]);
-          const float h2 = silu_mul(acc[i][j][g4 * 4 + 2], acc[i + 1][j][g4 * 4 + 2]);
-          const float h3 = silu_mul(acc[i][j][g4 * 4 + 3], acc[i + 1][j][g4 * 4 + 3]);
-          *reinterpret_cast<uint2*>(rowp + ((chunk ^ (t & MASK)) * 16)) =
-              make_uint2(pack_bf16x2(h0, h1), pack_bf16x2(h2, h3));
+          const int feat = f0 + (wf * (TF / 2) + i / 2) * 32 + g4 * 8 + half * 4;
+          dh[g4] = *reinterpret_cast<const f32x4_t*>(a.b_g + quad_at(a.N, row, min(feat, a.N - 4)));
         }
-      }
-    } else {
 #pragma unroll
-      for (int i = 0; i < TF; ++i) {
-#pragma unroll
-        for (int g4 = 0; g4 < 4; ++g4) {
-          const int chunk = (wf * TF + i) * 4 + g4;
-          *reinterpret_cast<uint2*>(rowp + ((chunk ^ (t & MASK)) * 16)) =
-              make_uint2(pack_bf16x2(acc[i][j][g4 * 4 + 0], acc[i][j][g4 * 4 + 1]),
-                         pack_bf16x2(acc[i][j][g4 * 4 + 2], acc[i][j][g4 * 4 + 3]));
+        for (int r = 0; r < 16; ++r) {
+          float dg, du;
+          swiglu_grad(dh[r >> 2][r & 3], acc[i][j][r], acc[i + 1][j][r], &dg, &du);
+          acc[i][j][r] = dg;
+          acc[i + 1][j][r] = du;
         }
       }
     }
   }
-  __syncthreads();
-  bf16_t* out = static_cast<bf16_t*>(a.out);
-  for (int idx = threadIdx.x; idx < BT * CPR; idx += kThreads) {
-    const int row = idx / CPR, c = idx % CPR;
-    const int feat = f0 + c * 8;
-    if (row < n_tok && feat < a.N) {
-      const uint4 v = *reinterpret_cast<const uint4*>(lds + row * RB + ((c ^ (row & MASK)) * 16));
-      *reinterpret_cast<uint4*>(out + (size_t(row_lo) + row) * a.ldo + feat) = v;
+  constexpr int kParts = MODE == kModeSwigluGrad ? 2 : 1;  // gates' half of the output rows, then the ups'
+#pragma unroll
+  for (int part = 0; part < kParts; ++part) {
+    if (part) __syncthreads();  // the half before has been read
+#pragma unroll
+    for (int j = 0; j < TT; ++j) {
+      const int t = (wt * TT + j) * 32 + tok_in;
+      unsigned char* rowp = lds + t * RB + half * 8;
+      if constexpr (MODE == kModeSwiglu) {
+#pragma unroll
+        for (int i = 0; i < TF; i += 2) {
+#pragma unroll
+          for (int g4 = 0; g4 < 4; ++g4) {
+            const int chunk = (wf * (TF / 2) + i / 2) * 4 + g4;
+            const float h0 = silu_mul(acc[i][j][g4 * 4 + 0], acc[i + 1][j][g4 * 4 + 0]);
+            const float h1 = silu_mul(acc[i][j][g4 * 4 + 1], acc[i + 1][j][g4 * 4 + 1]);
+            const float h2 = silu_mul(acc[i][j][g4 * 4 + 2], acc[i + 1][j][g4 * 4 + 2]);
+            const float h3 = silu_mul(acc[i][j][g4 * 4 + 3], acc[i + 1][j][g4 * 4 + 3]);
+            *reinterpret_cast<uint2*>(rowp + ((chunk ^ (t & MASK)) * 16)) =
+                make_uint2(pack_bf16x2(h0, h1), pack_bf16x2(h2, h3));
+          }
+        }
+      } else {
+        constexpr int STEP = MODE == kModeSwigluGrad ? 2 : 1;  // MFMA tiles alternate between the two halves
+#pragma unroll
+        for (int i = 0; i < TF; i += STEP) {
+#pragma unroll
+          for (int g4 = 0; g4 < 4; ++g4) {
+            const int chunk = (wf * (TF / STEP) + i / STEP) * 4 + g4;
+            const f32x16_t& c = acc[i + part][j];
+            *reinterpret_cast<uint2*>(rowp + ((chunk ^ (t & MASK)) * 16)) =
+                make_uint2(pack_bf16x2(c[g4 * 4 + 0], c[g4 * 4 + 1]), pack_bf16x2(c[g4 * 4 + 2], c[g4 * 4 + 3]));
+          }
+        }
+      }
+    }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < BT * CPR; idx += kThreads) {
+      const int row = idx / CPR, c = idx % CPR;
+      const int feat = f0 + c * 8;
+      if (row < n_tok && feat < a.N) {
+        const uint4 v = *reinterpret_cast<const uint4*>(lds + row * RB + ((c ^ (row & MASK)) * 16));
+        *reinterpret_cast<uint4*>(out + (size_t(row_lo) + row) * a.ldo + part * a.N + feat) = v;
+      }
     }
   }
 }
@@ -274,7 +327,7 @@ struct Bf16Cfg {
   static constexpr int BT = NWT * TT * 32;  // token rows per tile
   static constexpr int LDK = BK + 8;        // LDS row stride in elements: conflict-free 16-byte reads
   static constexpr int CPR = BK / 8;        // 16-byte chunks per tile row
-  static constexpr int FEAT = (MODE == kModeSwiglu) ? BW / 2 : BW;  // output features per tile
+  static constexpr int FEAT = kPaired<MODE> ? BW / 2 : BW;  // output features per tile
   static constexpr int W_CHUNKS = BW * CPR / kThreads;
   static constexpr int X_CHUNKS = BT * CPR / kThreads;
   static constexpr int kStageElems = (BW + BT) * LDK;
@@ -282,7 +335,7 @@ struct Bf16Cfg {
   static constexpr size_t kOutBytes = size_t(BT) * FEAT * 2;  // the output tile is staged in the ring's place
   static constexpr size_t kTileBytes = kRingBytes > kOutBytes ? kRingBytes : kOutBytes;
   static constexpr size_t kLdsBytes = kTileBytes + 520 * 4;
-  static_assert(MODE != kModeSwiglu || TF % 2 == 0, "gate/up tiles come in pairs");
+  static_assert(!kPaired<MODE> || TF % 2 == 0, "gate/up tiles come in pairs");
   static_assert((BW * CPR) % kThreads == 0 && (BT * CPR) % kThreads == 0, "loader shape");
   static_assert(BK % 16 == 0, "k-steps of 16");
 };
@@ -323,7 +376,7 @@ __global__ __launch_bounds__(64 * NWF * NWT, MINW) void gemm_bf16_kernel(GemmArg
     for (int i = 0; i < C::W_CHUNKS; ++i) {
       const int lr = lr0 + i * LR_STEP;
       int grow;
-      if constexpr (MODE == kModeSwiglu) {
+      if constexpr (kPaired<MODE>) {
         const int w_of = lr / (TF * 32), tf = (lr / 32) % TF, fr = lr & 31;
         const int feat = min(f0 + (w_of * (TF / 2) + tf / 2) * 32 + fr, a.N - 1);
         grow = (tf & 1) * a.N + feat;
@@ -485,7 +538,7 @@ struct DmaCfg {
   static constexpr int IPW = IPS / NW;     // ... per wave
   static constexpr int RPB = 256 / RB;     // rows per 256 bytes of bank space
   static constexpr int kStageBytes = ROWS * RB;
-  static constexpr int FEAT = (MODE == kModeSwiglu) ? BW / 2 : BW;
+  static constexpr int FEAT = kPaired<MODE> ? BW / 2 : BW;
   static constexpr int KS = BK / 16;
   static constexpr size_t kRingBytes = size_t(NSTAGE) * kStageBytes;
   static constexpr size_t kOutBytes = size_t(BT) * FEAT * 2;  // the output tile is staged in the ring's place
@@ -495,7 +548,7 @@ struct DmaCfg {
   static_assert(IPS % NW == 0, "instructions divide over the waves");
   static_assert(NSTAGE >= 2 && NSTAGE <= 6, "ring depth");
   static_assert((NSTAGE - 1) * IPW < 64, "vmcnt range");
-  static_assert(MODE != kModeSwiglu || TF % 2 == 0, "gate/up tiles come in pairs");
+  static_assert(!kPaired<MODE> || TF % 2 == 0, "gate/up tiles come in pairs");
 };
 
 // returns the number of tiles in the list
@@ -541,7 +594,7 @@ __device__ __forceinline__ int gemm_bf16_dma_body(const GemmArgs& a, unsigned ch
       src_chunk[i] = c;
       if (sr < C::BW) {
         int grow;
-        if constexpr (MODE == kModeSwiglu) {
+        if constexpr (kPaired<MODE>) {
           const int w_of = sr / (TF * 32), tf = (sr / 32) % TF, fr = sr & 31;
           const int feat = min(f0 + (w_of * (TF / 2) + tf / 2) * 32 + fr, a.N - 1);
           grow = (tf & 1) * a.N + feat;

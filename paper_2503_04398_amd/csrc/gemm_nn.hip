@@ -23,6 +23,53 @@ static int32_t launch_nn_ring(const GemmArgs& a, int max_rows, int per_cu, hipSt
   return SEMMOE_OK;
 }
 
+// more slices than the ring holds, and a table that fits beside the ring
+template <int TI, int TJ, int NSTAGE>
+static bool nn_w4_fits(const GemmArgs& a) {
+  using C = NnW4Cfg<TI, TJ, NSTAGE>;
+  DeviceInfo d;
+  if (cdiv(a.K, 64) <= NSTAGE || device_info(&d) != SEMMOE_OK) return false;
+  // per-lane offsets are 32-bit
+  return C::lds_bytes(a.nq) <= size_t(d.max_lds) && 128ull * a.ldw < (1ull << 31) && 2ull * C::BT * a.ldx < (1ull << 31);
+}
+
+template <int MODE, int TI, int TJ, int NSTAGE, int DMA_EVERY>
+static int32_t launch_nn_w4(const GemmArgs& a, int max_rows, hipStream_t s) {
+  using C = NnW4Cfg<TI, TJ, NSTAGE>;
+  auto kern = gemm_nn_w4_kernel<MODE, TI, TJ, NSTAGE, DMA_EVERY>;
+  static std::atomic<uint64_t> allowed{0};
+  const int32_t st = allow_max_dynamic_lds(&allowed, reinterpret_cast<const void*>(kern));
+  if (st != SEMMOE_OK) return st;
+  const long long bound = (long long)(max_rows / C::BT + a.nq) * cdiv(a.N, C::BW);
+  hipLaunchKernelGGL(kern, dim3(nn_grid(bound, 1)), dim3(256), C::lds_bytes(a.nq), s, a);
+  SEMMOE_LAUNCH_CHECK();
+  return SEMMOE_OK;
+}
+
+template <int MODE, int TJ, int NSTAGE>
+static int32_t launch_nn_split(const GemmArgs& a, int max_rows, hipStream_t s) {
+  using CH = NnW4Cfg<4, TJ, NSTAGE>;
+  using CP = NnW4Cfg<2, 2, 3>;
+  auto kern = gemm_nn_split_kernel<MODE, TJ, NSTAGE>;
+  static std::atomic<uint64_t> allowed{0};
+  const int32_t st = allow_max_dynamic_lds(&allowed, reinterpret_cast<const void*>(kern));
+  if (st != SEMMOE_OK) return st;
+  const long long bound = (long long)(max_rows / CH::BT + a.nq) * cdiv(a.N, CH::BW);
+  const int grid = nn_grid(bound, 1);
+  GemmArgs h = a;
+  h.sched_mode = 1;
+  h.sched_thr = 8;
+  GemmArgs t = h;
+  t.sched_mode = 2;
+  t.sched_g = grid;
+  t.sched_sub_t = CH::BT / CP::BT;
+  t.sched_sub_f = CH::BW / CP::BW;
+  const size_t lds = CH::lds_bytes(a.nq) > CP::lds_bytes(a.nq) ? CH::lds_bytes(a.nq) : CP::lds_bytes(a.nq);
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, s, h, t);
+  SEMMOE_LAUNCH_CHECK();
+  return SEMMOE_OK;
+}
+
 template <int MODE, int TT>
 static int32_t launch_nn_f32(const GemmArgs& a, int max_rows, hipStream_t s) {
   const long long bound = (long long)(max_rows / (32 * TT) + a.nq) * cdiv(a.N, 128);
@@ -32,16 +79,51 @@ static int32_t launch_nn_f32(const GemmArgs& a, int max_rows, hipStream_t s) {
 }
 
 template <int MODE>
-static int32_t launch_nn(int dtype, const GemmArgs& a, int max_rows, int est, hipStream_t s) {
-  if (dtype == SEMMOE_FP32) return est <= 32 ? launch_nn_f32<MODE, 1>(a, max_rows, s) : launch_nn_f32<MODE, 2>(a, max_rows, s);
-  if (est < 96) return launch_nn_ring<MODE, 2, 2, 2, 1, 64, 3>(a, max_rows, 2, s);
-  return launch_nn_ring<MODE, 2, 4, 4, 2, 64, 2>(a, max_rows, 1, s);
+static int32_t launch_nn_f32(const GemmArgs& a, int max_rows, int est, hipStream_t s) {
+  return est <= 32 ? launch_nn_f32<MODE, 1>(a, max_rows, s) : launch_nn_f32<MODE, 2>(a, max_rows, s);
+}
+
+// Tile shapes.  Means of rows an expert, 8 shapes of 1 to 128 experts (d 1024 to 7168, F 512 to 2880), groups spread lognormally
+// by 0.3; FFN gradients in us with one of the two products as 128 x 64 / 128 x 128 / 256 x 128 and pieces / 256 x 256 and pieces:
+//   * 128 columns x 64 tokens, ring of 4, while such tiles have a compute unit each: dh of 8 experts, d 7168, F 2048, 90 rows
+//     353 / 365 / 395 / 442, 130 rows 404 / 377; one expert of these, 900 rows 182 / 190, 1300 rows 317 / 278
+//   * 128 x 128 up to 80 rows, where the weights' stream is the time (128 experts of 40, d 2048, F 768: 414 / 407 / 411 / 427),
+//     and beyond while they have one each (16 experts of 90, d 4096, F 1536, dh: 279 / 263 / 283 / 312; 130 rows 310 / 327 / 314 / 341)
+//   * 256 x 256 from 192 rows on with five quarters of a round of them (8 experts of 400, d 7168, dx: 741 / 655 / 620 / 604; 600 rows of d
+//     2880, 273 tiles: 630 / 531 / 511 / 528), or, with groups of 1024 rows and more, three fifths (16 experts of 1300, d 2048, F
+//     768, dh: 456 / 437 / 428 / 422); 256 x 128 else
+// Shapes whose K is shorter than a ring, or with more groups than the tables hold, take 128 x 64 tiles with a barrier a slice.
+template <int MODE>
+static int32_t launch_nn_bf16(const GemmArgs& a, int max_rows, int est, hipStream_t s) {
+  DeviceInfo d;
+  const int32_t st = device_info(&d);
+  if (st != SEMMOE_OK) return st;
+  const long long cus = d.num_cu;
+  // The mean is that of all experts.  A rank that an affinity placement loads has some twice as many rows: one of 20865 where 8192 are
+  // expected 400 us as 256 x 256 tiles, 415 as 256 x 128.
+  if (a.offsets && (long long)a.nq * (est + 1) < max_rows) est *= 2;
+  // a ragged group's last tile is half full in the mean; times 100
+  auto tiles = [&](int bw, int bt) {
+    const long long rows = !a.offsets ? 100ll * cdiv(est, bt) : (est * 2 <= bt ? 100ll : 100ll * est / bt + 50);
+    return a.nq * rows * cdiv(a.N, bw);
+  };
+  if (tiles(128, 64) <= 100 * cus && nn_w4_fits<2, 1, 4>(a)) return launch_nn_w4<MODE, 2, 1, 4, 1>(a, max_rows, s);
+  if (nn_w4_fits<2, 2, 3>(a)) {
+    if (est < 80 || tiles(128, 128) <= 110 * cus) return launch_nn_w4<MODE, 2, 2, 3, 1>(a, max_rows, s);
+    const long long big = tiles(256, 256);
+    if (est >= 192 && (big >= 125 * cus || (est >= 1024 && big >= 60 * cus)) && nn_w4_fits<4, 4, 2>(a))
+      return launch_nn_split<MODE, 4, 2>(a, max_rows, s);
+    if (nn_w4_fits<4, 2, 3>(a)) return launch_nn_split<MODE, 2, 3>(a, max_rows, s);
+    return launch_nn_w4<MODE, 2, 2, 3, 1>(a, max_rows, s);
+  }
+  return launch_nn_ring<MODE, 2, 2, 2, 1, 64, 3>(a, max_rows, 2, s);
 }
 
 int32_t launch_gemm_nn(int mode, int dtype, const GemmArgs& a, int max_rows, int est, hipStream_t s) {
   if (a.nq <= 0 || max_rows <= 0) return SEMMOE_OK;
   if (a.nq > 512) return SEMMOE_EUNSUPPORTED;
-  return mode == kNnSwigluGrad ? launch_nn<kNnSwigluGrad>(dtype, a, max_rows, est, s) : launch_nn<kNnStore>(dtype, a, max_rows, est, s);
+  if (dtype == SEMMOE_FP32) return mode == kNnSums ? launch_nn_f32<kNnSums>(a, max_rows, est, s) : launch_nn_f32<kNnStore>(a, max_rows, est, s);
+  return mode == kNnSums ? launch_nn_bf16<kNnSums>(a, max_rows, est, s) : launch_nn_bf16<kNnStore>(a, max_rows, est, s);
 }
 
 }  // namespace semmoe

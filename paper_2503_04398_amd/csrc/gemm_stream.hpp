@@ -30,12 +30,12 @@ template <int MODE, int TW, int TT, int NWAVES = 4>
 struct StreamCfg {
   static constexpr int NW = NWAVES, kThreads = 64 * NW;
   static constexpr int BT = 16 * TT;
-  static constexpr int FEAT = (MODE == kModeSwiglu) ? TW * 8 : TW * 16;
+  static constexpr int FEAT = kPaired<MODE> ? TW * 8 : TW * 16;
   static constexpr int kStgWave = (TW + TT) * 2048;  // one step of one wave
   static constexpr int kRedBytes = NW * TW * TT * 1024;
   static constexpr int kTileBytes = NW * kStgWave > kRedBytes ? NW * kStgWave : kRedBytes;  // the two share their place
   static size_t lds_bytes(int nq) { return size_t(kTileBytes) + (size_t(nq) * 4 + 1) * 4; }  // + tile prefix + group table
-  static_assert(MODE != kModeSwiglu || TW % 2 == 0, "gate and up tiles in pairs");
+  static_assert(!kPaired<MODE> || TW % 2 == 0, "gate and up tiles in pairs");
 };
 
 // 16 bytes at uniform base + per-lane offset + uniform offset.  A buffer load and not a plain one: whether it passes by
@@ -150,8 +150,8 @@ __device__ __forceinline__ void gemm_stream_body(const GemmArgs& a, unsigned cha
 #pragma unroll
       for (int i = 0; i < 2 * TW; ++i) {
         const int wt = i >> 1;
-        const int row = ((MODE == kModeSwiglu) ? (wt >> 1) * 16 : wt * 16) + (i & 1) * 8;
-        wb[i] = *reinterpret_cast<const u32x4_t*>(((MODE == kModeSwiglu && (wt & 1)) ? ubase : wbase) +
+        const int row = (kPaired<MODE> ? (wt >> 1) * 16 : wt * 16) + (i & 1) * 8;
+        wb[i] = *reinterpret_cast<const u32x4_t*>(((kPaired<MODE> && (wt & 1)) ? ubase : wbase) +
                                                   (min(w_first + off_t(row) * w_ld + w_lane, w_last) + lane_at));
       }
 #pragma unroll
@@ -164,8 +164,8 @@ __device__ __forceinline__ void gemm_stream_body(const GemmArgs& a, unsigned cha
 #pragma unroll
         for (int i = 0; i < 2 * TW; ++i) {
           const int wt = i >> 1;  // gate and up tiles alternate
-          const int row = ((MODE == kModeSwiglu) ? (wt >> 1) * 16 : wt * 16) + (i & 1) * 8;
-          wb[i] = stream_load<decltype(nt)::value>((MODE == kModeSwiglu && (wt & 1)) ? ur : wr,
+          const int row = (kPaired<MODE> ? (wt >> 1) * 16 : wt * 16) + (i & 1) * 8;
+          wb[i] = stream_load<decltype(nt)::value>((kPaired<MODE> && (wt & 1)) ? ur : wr,
                                                    min(w_first + uint32_t(row) * w_ld + w_lane, w_last) + lane_at, at);
         }
       };
@@ -215,13 +215,24 @@ __device__ __forceinline__ void gemm_stream_body(const GemmArgs& a, unsigned cha
       for (int w = 1; w < NW; ++w) v += red[((w * TW + i) * TT + j) * 64 + lane];
       return v;
     };
-    constexpr int FT = (MODE == kModeSwiglu) ? TW / 2 : TW;  // 16-feature tiles of the output
+    constexpr int FT = kPaired<MODE> ? TW / 2 : TW;  // 16-feature tiles of the output
     for (int unit = wave; unit < FT * TT; unit += NW) {
       const int j = unit / FT, p = unit - j * FT;
       const int tok = j * 16 + l16, feat = r.f0 + p * 16 + g * 4;
       if (j * 16 >= r.n_tok) break;
-      f32x4_t v;
-      if constexpr (MODE == kModeSwiglu) {
+      f32x4_t v, v2;  // v2: dup of kModeSwigluGrad
+      if constexpr (MODE == kModeSwigluGrad) {
+        const f32x4_t gt = total_of(2 * p, j), up = total_of(2 * p + 1, j);
+        if (tok >= r.n_tok || feat >= a.N) continue;
+        const f32x4_t dh = *reinterpret_cast<const f32x4_t*>(a.b_g + quad_at(a.N, r.row_lo + tok, feat));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float dg, du;
+          swiglu_grad<F32>(dh[e], gt[e], up[e], &dg, &du);
+          v[e] = dg;
+          v2[e] = du;
+        }
+      } else if constexpr (MODE == kModeSwiglu) {
         const f32x4_t gt = total_of(2 * p, j), up = total_of(2 * p + 1, j);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = F32 ? gt[e] / (1.0f + expf(-gt[e])) * up[e] : silu_mul(gt[e], up[e]);
@@ -244,9 +255,14 @@ __device__ __forceinline__ void gemm_stream_body(const GemmArgs& a, unsigned cha
           }
       } else if constexpr (F32) {
         *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + row * a.ldo + feat) = v;
+        if constexpr (MODE == kModeSwigluGrad)
+          *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + row * a.ldo + a.N + feat) = v2;
       } else {
         *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + row * a.ldo + feat) =
             make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        if constexpr (MODE == kModeSwigluGrad)
+          *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + row * a.ldo + a.N + feat) =
+              make_uint2(pack_bf16x2(v2[0], v2[1]), pack_bf16x2(v2[2], v2[3]));
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

@@ -83,7 +83,7 @@ struct W4Cfg {
   static constexpr int RPB = 256 / RB;     // rows per 256 bytes of bank space
   static constexpr int KS = BK / 16;       // k-steps (MFMA depth 16) per slice
   static constexpr int kStageBytes = ROWS * RB;
-  static constexpr int FEAT = (MODE == kModeSwiglu) ? BW / 2 : BW;
+  static constexpr int FEAT = kPaired<MODE> ? BW / 2 : BW;
   static constexpr size_t kRingBytes = size_t(NSTAGE) * kStageBytes;
   static constexpr int NB = TJ == 4 ? 2 : 1;           // blocks of 32 features that an epilogue pass stages
   static constexpr int kStgRow = NB * 64 + 16;         // staging row: 32*NB bf16 + pad against bank conflicts
@@ -202,7 +202,7 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
     auto w_off = [&](int sr) __attribute__((always_inline)) {  // weight row sr of the tile
       const int c = d_pos ^ ((sr / C::RPB) % C::CPR);
       int grow;
-      if constexpr (MODE == kModeSwiglu) {
+      if constexpr (kPaired<MODE>) {
         // quadrant wf: MFMA tiles 0,2 are gate rows, 1,3 the matching up rows, of two blocks of 32 features
         const int tf = (sr >> 5) & 3, fr = sr & 31;
         const int feat = min(t.f0 + ((sr >> 7) * 2 + (tf >> 1)) * 32 + fr, a.N - 1);
@@ -409,8 +409,19 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
       }
       continue;
     }
-    constexpr int NB = C::NB;
-    constexpr int kPasses = ((MODE == kModeSwiglu) ? 2 : 4) / NB;  // 32*NB output features per pass
+    constexpr int NB = MODE == kModeSwigluGrad ? 1 : C::NB;  // its two results and dh take the registers of a second block
+    constexpr int kPasses = (kPaired<MODE> ? 2 : 4) / NB;  // 32*NB output features per pass
+    // kModeSwigluGrad: a lane's part of dh for the pass to come, four features of a token 16 bytes
+    f32x4_t dh[4];
+    auto fetch_dh = [&](int j, int h) __attribute__((always_inline)) {
+      const int row = t.row_lo + min((j * 2 + wt) * 32 + tok_in, t.n_tok - 1);
+      int col = t.f0 + wf * 64 + h * NB * 32 + half * 4;
+      asm volatile("" : "+v"(col));  // addresses kept from pass to pass would be spilled
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4)
+        dh[g4] = *reinterpret_cast<const f32x4_t*>(a.b_g + quad_at(a.N, row, min(col + g4 * 8, a.N - 4)));
+    };
+    if constexpr (MODE == kModeSwigluGrad) fetch_dh(0, 0);
 #pragma unroll
     for (int j = 0; j < TJ; ++j) {
       if (j >= nj) break;
@@ -420,7 +431,7 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
         // here: left alone, the compiler moves all 256 of them to vector registers at the end of the K loop, and
         // the register pressure of that spills the load offsets inside the K loop.
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (MODE == kModeSwiglu) {
+        if constexpr (kPaired<MODE>) {
 #pragma unroll
           for (int i = 0; i < 2 * NB; ++i) asm volatile("" : "+a"(acc[2 * NB * h + i][j]));
         } else {
@@ -428,39 +439,66 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
           for (int i = 0; i < NB; ++i) asm volatile("" : "+a"(acc[NB * h + i][j]));
         }
         unsigned char* wp = stg + tok_in * C::kStgRow + half * 8;
+        constexpr int kParts = MODE == kModeSwigluGrad ? 2 : 1;  // gates' half of the output rows, then the ups'
+        uint2 dgu[2][NB][4];  // kModeSwigluGrad: the pass's dgate and dup, rounded
+        if constexpr (MODE == kModeSwigluGrad) {
+          static_assert(NB == 1, "dh of a pass");
+          f32x4_t dh_now[4];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {  // block of 32 features inside the pass
+          for (int g4 = 0; g4 < 4; ++g4) dh_now[g4] = dh[g4];
+          fetch_dh(h + 1 < kPasses ? j : j + 1, h + 1 < kPasses ? h + 1 : 0);  // past the last pass: some row again
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int g4 = 0; g4 < 4; ++g4) {
-            uint2 v;
-            if constexpr (MODE == kModeSwiglu) {
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
               const f32x16_t& g = acc[2 * (NB * h + b)][j];
               const f32x16_t& u = acc[2 * (NB * h + b) + 1][j];
-              v.x = cvt_pk_bf16(silu_mul_fast(g[g4 * 4 + 0], u[g4 * 4 + 0]), silu_mul_fast(g[g4 * 4 + 1], u[g4 * 4 + 1]));
-              v.y = cvt_pk_bf16(silu_mul_fast(g[g4 * 4 + 2], u[g4 * 4 + 2]), silu_mul_fast(g[g4 * 4 + 3], u[g4 * 4 + 3]));
-            } else {
-              const f32x16_t& c = acc[NB * h + b][j];
-              v.x = cvt_pk_bf16(c[g4 * 4 + 0], c[g4 * 4 + 1]);
-              v.y = cvt_pk_bf16(c[g4 * 4 + 2], c[g4 * 4 + 3]);
-            }
-            *reinterpret_cast<uint2*>(wp + (b * 4 + g4) * 16) = v;
-          }
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_wave_barrier();
-        constexpr int kLpr = 4 * NB, kRpr = 64 / kLpr;  // lanes per staged row, rows per read-back
-        const int b_row = lane / kLpr, b_chunk = lane % kLpr;
-        const int feat = t.f0 + (MODE == kModeSwiglu ? wf * 64 : wf * 128) + h * NB * 32 + b_chunk * 8;
+              float dg[4], du[4];
 #pragma unroll
-        for (int p = 0; p < 32 / kRpr; ++p) {
-          const int sr = p * kRpr + b_row;
-          const int row = (j * 2 + wt) * 32 + sr;
-          const uint4 v = *reinterpret_cast<const uint4*>(stg + sr * C::kStgRow + b_chunk * 16);
-          if (row < t.n_tok && feat < a.N)
-            *reinterpret_cast<uint4*>(out + (size_t(t.row_lo) + row) * a.ldo + feat) = v;
+              for (int e = 0; e < 4; ++e) swiglu_grad(dh_now[g4][e], g[g4 * 4 + e], u[g4 * 4 + e], &dg[e], &du[e]);
+              dgu[0][b][g4] = make_uint2(cvt_pk_bf16(dg[0], dg[1]), cvt_pk_bf16(dg[2], dg[3]));
+              dgu[1][b][g4] = make_uint2(cvt_pk_bf16(du[0], du[1]), cvt_pk_bf16(du[2], du[3]));
+            }
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {  // block of 32 features inside the pass
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
+              uint2 v;
+              if constexpr (MODE == kModeSwigluGrad) {
+                v = dgu[part][b][g4];
+              } else if constexpr (MODE == kModeSwiglu) {
+                const f32x16_t& g = acc[2 * (NB * h + b)][j];
+                const f32x16_t& u = acc[2 * (NB * h + b) + 1][j];
+                v.x = cvt_pk_bf16(silu_mul_fast(g[g4 * 4 + 0], u[g4 * 4 + 0]), silu_mul_fast(g[g4 * 4 + 1], u[g4 * 4 + 1]));
+                v.y = cvt_pk_bf16(silu_mul_fast(g[g4 * 4 + 2], u[g4 * 4 + 2]), silu_mul_fast(g[g4 * 4 + 3], u[g4 * 4 + 3]));
+              } else {
+                const f32x16_t& c = acc[NB * h + b][j];
+                v.x = cvt_pk_bf16(c[g4 * 4 + 0], c[g4 * 4 + 1]);
+                v.y = cvt_pk_bf16(c[g4 * 4 + 2], c[g4 * 4 + 3]);
+              }
+              *reinterpret_cast<uint2*>(wp + (b * 4 + g4) * 16) = v;
+            }
+          }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          __builtin_amdgcn_wave_barrier();
+          constexpr int kLpr = 4 * NB, kRpr = 64 / kLpr;  // lanes per staged row, rows per read-back
+          const int b_row = lane / kLpr, b_chunk = lane % kLpr;
+          const int feat = t.f0 + (kPaired<MODE> ? wf * 64 : wf * 128) + h * NB * 32 + b_chunk * 8;
+#pragma unroll
+          for (int p = 0; p < 32 / kRpr; ++p) {
+            const int sr = p * kRpr + b_row;
+            const int row = (j * 2 + wt) * 32 + sr;
+            const uint4 v = *reinterpret_cast<const uint4*>(stg + sr * C::kStgRow + b_chunk * 16);
+            if (row < t.n_tok && feat < a.N)
+              *reinterpret_cast<uint4*>(out + (size_t(t.row_lo) + row) * a.ldo + part * a.N + feat) = v;
+          }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          __builtin_amdgcn_wave_barrier();
+        }
       }
     }
   }
@@ -525,7 +563,7 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
         const int sr = (wave * kIpwW + i) * C::RPI + d_row;
         const int c = d_pos ^ ((sr / C::RPB) % C::CPR);
         int grow;
-        if constexpr (MODE == kModeSwiglu) {
+        if constexpr (kPaired<MODE>) {
           // a wave's two MFMA tiles are the gate rows and the matching up rows of one block of 32 features
           const int w_of = sr >> 6, tf = (sr >> 5) & 1, fr = sr & 31;
           grow = tf * a.N + min(at.f0 + w_of * 32 + fr, a.N - 1);
@@ -681,7 +719,7 @@ template <int MODE, int NSTAGE>
 __global__ __launch_bounds__(256, 1) void gemm_bf16_piece_kernel(GemmArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
   if (a.sched_fine) {
-    const TileWalk probe = make_walk(a, reinterpret_cast<int*>(lds_raw), 128, (MODE == kModeSwiglu) ? 64 : 128);
+    const TileWalk probe = make_walk(a, reinterpret_cast<int*>(lds_raw), 128, kPaired<MODE> ? 64 : 128);
     __syncthreads();
     if (probe.total > 0 && probe.total * 2 <= int(gridDim.x)) {
       gemm_bf16_piece_body<MODE, NSTAGE, 1>(a, lds_raw, 4, false);
@@ -702,7 +740,7 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_split_kernel(GemmArgs hea
   __syncthreads();  // the head's last output staging has been read
   // few parent tiles left over: 128 x 64 pieces, eight per parent tile, so that twice as many compute units take part
   // (a piece walks all of K however few there are: its time does not shrink with their number)
-  const TileWalk probe = make_walk(tail, reinterpret_cast<int*>(lds_raw), 128, (MODE == kModeSwiglu) ? 64 : 128);
+  const TileWalk probe = make_walk(tail, reinterpret_cast<int*>(lds_raw), 128, kPaired<MODE> ? 64 : 128);
   __syncthreads();
   if (tail.sched_fine && probe.total > 0 && probe.total * 2 <= int(gridDim.x)) {
     gemm_bf16_piece_body<MODE, PIECE_RING, 1>(tail, lds_raw, TJ);  // 64 tokens a piece

@@ -184,6 +184,15 @@ def test_ffn_grad(rows, d, F, dtype):
     _ffn(rows, d, F, dtype, seed=len(rows) + d)
 
 
+# every tile shape with K in whole slices and with a last one that is half, barely or nearly full, columns that end inside a tile:
+# few tiles (128 x 64), few rows (128 x 128), 80 rows and more (256 x 128), 192 and more with many tiles (256 x 256)
+@pytest.mark.parametrize("rows,d,F", [
+    ((70, 20, 5), 520, 264), ((3, 40) * 20, 776, 648), ((90, 130, 100) * 16, 1032, 328), ((250, 200, 300, 190) * 14, 520, 712),
+    ((250, 200, 300, 190) * 8, 1016, 776), ((130,) * 40, 312, 1016), ((1100, 1400, 900, 1300) * 2, 568, 1160)])
+def test_ffn_grad_with_partial_slices(rows, d, F):
+    _ffn(rows, d, F, "bf16", seed=d + len(rows))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("rank", [0, 1, 3])
 def test_ffn_grad_of_one_rank(rank, dtype):
