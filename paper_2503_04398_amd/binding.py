@@ -172,15 +172,15 @@ def _ptr(t):
     return t.ctypes.data
 
 
-def _rows(t, n_cols: int, name: str):
-    """(pointer, distance of rows in elements) of a matrix whose rows are runs of n_cols numbers, however far apart"""
-    if t is None:
-        return None, 0
+def _row_distance(t, n_cols: int, name: str) -> int:
+    """distance of rows, in elements, of a matrix whose rows are runs of n_cols numbers, however far apart"""
     if t.dim() != 2 or t.shape[1] != n_cols or t.stride(1) != 1:
         raise ValueError("%s must be a matrix of rows of %d numbers, each row one run of memory" % (name, n_cols))
-    if t.shape[0] > 1 and t.stride(0) < n_cols:  # a broadcast row, too: the library takes a distance of 0 as packed
+    if t.shape[0] <= 1:
+        return n_cols
+    if t.stride(0) < n_cols:  # a broadcast row, too: the library takes a distance of 0 as packed
         raise ValueError("rows of %s overlap" % name)
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else n_cols)
+    return t.stride(0)
 
 
 def _stream():
@@ -204,6 +204,7 @@ class SemMoE:
         self.ws_bytes = 0
         self.ws_shared = None
         self._own_ws = {}   # workspaces of the calls that name a size of their own, by call
+        self._adapter_calls = {}  # config, shape and workspace bytes of the adapter calls seen, by their shapes
         self._old_ws = []   # smaller ones before them: a captured graph may still hold their addresses
         self._c_config = None  # (values, C struct of them)
         if allocate_workspace:
@@ -502,47 +503,50 @@ class SemMoE:
             C.byref(c), _stream(), _ptr(req_offsets), int(n_req), _ptr(adapter_of_req), int(n_adapters), _ptr(order),
             _ptr(adapter_offsets)))
 
-    def _adapter_shape(self, call, X, order, adapter_offsets, A, B, scale):
+    def _adapter_call(self, call, X, order, adapter_offsets, A, B, scale, *rows):
+        """(config, shape, workspace bytes) of an adapter call: made and checked once for shapes and distances of rows, which a
+        serving step repeats for every layer; the call itself then costs the host as much as its kernels take.
+        rows: (tensor or None, columns of the call's d_in (0) or d_out (1), field of the shape, name)"""
+        key = (call, _config_values(self.cfg), X.shape, order.shape, adapter_offsets.shape, A.shape, B.shape,
+               scale is None or scale.shape, *((None if t is None else (t.shape, t.stride())) for t, _, _, _ in rows))
+        made = self._adapter_calls.get(key)
+        if made is not None:
+            return made
         n_ad, rank, d_in = A.shape
-        if B.dim() != 3 or B.shape[0] != n_ad or B.shape[2] != rank or adapter_offsets.shape[0] != n_ad + 1 \
-                or order.shape[0] != X.shape[0] or (scale is not None and tuple(scale.shape) != (n_ad,)):
+        if B.dim() != 3 or B.shape[0] != n_ad or B.shape[2] != rank or tuple(adapter_offsets.shape) != (n_ad + 1,) \
+                or tuple(order.shape) != (X.shape[0],) or (scale is not None and tuple(scale.shape) != (n_ad,)):
             raise SemMoEError("%s: shapes must be A[n,r,d_in], B[n,d_out,r], adapter_offsets[n+1], order[T], scale[n]" % call, -2)
-        return self._cfg(T=X.shape[0]), _CAdapterShape(n_ad, rank, d_in, B.shape[1], 0, 0, 0, 0)
-
-    def _adapter_workspace(self, c, s):
+        c, s = self._cfg(T=X.shape[0]), _CAdapterShape(n_ad, rank, d_in, B.shape[1], 0, 0, 0, 0)
+        for t, wide, field, name in rows:
+            if t is not None:
+                setattr(s, field, _row_distance(t, s.d_out if wide else s.d_in, name))
+                if t.shape[0] != X.shape[0]:
+                    raise SemMoEError("%s: all row tensors have X's rows" % call, -2)
         n = C.c_size_t(0)
         self._check("semmoe_adapter_workspace_bytes",
                     self.lib.semmoe_adapter_workspace_bytes(C.byref(c), C.byref(s), C.byref(n)))
-        return self._workspace("adapters", int(n.value))
+        if len(self._adapter_calls) >= 256:
+            self._adapter_calls.clear()
+        self._adapter_calls[key] = made = (c, s, int(n.value))
+        return made
 
     def adapters(self, X, order, adapter_offsets, A, B, Y, Y_base=None, scale=None):
         """Y = Y_base + scale * B (A x) by each token's adapter; Y_base=None adds to nothing, Y_base=Y adds in place"""
-        c, s = self._adapter_shape("adapters", X, order, adapter_offsets, A, B, scale)
-        x, s.ldx = _rows(X, s.d_in, "X")
-        base, s.ld_base = _rows(Y_base, s.d_out, "Y_base")
-        y, s.ld_out = _rows(Y, s.d_out, "Y")
-        self._same_rows("adapters", X, Y_base, Y)
-        ws, n = self._adapter_workspace(c, s)
+        c, s, need = self._adapter_call("adapters", X, order, adapter_offsets, A, B, scale, (X, 0, "ldx", "X"),
+                                        (Y_base, 1, "ld_base", "Y_base"), (Y, 1, "ld_out", "Y"))
+        ws, n = self._workspace("adapters", need)
         self._check("semmoe_adapters", self.lib.semmoe_adapters(
-            C.byref(c), _stream(), C.byref(s), x, _ptr(order), _ptr(adapter_offsets), _ptr(A), _ptr(B), _ptr(scale), base, y,
-            ws, n))
+            C.byref(c), _stream(), C.byref(s), X.data_ptr(), _ptr(order), _ptr(adapter_offsets), _ptr(A), _ptr(B), _ptr(scale),
+            None if Y_base is None else Y_base.data_ptr(), Y.data_ptr(), ws, n))
 
     def adapters_grad(self, X, dY, order, adapter_offsets, A, B, dX=None, dA=None, dB=None, dX_base=None, scale=None):
         """each of dX, dA, dB may be left out; dX_base=dX adds in place"""
-        c, s = self._adapter_shape("adapters_grad", X, order, adapter_offsets, A, B, scale)
-        x, s.ldx = _rows(X, s.d_in, "X")
-        dy, s.ldy = _rows(dY, s.d_out, "dY")
-        base, s.ld_base = _rows(dX_base, s.d_in, "dX_base")
-        dx, s.ld_out = _rows(dX, s.d_in, "dX")
-        self._same_rows("adapters_grad", X, dY, dX_base, dX)
+        c, s, need = self._adapter_call("adapters_grad", X, order, adapter_offsets, A, B, scale, (X, 0, "ldx", "X"),
+                                        (dY, 1, "ldy", "dY"), (dX_base, 0, "ld_base", "dX_base"), (dX, 0, "ld_out", "dX"))
         if (dA is not None and dA.shape != A.shape) or (dB is not None and dB.shape != B.shape):
             raise SemMoEError("adapters_grad: dA and dB have the shapes of A and B", -2)
-        ws, n = self._adapter_workspace(c, s)
+        ws, n = self._workspace("adapters", need)
         self._check("semmoe_adapters_grad", self.lib.semmoe_adapters_grad(
-            C.byref(c), _stream(), C.byref(s), x, dy, _ptr(order), _ptr(adapter_offsets), _ptr(A), _ptr(B), _ptr(scale), base,
-            dx, _ptr(dA), _ptr(dB), ws, n))
-
-    @staticmethod
-    def _same_rows(call, first, *others):
-        if any(t is not None and t.shape[0] != first.shape[0] for t in others):
-            raise SemMoEError("%s: all row tensors have X's rows" % call, -2)
+            C.byref(c), _stream(), C.byref(s), X.data_ptr(), dY.data_ptr(), _ptr(order), _ptr(adapter_offsets), _ptr(A), _ptr(B),
+            _ptr(scale), None if dX_base is None else dX_base.data_ptr(), None if dX is None else dX.data_ptr(), _ptr(dA),
+            _ptr(dB), ws, n))

@@ -47,70 +47,34 @@ __device__ __forceinline__ typename Elem<F32>::type to_act(float f) {
   if constexpr (F32) return f; else return f32_to_bf16(f);
 }
 
-// 16 bytes whose numbers lie `stride` elements apart in LDS (a fragment along the other dimension)
-template <bool F32>
-__device__ __forceinline__ u32x4_t gather_piece(const typename Elem<F32>::type* p, int stride) {
-  u32x4_t v;
+__device__ __forceinline__ u32x4_t load_piece(const void* p) { return *reinterpret_cast<const u32x4_t*>(p); }
+
+// the compiler keeps LDS accesses on both sides in place; a wave's own LDS operations complete in order
+__device__ __forceinline__ void lds_fence() { asm volatile("" ::: "memory"); }
+
+typedef __attribute__((ext_vector_type(4))) short i16x4_t;
+typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
+
+__device__ __forceinline__ unsigned lds_address(const void* p) { return static_cast<unsigned>(reinterpret_cast<size_t>(p)); }
+
+// Fragment across the rows of a matrix in LDS: lane gets the kPer16 numbers of one column in rows row0 + kPer16 * (lane / 16) + 0, 1, ...
+// at(row, col): address of a number.  bf16: two ds_read_b64_tr_b16, where lane i of 16 points at four consecutive columns
+// 4 (i % 4) of row i / 4 and gets four rows of column i; fp32: a number a row.
+template <bool F32, typename At>
+__device__ __forceinline__ u32x4_t column_piece(int lane, At at) {
+  const int l16 = lane & 15, g4 = lane >> 4;
   if constexpr (F32) {
+    u32x4_t v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(p[e * stride]);
+    for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const uint32_t*>(at(g4 * 4 + e, l16));
+    return v;
   } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = uint32_t(p[2 * e * stride]) | (uint32_t(p[(2 * e + 1) * stride]) << 16);
+    const unsigned a0 = lds_address(at(g4 * 8 + (l16 >> 2), (l16 & 3) * 4));
+    const unsigned a1 = lds_address(at(g4 * 8 + 4 + (l16 >> 2), (l16 & 3) * 4));
+    const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_i16x4*>(a0));
+    const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_i16x4*>(a1));
+    return __builtin_bit_cast(u32x4_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
-  return v;
-}
-
-// The ordered tokens of group g: positions [lo, hi).  Group n_adapters: tokens of requests without an adapter, and -1
-// behind them.  Offsets are clamped, so that no position lies outside the order whatever they hold.
-struct Span {
-  int lo, hi;
-};
-__device__ __forceinline__ Span group_span(const int32_t* __restrict__ offsets, int n_adapters, int T, int g) {
-  Span s;
-  s.lo = min(max(offsets[g], 0), T);
-  s.hi = g < n_adapters ? min(max(offsets[g + 1], s.lo), T) : T;
-  return s;
-}
-
-// Items of the groups: group g has max(least, ceil(tokens / per)) of them; pre[g] = items before it (LDS, n_groups + 1).
-// Wave 0 scans; ends with a barrier.
-__device__ __forceinline__ int build_items(const int32_t* __restrict__ offsets, int n_adapters, int n_groups, int T, int per,
-                                           int least, int* pre) {
-  const int tid = threadIdx.x;
-  if (tid < 64) {
-    const int each = (n_groups + 63) / 64;
-    const int lo = min(tid * each, n_groups), hi = min(lo + each, n_groups);
-    int s = 0;
-    for (int g = lo; g < hi; ++g) {
-      const Span sp = group_span(offsets, n_adapters, T, g);
-      s += max(least, (sp.hi - sp.lo + per - 1) / per);
-    }
-    int incl = s;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int v = __shfl_up(incl, off);
-      if (tid >= off) incl += v;
-    }
-    int run = incl - s;
-    if (tid == 0) pre[0] = 0;
-    for (int g = lo; g < hi; ++g) {
-      const Span sp = group_span(offsets, n_adapters, T, g);
-      run += max(least, (sp.hi - sp.lo + per - 1) / per);
-      pre[g + 1] = run;
-    }
-  }
-  __syncthreads();
-  return pre[n_groups];
-}
-
-__device__ __forceinline__ int item_group(const int* pre, int n_groups, int item) {
-  int lo = 0, hi = n_groups;  // pre[lo] <= item < pre[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (pre[mid] <= item) lo = mid; else hi = mid;
-  }
-  return lo;
 }
 
 struct AdapterArgs {
@@ -119,8 +83,64 @@ struct AdapterArgs {
   int T, n_adapters, rank;
 };
 
+// Group g: the ordered tokens [lo, hi) of adapter g; group n_adapters: tokens of requests without an adapter, and -1 behind them.
+// A group has max(least, ceil(tokens / per)) items.  Every wave finds an item by itself, 64 groups at a time: one load and a
+// scan across the lanes, no LDS and no barrier in front of a kernel of a few microseconds.  Offsets are clamped, so that no
+// position lies outside the order whatever they hold.
+struct Item {
+  int g, lo, hi, first, count;  // group, its positions, its first item and their number
+};
+__device__ __forceinline__ bool find_item(const AdapterArgs& a, int n_groups, int per, int least, int item, Item* it) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int g0 = 0; g0 < n_groups; g0 += 64) {
+    const int g = min(g0 + lane, n_groups - 1);
+    const int lo = min(max(a.offsets[g], 0), a.T);
+    const int end = g < a.n_adapters ? min(max(a.offsets[min(g + 1, a.n_adapters)], lo), a.T) : a.T;
+    const int c = g0 + lane < n_groups ? max(least, (end - lo + per - 1) / per) : 0;
+    int incl = c;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int v = __shfl_up(incl, off);
+      if (lane >= off) incl += v;
+    }
+    const int total = __builtin_amdgcn_readlane(incl, 63);
+    if (item < before + total) {
+      const int l = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(before + incl > item)) - 1);
+      it->g = g0 + l;
+      it->lo = __builtin_amdgcn_readlane(lo, l);
+      it->hi = __builtin_amdgcn_readlane(end, l);
+      it->count = __builtin_amdgcn_readlane(c, l);
+      it->first = before + __builtin_amdgcn_readlane(incl, l) - it->count;
+      return true;
+    }
+    before += total;
+  }
+  return false;
+}
+
+// The sum over the parts of four numbers of u: four loads in flight at a time, added in order.
+__device__ __forceinline__ f32x4_t sum_parts(const float* p, size_t plane, int parts) {
+  f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int q = 0; q < parts; q += 4) {
+    f32x4_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const f32x4_t*>(p + plane * min(q + i, parts - 1));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (q + i < parts) s += v[i];
+  }
+  return s;
+}
+
 // ---- shrink: U[part][position][j] = s_a * sum over the part's k of R[token, k] F_a(j, k) ------------------------------
 // TR = false: F_a = A_a [rank][K], rows along k.  TR = true: F_a = B_a [K][rank].
+//
+// A read stream with matrix instructions attached.  A workgroup's four waves share a tile of 16 TT tokens and cut the part's k
+// between them, 128 bytes of every row at a time, so that no wave waits for another inside the tile.  A load covers 8 rows x 128
+// bytes (four neighbouring lanes in one 64-byte segment; fragments loaded as they are put them into four rows), one step ahead
+// into registers, and goes through LDS of the wave's own to become fragments.  A slice of B is one run of memory and is read
+// across (column_piece).  Few tiles: k in parts over workgroups, whose planes `expand` and `outer` add.
 struct ShrinkArgs {
   AdapterArgs ad;
   const void* R;       // rows, act type
@@ -132,101 +152,134 @@ struct ShrinkArgs {
 };
 
 template <bool F32, int RT, int TT, bool TR>
-__global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs a) {
+__device__ __forceinline__ void shrink_body(const ShrinkArgs& a, int block, unsigned char* lds_raw) {
   using E = Elem<F32>;
   using elem = typename E::type;
   constexpr int BT = 16 * TT, KSL = 128 / E::kSize;  // tokens of a tile; numbers in 128 bytes of a row
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-  const int n_ad = a.ad.n_adapters, r = a.ad.rank;
-  int* pre = reinterpret_cast<int*>(lds_raw);
-  unsigned char* body = lds_raw + ((n_ad + 2) * 4 + 15) / 16 * 16;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g4 = lane >> 4;
+  const int r = a.ad.rank;
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Item it;
+  const int item = block / a.parts, part = block - item * a.parts;
+  if (!find_item(a.ad, a.ad.n_adapters, BT, 0, item, &it)) return;  // the whole workgroup
+  const int p0 = it.lo + (item - it.first) * BT, n_tok = min(BT, it.hi - p0);
 
-  const int items = build_items(a.ad.offsets, n_ad, n_ad, a.ad.T, BT, 0, pre);
-  const int item = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
-  if (item >= items) return;
-  const int g = item_group(pre, n_ad, item);
-  const Span sp = group_span(a.ad.offsets, n_ad, a.ad.T, g);
-  const int p0 = sp.lo + (item - pre[g]) * BT, n_tok = min(BT, sp.hi - p0);
-  if (n_tok <= 0) return;
-
-  const elem* row[TT];
+  // load layout: row lane / 8 of 8, 16 bytes at lane % 8 of 128
+  const int l_row = lane >> 3, l_k = (lane & 7) * E::kPer16;
+  const elem* x_row[2 * TT];
 #pragma unroll
-  for (int t = 0; t < TT; ++t) {
-    const int tok = a.ad.order[p0 + min(t * 16 + l16, n_tok - 1)];
-    row[t] = static_cast<const elem*>(a.R) + size_t(min(max(tok, 0), a.ad.T - 1)) * a.ldr;
+  for (int i = 0; i < 2 * TT; ++i) {
+    const int tok = a.ad.order[p0 + min(i * 8 + l_row, n_tok - 1)];
+    x_row[i] = static_cast<const elem*>(a.R) + size_t(min(max(tok, 0), a.ad.T - 1)) * a.ldr;
   }
-  const elem* F = static_cast<const elem*>(a.F) + size_t(g) * r * a.K;
+  const elem* F = static_cast<const elem*>(a.F) + size_t(it.g) * r * a.K;
+  const int k_hi = min(a.K, part * a.part_k + a.part_k);
 
   f32x4_t acc[RT][TT];
 #pragma unroll
   for (int j = 0; j < RT; ++j)
 #pragma unroll
     for (int t = 0; t < TT; ++t) acc[j][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-
-  const int k_lo = part * a.part_k, k_hi = min(a.K, k_lo + a.part_k);
-  elem* stg = reinterpret_cast<elem*>(body) + size_t(wave) * KSL * (16 * RT + E::kPer16);  // TR: a wave's slice of B
-  constexpr int LDB = 16 * RT + E::kPer16;
-  for (int k0 = k_lo + wave * KSL; k0 < k_hi; k0 += 4 * KSL) {
-    if constexpr (TR) {  // [KSL][rank] of B is one run of memory
-      const int per_row = r / E::kPer16, n_k = min(KSL, k_hi - k0);
-      for (int c = lane; c < KSL * per_row; c += 64) {
-        const int kk = c / per_row, jj = c % per_row;
-        const u32x4_t v = kk < n_k ? *reinterpret_cast<const u32x4_t*>(F + size_t(k0 + kk) * r + jj * E::kPer16)
-                                   : u32x4_t{0, 0, 0, 0};
-        *reinterpret_cast<u32x4_t*>(stg + kk * LDB + jj * E::kPer16) = v;
+  u32x4_t xb[2 * TT], fb[2 * RT];
+  const u32x4_t zero = {0, 0, 0, 0};
+  auto fetch = [&](int k0) __attribute__((always_inline)) {
+    const bool in = k0 + l_k < k_hi;
+#pragma unroll
+    for (int i = 0; i < 2 * TT; ++i) xb[i] = in ? load_piece(x_row[i] + k0 + l_k) : zero;
+#pragma unroll
+    for (int i = 0; i < 2 * RT; ++i) {
+      if constexpr (TR) {
+        const int at = (i * 64 + lane) * E::kPer16;
+        fb[i] = at < min(KSL, k_hi - k0) * r ? load_piece(F + size_t(k0) * r + at) : zero;
+      } else {
+        fb[i] = in ? load_piece(F + size_t(min(i * 8 + l_row, r - 1)) * a.K + k0 + l_k) : zero;
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
+  };
+
+  unsigned char* const stg = lds_raw + wave * (TT + RT) * 2048;
+  unsigned char* const f_stg = stg + TT * 2048;
+  // rows of 128 bytes; piece c of row i lies at c ^ (i / 2 % 8)
+  const int put0 = l_row * 128 + (((lane & 7) ^ ((l_row >> 1) & 7)) * 16);
+  const int put1 = (l_row + 8) * 128 + (((lane & 7) ^ ((l_row >> 1) + 4)) * 16);
+  int k0 = part * a.part_k + wave * KSL;
+  if (k0 < k_hi) fetch(k0);
+  while (k0 < k_hi) {
+#pragma unroll
+    for (int i = 0; i < 2 * TT; ++i) *reinterpret_cast<u32x4_t*>(stg + (i >> 1) * 2048 + (i & 1 ? put1 : put0)) = xb[i];
+#pragma unroll
+    for (int i = 0; i < 2 * RT; ++i)
+      *reinterpret_cast<u32x4_t*>(f_stg + (TR ? i * 1024 + lane * 16 : (i >> 1) * 2048 + (i & 1 ? put1 : put0))) = fb[i];
+    lds_fence();
+    k0 += 4 * KSL;
+    if (k0 < k_hi) fetch(k0);
+    lds_fence();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int kk = h * E::kStep + g4 * E::kPer16, k = k0 + kk;
-      const bool in = k < k_hi;
+      const int at = l16 * 128 + (((h * 4 + g4) ^ ((l16 >> 1) & 7)) * 16);
       u32x4_t x[TT];
 #pragma unroll
-      for (int t = 0; t < TT; ++t) x[t] = in ? *reinterpret_cast<const u32x4_t*>(row[t] + k) : u32x4_t{0, 0, 0, 0};
+      for (int t = 0; t < TT; ++t) x[t] = *reinterpret_cast<const u32x4_t*>(stg + t * 2048 + at);
 #pragma unroll
       for (int j = 0; j < RT; ++j) {
         u32x4_t f;
-        if constexpr (TR)
-          f = gather_piece<F32>(stg + kk * LDB + min(j * 16 + l16, r - 1), LDB);
+        if constexpr (TR)  // rank numbers from r on are of the next row, and in results that nobody stores
+          f = column_piece<F32>(lane, [&](int row, int col) { return f_stg + size_t((h * E::kStep + row) * r + (F32 ? min(j * 16 + col, r - 1) : j * 16 + col)) * E::kSize; });
         else
-          f = in ? *reinterpret_cast<const u32x4_t*>(F + size_t(min(j * 16 + l16, r - 1)) * a.K + k) : u32x4_t{0, 0, 0, 0};
+          f = *reinterpret_cast<const u32x4_t*>(f_stg + j * 2048 + at);
 #pragma unroll
         for (int t = 0; t < TT; ++t) acc[j][t] = piece_mfma<F32>(f, x[t], acc[j][t]);
       }
     }
-    if constexpr (TR) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    lds_fence();
   }
 
-  // the four waves' sums meet in LDS, a tile of tokens at a time
-  const float s = a.scale ? a.scale[g] : 1.0f;
-  f32x4_t* red = reinterpret_cast<f32x4_t*>(body);  // [wave][RT][64]
+  // the four waves' sums meet in the staging areas' place
+  f32x4_t* red = reinterpret_cast<f32x4_t*>(lds_raw);  // [wave][RT * TT][64]
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < RT; ++j)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) red[((wave * RT + j) * TT + t) * 64 + lane] = acc[j][t];
+  __syncthreads();
+  const float s = a.scale ? a.scale[it.g] : 1.0f;
   float* U = a.U + size_t(part) * a.ad.T * r;
+  for (int u = wave; u < RT * TT; u += 4) {
+    f32x4_t v = red[u * 64 + lane];
 #pragma unroll
-  for (int t = 0; t < TT; ++t) {
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < RT; ++j) red[(wave * RT + j) * 64 + lane] = acc[j][t];
-    __syncthreads();
-    for (int j = wave; j < RT; j += 4) {
-      f32x4_t v = red[j * 64 + lane];
-#pragma unroll
-      for (int w = 1; w < 4; ++w) v += red[(w * RT + j) * 64 + lane];
-      const int tok = t * 16 + l16, jj = j * 16 + g4 * 4;
-      if (tok < n_tok && jj < r) *reinterpret_cast<f32x4_t*>(U + size_t(p0 + tok) * r + jj) = v * s;
-    }
+    for (int w = 1; w < 4; ++w) v += red[(w * RT * TT + u) * 64 + lane];
+    const int tok = (u % TT) * 16 + l16, j = (u / TT) * 16 + g4 * 4;
+    if (tok < n_tok && j < r) *reinterpret_cast<f32x4_t*>(U + size_t(p0 + tok) * r + j) = v * s;
   }
+}
+
+template <bool F32, int RT, int TT>
+__global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+  shrink_body<F32, RT, TT, false>(a, blockIdx.x, lds_raw);
+}
+
+// v of dY and B, and u of X and A, side by side: each alone leaves part of the chip idle
+template <bool F32, int RT, int TT>
+__global__ __launch_bounds__(256) void shrink_both_kernel(const ShrinkArgs v, int v_blocks, const ShrinkArgs u) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+  if (int(blockIdx.x) < v_blocks) shrink_body<F32, RT, TT, true>(v, blockIdx.x, lds_raw);
+  else shrink_body<F32, RT, TT, false>(u, blockIdx.x - v_blocks, lds_raw);
 }
 
 // ---- expand: Out[token, n] = Base[token, n] + sum over j of F_a(n, j) U[position][j] -----------------------------------
 // TR = false: F_a = B_a [N][rank].  TR = true: F_a = A_a [rank][N].  Group n_adapters: Out = Base.
+//
+// Streams rows of Base in and rows of Out out.  A wave keeps the fragments of u for its 16 TT tokens and walks over 32 columns at a
+// time (its workgroup over 128), the next columns' Base and factor requested before the present ones are multiplied.  The
+// columns of a factor are dealt to the two MFMA tiles so that a lane ends with whole 16-byte pieces of a row: no LDS, no
+// barrier.  A_a's columns go through LDS of the wave's own and are read across.
 struct ExpandArgs {
   AdapterArgs ad;
   const float* U;
   int parts;
   const void* F;
-  int N;
+  int N, chunks;     // 128-column steps of a workgroup
   const void* Base;  // act or nullptr (zero)
   size_t ld_base;
   void* Out;
@@ -239,92 +292,167 @@ template <bool F32, int RT, int TT, bool TR>
 __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
   using E = Elem<F32>;
   using elem = typename E::type;
-  constexpr int BT = 16 * TT, NC = kExpandCols, LDD = NC + 4;
-  constexpr int RP = (16 * RT + E::kStep - 1) / E::kStep * E::kStep, LDU = RP + E::kPer16, KS = RP / E::kStep;
+  constexpr int BT = 16 * TT;
+  constexpr int KS = (16 * RT + E::kStep - 1) / E::kStep;
+  constexpr int NP = F32 ? 2 : 1;             // 16-byte pieces a lane has of a token's 32 columns
+  constexpr int RB = 32 * E::kSize;           // TR: bytes of a row in LDS
+  constexpr int LPR = RB / 16, NF = TR ? (RT * 16 * LPR + 63) / 64 : 2 * KS;  // lanes of a row; loads of a step's factor
   extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
   const int n_ad = a.ad.n_adapters, r = a.ad.rank;
-  int* pre = reinterpret_cast<int*>(lds_raw);
-  float* delta = reinterpret_cast<float*>(lds_raw + ((n_ad + 2) * 4 + 15) / 16 * 16);  // [BT][LDD]
-  elem* Us = reinterpret_cast<elem*>(delta + BT * LDD);                                // [BT][LDU]
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g4 = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cuts = (a.N + a.chunks * kExpandCols - 1) / (a.chunks * kExpandCols);
+  const int item = blockIdx.x / cuts, cut = blockIdx.x - item * cuts;
+  Item it;
+  if (!find_item(a.ad, n_ad + 1, BT, 0, item, &it)) return;
+  const int p0 = it.lo + (item - it.first) * BT, n_tok = min(BT, it.hi - p0);
+  const bool none = it.g == n_ad;
+  if (none && a.Base == a.Out) return;  // the same rows
+  const int c_hi = min(a.N, (cut + 1) * a.chunks * kExpandCols);
+  int c0 = cut * a.chunks * kExpandCols + wave * 32;
+  if (c0 >= c_hi) return;  // no barrier below
 
-  const int items = build_items(a.ad.offsets, n_ad, n_ad + 1, a.ad.T, BT, 0, pre);
-  const int n_chunks = (a.N + NC - 1) / NC;
-  const int item = blockIdx.x / n_chunks, n0 = (blockIdx.x % n_chunks) * NC;
-  if (item >= items) return;
-  const int g = item_group(pre, n_ad + 1, item);
-  const Span sp = group_span(a.ad.offsets, n_ad, a.ad.T, g);
-  const int p0 = sp.lo + (item - pre[g]) * BT, n_tok = min(BT, sp.hi - p0);
-  if (n_tok <= 0) return;
-  const bool none = g == n_ad;
-  if (none && a.Base == a.Out && a.ld_base == a.ldo) return;
+  // column of row m of MFMA tile i: a lane's results 4 g4 + 0..3 of the two tiles are pieces of a row
+  auto col_of = [](int m, int i) { return F32 ? 16 * i + m : 8 * (m >> 2) + 4 * i + (m & 3); };
+  auto piece_col = [&](int q) { return F32 ? 16 * q + 4 * g4 : 8 * g4; };
 
-  if (!none) {
-    for (int i = tid; i < BT * (RP / 4); i += 256) {
-      const int t = i / (RP / 4), j = i % (RP / 4) * 4;
-      f32x4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (t < n_tok && j < r)
-        for (int p = 0; p < a.parts; ++p)
-          v += *reinterpret_cast<const f32x4_t*>(a.U + (size_t(p) * a.ad.T + p0 + t) * r + j);
+  const elem* base_row[TT];
+  elem* out_row[TT];
+  bool there[TT];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) Us[t * LDU + j + e] = to_act<F32>(v[e]);
+  for (int t = 0; t < TT; ++t) {
+    const int tok = t * 16 + l16 < n_tok ? a.ad.order[p0 + t * 16 + l16] : -1;
+    there[t] = unsigned(tok) < unsigned(a.ad.T);
+    const size_t row = there[t] ? tok : 0;
+    base_row[t] = static_cast<const elem*>(a.Base) + row * a.ld_base;
+    out_row[t] = static_cast<elem*>(a.Out) + row * a.ldo;
+  }
+  const u32x4_t zero = {0, 0, 0, 0};
+  u32x4_t u[KS][TT];
+  {
+    // all numbers of a part, up to 16 loads, on their way together; the parts in order
+    constexpr int NV = KS * TT * (E::kPer16 / 4);
+    f32x4_t f[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) f[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    auto at = [&](int i) {  // number of the i-th four, or none
+      const int ks = i / (TT * (E::kPer16 / 4)), t = i / (E::kPer16 / 4) % TT, k = ks * E::kStep + g4 * E::kPer16 + i % (E::kPer16 / 4) * 4;
+      return !none && k < r && t * 16 + l16 < n_tok ? (p0 + t * 16 + l16) * (long long)r + k : -1ll;
+    };
+    const size_t plane = size_t(a.ad.T) * r;
+    constexpr int UP = NV >= 16 ? 1 : (NV >= 8 ? 2 : 4);  // parts at a time
+    for (int p = 0; p < a.parts; p += UP) {
+      f32x4_t v[UP][NV];
+#pragma unroll
+      for (int x = 0; x < UP; ++x)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          v[x][i] = at(i) >= 0 ? *reinterpret_cast<const f32x4_t*>(a.U + plane * min(p + x, a.parts - 1) + at(i)) : f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int x = 0; x < UP; ++x)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (p + x < a.parts) f[i] += v[x][i];
     }
-    __syncthreads();
-    const elem* F = static_cast<const elem*>(a.F) + size_t(g) * r * a.N;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          if constexpr (F32) u[ks][t][x] = __float_as_uint(f[ks * TT + t][x]);
+          else  // the operand's rounding
+            u[ks][t][x] = pack_bf16x2(f[(ks * TT + t) * 2 + (x >> 1)][(x & 1) * 2], f[(ks * TT + t) * 2 + (x >> 1)][(x & 1) * 2 + 1]);
+        }
+  }
+
+  const elem* F = static_cast<const elem*>(a.F) + size_t(none ? 0 : it.g) * r * a.N;
+  u32x4_t fb[NF], bs[TT][NP];
+  auto fetch = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int q = 0; q < NP; ++q)
+        bs[t][q] = a.Base && there[t] && c + piece_col(q) < c_hi ? load_piece(base_row[t] + c + piece_col(q)) : zero;
+    if (none) return;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      if constexpr (TR) {
+        const int row = (i * 64 + lane) / LPR, n = c + (lane % LPR) * E::kPer16;
+        fb[i] = row < r && n < c_hi ? load_piece(F + size_t(row) * a.N + n) : zero;
+      } else {
+        const int k = (i >> 1) * E::kStep + g4 * E::kPer16, n = min(c + col_of(l16, i & 1), a.N - 1);
+        fb[i] = k < r ? load_piece(F + size_t(n) * r + k) : zero;
+      }
+    }
+  };
+  unsigned char* const stg = lds_raw + wave * KS * E::kStep * RB;  // TR
+  if constexpr (TR) {  // rows that no load fills
+    for (int i = NF * 64 + lane; i < KS * E::kStep * LPR; i += 64) *reinterpret_cast<u32x4_t*>(stg + i * 16) = zero;
+  }
+
+  fetch(c0);
+  for (; c0 < c_hi; c0 += kExpandCols) {
+    u32x4_t now[TT][NP], f_now[NF];
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int q = 0; q < NP; ++q) now[t][q] = bs[t][q];
+#pragma unroll
+    for (int i = 0; i < NF; ++i) f_now[i] = fb[i];
+    if constexpr (TR) {
+      lds_fence();
+#pragma unroll
+      for (int i = 0; i < NF; ++i)
+        if (NF * 64 <= KS * E::kStep * LPR || i * 64 + lane < KS * E::kStep * LPR) *reinterpret_cast<u32x4_t*>(stg + (i * 64 + lane) * 16) = f_now[i];
+      lds_fence();
+    }
+    if (c0 + kExpandCols < c_hi) fetch(c0 + kExpandCols);
     f32x4_t acc[2][TT];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int t = 0; t < TT; ++t) acc[i][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const int k = ks * E::kStep + g4 * E::kPer16;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int n = min(n0 + wave * 32 + i * 16 + l16, a.N - 1);
-        u32x4_t f = {0, 0, 0, 0};
-        if (k < r) {
-          if constexpr (TR) f = gather_piece<F32>(F + size_t(k) * a.N + n, a.N);
-          else f = *reinterpret_cast<const u32x4_t*>(F + size_t(n) * r + k);
-        }
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-          acc[i][t] = piece_mfma<F32>(f, *reinterpret_cast<const u32x4_t*>(Us + (t * 16 + l16) * LDU + k), acc[i][t]);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int t = 0; t < TT; ++t)
-        *reinterpret_cast<f32x4_t*>(delta + (t * 16 + l16) * LDD + wave * 32 + i * 16 + g4 * 4) = acc[i][t];
-    __syncthreads();
-  }
-
-  constexpr int CPR = NC / E::kPer16;  // 16-byte pieces of a row
-  for (int i = tid; i < n_tok * CPR; i += 256) {
-    const int t = i / CPR, c = i % CPR * E::kPer16, n = n0 + c;
-    const int tok = a.ad.order[p0 + t];
-    if (n >= a.N || unsigned(tok) >= unsigned(a.ad.T)) continue;
-    u32x4_t v = {0, 0, 0, 0};
-    if (a.Base) v = *reinterpret_cast<const u32x4_t*>(static_cast<const elem*>(a.Base) + size_t(tok) * a.ld_base + n);
     if (!none) {
-      const float* dl = delta + t * LDD + c;
-      if constexpr (F32) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + dl[e]);
-      } else {
+      for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          v[e] = pack_bf16x2(__uint_as_float(v[e] << 16) + dl[2 * e], __uint_as_float(v[e] & 0xffff0000u) + dl[2 * e + 1]);
-      }
+        for (int i = 0; i < 2; ++i) {
+          u32x4_t f;
+          // read across: lane i of 16 points at the columns 4 (i % 4) .. of the 16 that its tile holds
+          if constexpr (TR) f = column_piece<F32>(lane, [&](int row, int col) { return stg + (ks * E::kStep + row) * RB + col_of(col, i) * E::kSize; });
+          else f = f_now[ks * 2 + i];
+#pragma unroll
+          for (int t = 0; t < TT; ++t) acc[i][t] = piece_mfma<F32>(f, u[ks][t], acc[i][t]);
+        }
     }
-    *reinterpret_cast<u32x4_t*>(static_cast<elem*>(a.Out) + size_t(tok) * a.ldo + n) = v;
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int q = 0; q < NP; ++q) {
+        const int n = c0 + piece_col(q);
+        if (!there[t] || n >= c_hi) continue;
+        u32x4_t v = now[t][q];
+        if constexpr (F32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + acc[q][t][e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[e] = pack_bf16x2(__uint_as_float(v[e] << 16) + acc[e >> 1][t][(e & 1) * 2],
+                               __uint_as_float(v[e] & 0xffff0000u) + acc[e >> 1][t][(e & 1) * 2 + 1]);
+        }
+        *reinterpret_cast<u32x4_t*>(out_row[t] + n) = v;
+      }
   }
 }
 
 // ---- outer: dF_a = sum over a's tokens of U[position][j] R[token][c] ---------------------------------------------------
 // SWAP = false: dF_a [rank][C] (c along a row).  SWAP = true: dF_a [C][rank].  An adapter's tokens are cut into segments;
 // one with several of them leaves fp32 sums, which `outer_join` adds in the order of the segments.
+//
+// Both operands run along the tokens, so a slice of 64 rows x 256 bytes and the numbers of its tokens go to LDS and are read
+// across; the next slice's rows are on their way meanwhile.
 struct OuterArgs {
   AdapterArgs ad;
   const float* U;
@@ -337,107 +465,145 @@ struct OuterArgs {
   void* dF;        // act [n_adapters][rank * C]
 };
 
-constexpr int kOuterCols = 64, kOuterTok = 64;
+constexpr int kOuterTok = 64;
+template <bool F32>
+constexpr int kOuterCols = 256 / Elem<F32>::kSize;
 
 template <bool F32, int RT, bool SWAP>
-__global__ __launch_bounds__(256) void outer_kernel(const OuterArgs a) {
+__device__ __forceinline__ void outer_body(const OuterArgs& a, int block, unsigned char* lds_raw) {
   using E = Elem<F32>;
   using elem = typename E::type;
-  constexpr int NC = kOuterCols, KT = kOuterTok, LDR = NC + E::kPer16, LDU = 16 * RT + E::kPer16;
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-  const int n_ad = a.ad.n_adapters, r = a.ad.rank;
-  int* pre = reinterpret_cast<int*>(lds_raw);
-  elem* Rs = reinterpret_cast<elem*>(lds_raw + ((n_ad + 2) * 4 + 15) / 16 * 16);  // [KT][LDR]
-  elem* Us = Rs + KT * LDR;                                                        // [KT][LDU]
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g4 = lane >> 4;
-
-  const int items = build_items(a.ad.offsets, n_ad, n_ad, a.ad.T, a.seg, 1, pre);
+  constexpr int NC = kOuterCols<F32>, KT = kOuterTok, CT = NC / 64;  // 16-column tiles of a wave
+  constexpr int RBU = 16 * RT * E::kSize + 16;                       // bytes of a token's numbers in LDS
+  constexpr int NU = KT * RT * 4 / 256;                              // their loads a thread
+  unsigned char* const Rs = lds_raw;               // [KT][256 bytes], 32-byte pairs of pieces swapped about by the row
+  unsigned char* const Us = lds_raw + KT * 256;    // [KT][RBU]
+  const int r = a.ad.rank;
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_chunks = (a.C + NC - 1) / NC;
-  const int item = blockIdx.x / n_chunks, c0 = (blockIdx.x % n_chunks) * NC;
-  if (item >= items) return;
-  const int g = item_group(pre, n_ad, item);
-  const Span sp = group_span(a.ad.offsets, n_ad, a.ad.T, g);
-  const int p0 = sp.lo + (item - pre[g]) * a.seg, p1 = min(sp.hi, p0 + a.seg);
-  const bool whole = pre[g + 1] - pre[g] == 1;
+  const int item = block / n_chunks, c0 = (block - item * n_chunks) * NC;
+  Item it;
+  if (!find_item(a.ad, a.ad.n_adapters, a.seg, 1, item, &it)) return;
+  const int p0 = it.lo + (item - it.first) * a.seg, p1 = min(it.hi, p0 + a.seg);
 
-  f32x4_t acc[RT];
+  // the four rows that 16 lanes read across lie 64 bytes apart modulo the banks' 256, rows 8 apart in the other half
+  auto r_at = [&](int row, int col_byte) { return Rs + row * 256 + (col_byte ^ (((row & 3) ^ ((row >> 3) & 1) * 4) << 5)); };
+  const int l_row = tid >> 4, l_col = (tid & 15) * E::kPer16;
+  const u32x4_t zero = {0, 0, 0, 0};
+  u32x4_t xb[4];
+  f32x4_t ub[NU];
+  int tok[4];
+  auto tokens = [&](int p) __attribute__((always_inline)) {
 #pragma unroll
-  for (int j = 0; j < RT; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int p = p0; p < p1; p += KT) {
-    constexpr int CPR = NC / E::kPer16;
-    for (int i = tid; i < KT * CPR; i += 256) {
-      const int t = i / CPR, c = i % CPR * E::kPer16;
-      u32x4_t v = {0, 0, 0, 0};
-      if (p + t < p1 && c0 + c < a.C) {
-        const int tok = a.ad.order[p + t];
-        if (unsigned(tok) < unsigned(a.ad.T))
-          v = *reinterpret_cast<const u32x4_t*>(static_cast<const elem*>(a.R) + size_t(tok) * a.ldr + c0 + c);
-      }
-      *reinterpret_cast<u32x4_t*>(Rs + t * LDR + c) = v;
+    for (int i = 0; i < 4; ++i) tok[i] = p + i * 16 + l_row < p1 ? a.ad.order[p + i * 16 + l_row] : -1;
+  };
+  auto fetch = [&](int p) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      xb[i] = unsigned(tok[i]) < unsigned(a.ad.T) && c0 + l_col < a.C
+                  ? load_piece(static_cast<const elem*>(a.R) + size_t(tok[i]) * a.ldr + c0 + l_col) : zero;
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      const int t = (i * 256 + tid) / (RT * 4), j = (i * 256 + tid) % (RT * 4) * 4;
+      ub[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+      if (p + t < p1 && j < r) ub[i] = sum_parts(a.U + size_t(p + t) * r + j, size_t(a.ad.T) * r, a.parts);
     }
-    for (int i = tid; i < KT * RT * 4; i += 256) {
-      const int t = i / (RT * 4), j = i % (RT * 4) * 4;
-      f32x4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (p + t < p1 && j < r)
-        for (int q = 0; q < a.parts; ++q)
-          v += *reinterpret_cast<const f32x4_t*>(a.U + (size_t(q) * a.ad.T + p + t) * r + j);
+  };
+
+  f32x4_t acc[CT][RT];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) Us[t * LDU + j + e] = to_act<F32>(v[e]);
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int j = 0; j < RT; ++j) acc[c][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  tokens(p0);
+  fetch(p0);
+  tokens(p0 + KT);
+  for (int p = p0; p < p1; p += KT) {
+    __syncthreads();  // the slice before has been read
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4_t*>(r_at(i * 16 + l_row, (tid & 15) * 16)) = xb[i];
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      unsigned char* const o = Us + (i * 256 + tid) / (RT * 4) * RBU + (i * 256 + tid) % (RT * 4) * 4 * E::kSize;
+      if constexpr (F32) *reinterpret_cast<f32x4_t*>(o) = ub[i];
+      else *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(ub[i][0], ub[i][1]), pack_bf16x2(ub[i][2], ub[i][3]));
     }
     __syncthreads();
+    if (p + KT < p1) {
+      fetch(p + KT);
+      tokens(p + 2 * KT);
+    }
 #pragma unroll
     for (int ks = 0; ks < KT / E::kStep; ++ks) {
-      const int k = ks * E::kStep + g4 * E::kPer16;
-      const u32x4_t x = gather_piece<F32>(Rs + k * LDR + wave * 16 + l16, LDR);
+      u32x4_t x[CT];
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+        x[c] = column_piece<F32>(lane, [&](int row, int col) { return r_at(ks * E::kStep + row, ((wave * CT + c) * 16 + col) * E::kSize); });
 #pragma unroll
       for (int j = 0; j < RT; ++j) {
-        const u32x4_t u = gather_piece<F32>(Us + k * LDU + j * 16 + l16, LDU);
-        acc[j] = SWAP ? piece_mfma<F32>(u, x, acc[j]) : piece_mfma<F32>(x, u, acc[j]);
+        const u32x4_t u = column_piece<F32>(lane, [&](int row, int col) { return Us + (ks * E::kStep + row) * RBU + (j * 16 + col) * E::kSize; });
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[c][j] = SWAP ? piece_mfma<F32>(u, x[c], acc[c][j]) : piece_mfma<F32>(x[c], u, acc[c][j]);
       }
     }
-    __syncthreads();
   }
 
-  // SWAP = false: lane holds columns 4 g4 + 0..3 of its wave's 16 for rank number l16 of tile j; SWAP = true: rank numbers
-  // 4 g4 + 0..3 of tile j for column l16
+  // SWAP = false: lane holds columns 4 g4 + 0..3 of tile c for rank number l16 of tile j; SWAP = true: rank numbers 4 g4 + 0..3 of
+  // tile j for column l16
 #pragma unroll
-  for (int j = 0; j < RT; ++j) {
-    const int c = c0 + wave * 16 + (SWAP ? l16 : g4 * 4), jj = j * 16 + (SWAP ? g4 * 4 : l16);
-    if (c >= a.C || jj >= r) continue;
-    const size_t at = SWAP ? size_t(c) * r + jj : size_t(jj) * a.C + c;
-    if (!whole) {
-      *reinterpret_cast<f32x4_t*>(a.partial + size_t(item) * r * a.C + at) = acc[j];
-      continue;
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int j = 0; j < RT; ++j) {
+      const int c = c0 + (wave * CT + ct) * 16 + (SWAP ? l16 : g4 * 4), jj = j * 16 + (SWAP ? g4 * 4 : l16);
+      if (c >= a.C || jj >= r) continue;
+      const size_t at = SWAP ? size_t(c) * r + jj : size_t(jj) * a.C + c;
+      const f32x4_t v = acc[ct][j];
+      if (it.count > 1) {
+        if (item < a.max_items) *reinterpret_cast<f32x4_t*>(a.partial + size_t(item) * r * a.C + at) = v;
+        continue;
+      }
+      elem* o = static_cast<elem*>(a.dF) + size_t(it.g) * r * a.C + at;
+      if constexpr (F32) *reinterpret_cast<f32x4_t*>(o) = v;
+      else *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     }
-    elem* o = static_cast<elem*>(a.dF) + size_t(g) * r * a.C + at;
-    if constexpr (F32) {
-      *reinterpret_cast<f32x4_t*>(o) = acc[j];
-    } else {
-      *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(acc[j][0], acc[j][1]), pack_bf16x2(acc[j][2], acc[j][3]));
-    }
-  }
+}
+
+// dA of v and X, and dB of u and dY, side by side
+template <bool F32, int RT>
+__global__ __launch_bounds__(256) void outer_kernel(const OuterArgs da, int da_blocks, const OuterArgs db) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+  if (int(blockIdx.x) < da_blocks) outer_body<F32, RT, false>(da, blockIdx.x, lds_raw);
+  else outer_body<F32, RT, true>(db, blockIdx.x - da_blocks, lds_raw);
 }
 
 template <bool F32>
-__global__ __launch_bounds__(256) void outer_join_kernel(const OuterArgs a) {
+__global__ __launch_bounds__(256) void outer_join_kernel(const OuterArgs da, int da_blocks, const OuterArgs db) {
   using elem = typename Elem<F32>::type;
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-  const int n_ad = a.ad.n_adapters;
-  int* pre = reinterpret_cast<int*>(lds_raw);
-  build_items(a.ad.offsets, n_ad, n_ad, a.ad.T, a.seg, 1, pre);
-  const int g = blockIdx.y, first = pre[g], n = min(pre[g + 1], a.max_items) - first;
-  if (n <= 1) return;
+  const bool first = int(blockIdx.x) < da_blocks;
+  const OuterArgs& a = first ? da : db;
+  const int own = blockIdx.y;
+  auto segments = [&](int g) {
+    const int lo = min(max(a.ad.offsets[g], 0), a.ad.T), hi = min(max(a.ad.offsets[g + 1], lo), a.ad.T);
+    return max(1, (hi - lo + a.seg - 1) / a.seg);
+  };
+  const int n_seg = segments(own);
+  if (n_seg <= 1) return;
+  // its first segment's place: those of the adapters before it
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int g = lane; g < own; g += 64) before += segments(g);
+#pragma unroll
+  for (int off = 32; off; off >>= 1) before += __shfl_xor(before, off);
+  const int n = min(n_seg, a.max_items - before);
   const size_t size = size_t(a.ad.rank) * a.C;
-  for (size_t i = (size_t(blockIdx.x) * 256 + threadIdx.x) * 4; i < size; i += size_t(gridDim.x) * 1024) {
-    f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.partial + first * size + i);
-    for (int q = 1; q < n; ++q) v += *reinterpret_cast<const f32x4_t*>(a.partial + (first + q) * size + i);
-    elem* o = static_cast<elem*>(a.dF) + g * size + i;
-    if constexpr (F32) {
-      *reinterpret_cast<f32x4_t*>(o) = v;
-    } else {
-      *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-    }
-  }
+  const size_t i = (size_t(first ? blockIdx.x : blockIdx.x - da_blocks) * 256 + threadIdx.x) * 4;
+  if (i >= size || n <= 0) return;
+  f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.partial + before * size + i);
+  for (int q = 1; q < n; ++q) v += *reinterpret_cast<const f32x4_t*>(a.partial + (before + q) * size + i);
+  elem* o = static_cast<elem*>(a.dF) + own * size + i;
+  if constexpr (F32) *reinterpret_cast<f32x4_t*>(o) = v;
+  else *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
 }
 
 // ---- index ---------------------------------------------------------------------------------------------------------------
@@ -509,42 +675,54 @@ __global__ __launch_bounds__(256) void adapter_index_kernel(const IndexArgs a, i
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
 struct AdapterPlan {
-  int shrink_tt, expand_tt;       // 16-token tiles a workgroup takes
-  int part_k_in, parts_in;        // shrink over d_in
-  int part_k_out, parts_out;      // shrink over d_out
-  int seg;                        // tokens of a segment of `outer`
-  long long tiles(int tt, int T, int groups) const { return T / (16 * tt) + (groups < T ? groups : T); }
+  int shrink_tt, expand_tt;    // 16-token tiles a workgroup takes
+  int part_k_in, parts_in;     // shrink over d_in
+  int part_k_out, parts_out;   // shrink over d_out
+  int chunks_in, chunks_out;   // expand: 128-column steps of a workgroup, rows of d_in and of d_out
+  int seg;                     // tokens of a segment of `outer`
+  // tiles of the groups, at most: the lengths live on the device
+  static long long tiles(int tt, int T, int groups) { return T / (16 * tt) + (groups < T ? groups : T); }
 };
 
-// K cut into parts until the tiles fill the chip about twice, each part at least 1 KB of a row
+// K cut into parts until there are some 400 workgroups.  Every part is a plane that each reader of u adds: 4096 x 4096, rank 16 on 256
+// tokens of 8 adapters (24 tiles) 8.7 us with 8 parts, 10.1 with 16; 512 tokens (36 tiles) 10.1 / 11.6 / 15.2 with 5 / 10 / 16; 2048
+// tokens (132 tiles) 21.6 / 18.9 / 17.3 with 1 / 2 / 5.
 static void cut_k(int K, int es, long long tiles, int* part_k, int* parts) {
   const int unit = 512 / es;  // a slice for each of the four waves
   const int units = cdiv(K, unit);
-  long long want = tiles > 0 ? 512 / tiles : 1;
-  want = want < 1 ? 1 : (want > 16 ? 16 : want);
-  const int most = units < 2 ? 1 : units / 2;
-  int n = int(want < most ? want : most);
-  const int per = cdiv(units, n);
+  long long want = tiles > 0 ? 400 / tiles : 1;
+  want = want < 1 ? 1 : (want > 6 ? 6 : want);
+  const int per = cdiv(units, int(want < units ? want : units));
   *part_k = per * unit;
   *parts = cdiv(units, per);
 }
 
+// Workgroups that share a tile's columns: each reads the tile's u, so no more than fill the chip; 64-token tiles, of which a compute
+// unit holds two, twice that (16384 tokens, 7168 columns: 201 us with 1024 workgroups, 177 with 2048).
+static int cut_columns(int N, int tt, long long tiles) {
+  const int steps = cdiv(N, kExpandCols);
+  long long cuts = tiles > 0 ? (tt <= 2 ? 896 : 2048) / tiles : 1;
+  cuts = cuts < 1 ? 1 : (cuts > steps ? steps : cuts);
+  return cdiv(steps, int(cuts));
+}
+
+// Tokens of a tile.  A tile reads the whole of its adapter's factor, so many tokens want large tiles; few want many tiles: 16 / 32 / 64
+// tokens in both kernels, us: 1000 tokens of 8 adapters, 4096 x 4096, rank 64: 23 / 29 / 43; 16384 tokens of 4, 7168 x 7168, rank 16: 204 /
+// 191 / 179, with 32 in shrink and 64 in expand 177; 4096 of 64 adapters, 2880 x 2880, rank 128: 61 / 52 / 62.
 static AdapterPlan plan_of(const semmoe_config* cfg, const semmoe_adapter_shape* s) {
   AdapterPlan p;
   const int T = cfg->T, es = int(act_bytes(cfg));
-  const int mean = T / s->n_adapters;
-  const int rt = cdiv(s->rank, 16);
-  p.shrink_tt = mean <= 24 ? 1 : (rt > 4 || mean <= 48 ? 2 : 4);
-  p.expand_tt = mean <= 24 ? 1 : (mean <= 48 ? 2 : 4);
-  const long long tiles = p.tiles(p.shrink_tt, T, s->n_adapters);
+  const int mean = T / s->n_adapters, most = mean <= 24 ? 1 : (mean <= 48 ? 2 : 4);
+  const int shrink_tt = (long long)T * s->rank >= 8192 * 64 || T >= 8192 ? 2 : 1, expand_tt = T >= 8192 ? 4 : (T >= 2048 ? 2 : 1);
+  p.shrink_tt = shrink_tt < most ? shrink_tt : most;
+  p.expand_tt = expand_tt < most ? expand_tt : most;
+  const long long tiles = p.tiles(p.shrink_tt, T, s->n_adapters), e_tiles = p.tiles(p.expand_tt, T, s->n_adapters + 1);
   cut_k(s->d_in, es, tiles, &p.part_k_in, &p.parts_in);
   cut_k(s->d_out, es, tiles, &p.part_k_out, &p.parts_out);
-  const long long chunks = cdiv(s->d_in < s->d_out ? s->d_in : s->d_out, kOuterCols);
-  long long segs = 1024 / (chunks > 0 ? chunks : 1);
-  segs = segs < 1 ? 1 : segs;
-  long long seg = T / segs;
-  seg = (seg + 255) / 256 * 256;
-  p.seg = int(seg < 256 ? 256 : seg);
+  p.chunks_in = cut_columns(s->d_in, p.expand_tt, e_tiles);
+  p.chunks_out = cut_columns(s->d_out, p.expand_tt, e_tiles);
+  const int seg = cdiv(cdiv(T, 8), kOuterTok) * kOuterTok;
+  p.seg = seg < 1024 ? 1024 : (seg > 8192 ? 8192 : seg);
   return p;
 }
 
@@ -553,6 +731,9 @@ static size_t u_floats(const semmoe_config* cfg, const semmoe_adapter_shape* s, 
 }
 static size_t partial_items(const semmoe_config* cfg, const semmoe_adapter_shape* s, const AdapterPlan& p) {
   return size_t(cfg->T) / p.seg + s->n_adapters;
+}
+static size_t partial_floats(const semmoe_config* cfg, const semmoe_adapter_shape* s, const AdapterPlan& p, int width) {
+  return cfg->T > p.seg ? partial_items(cfg, s, p) * s->rank * width : 0;  // else no adapter has a second segment
 }
 
 static int32_t check_shape(const semmoe_config* cfg, const semmoe_adapter_shape* s) {
@@ -590,13 +771,9 @@ static int32_t with_token_tiles(int tt, F f) {
   return f(std::integral_constant<int, 4>{});
 }
 
-static size_t pre_bytes(int n_ad) { return ((size_t(n_ad) + 2) * 4 + 15) / 16 * 16; }
-
 // One launch of 256 threads a workgroup.  `allowed`: the kernel's own flag word (allow_max_dynamic_lds).
-template <typename K, typename A>
-static int32_t launch_groups(K kern, std::atomic<uint64_t>* allowed, long long groups, size_t lds, hipStream_t s, const A& a) {
-  if (groups <= 0) return SEMMOE_OK;
-  if (groups >= (1ll << 24)) return SEMMOE_EUNSUPPORTED;  // 2^32 threads a launch
+template <typename... P, typename... A>
+static int32_t launch_groups(void (*kern)(P...), std::atomic<uint64_t>* allowed, dim3 groups, size_t lds, hipStream_t s, A... args) {
   if (lds > 48 * 1024) {
     DeviceInfo d;
     int32_t st = device_info(&d);
@@ -605,69 +782,87 @@ static int32_t launch_groups(K kern, std::atomic<uint64_t>* allowed, long long g
     st = allow_max_dynamic_lds(allowed, reinterpret_cast<const void*>(kern));
     if (st != SEMMOE_OK) return st;
   }
-  hipLaunchKernelGGL(kern, dim3(unsigned(groups)), dim3(256), lds, s, a);
+  hipLaunchKernelGGL(kern, groups, dim3(256), lds, s, args...);
   SEMMOE_LAUNCH_CHECK();
   return SEMMOE_OK;
 }
+constexpr long long kMostGroups = 1ll << 24;  // 2^32 threads a launch
 
-template <bool F32, bool TR>
+template <bool F32, int RT, int TT>
+constexpr size_t kShrinkLds = 4 * (TT + RT) * 2048 > 4 * RT * TT * 1024 ? 4 * (TT + RT) * 2048 : 4 * RT * TT * 1024;
+
+template <typename F>
+static int32_t with_shrink_tiles(int rank, int tt, F f) {
+  return with_rank_tiles(rank, [&](auto rt) -> int32_t {
+    if (tt <= 1) return f(rt, std::integral_constant<int, 1>{});
+    return f(rt, std::integral_constant<int, 2>{});
+  });
+}
+
+template <bool F32>
 static int32_t launch_shrink(const ShrinkArgs& a, int tt, long long tiles, hipStream_t s) {
-  return with_rank_tiles(a.ad.rank, [&](auto rt) {
-    return with_token_tiles(tt, [&](auto t4) -> int32_t {
-      constexpr int RT = decltype(rt)::value, TT = decltype(t4)::value;
-      using E = Elem<F32>;
-      auto kern = shrink_kernel<F32, RT, TT, TR>;
-      const size_t red = size_t(4) * RT * 1024;
-      const size_t stage = TR ? size_t(4) * (128 / E::kSize) * (16 * RT + E::kPer16) * E::kSize : 0;
-      const size_t lds = pre_bytes(a.ad.n_adapters) + (red > stage ? red : stage);
-      static std::atomic<uint64_t> allowed{0};
-      return launch_groups(kern, &allowed, tiles * a.parts, lds, s, a);
-    });
+  if (tiles <= 0) return SEMMOE_OK;
+  if (tiles * a.parts >= kMostGroups) return SEMMOE_EUNSUPPORTED;
+  return with_shrink_tiles(a.ad.rank, tt, [&](auto rt, auto t4) -> int32_t {
+    constexpr int RT = decltype(rt)::value, TT = decltype(t4)::value;
+    static std::atomic<uint64_t> allowed{0};
+    return launch_groups(shrink_kernel<F32, RT, TT>, &allowed, dim3(unsigned(tiles * a.parts)), kShrinkLds<F32, RT, TT>, s, a);
+  });
+}
+
+template <bool F32>
+static int32_t launch_shrink_both(const ShrinkArgs& v, const ShrinkArgs& u, bool want_v, bool want_u, int tt, long long tiles, hipStream_t s) {
+  const long long vb = want_v ? tiles * v.parts : 0, ub = want_u ? tiles * u.parts : 0;
+  if (vb + ub <= 0) return SEMMOE_OK;
+  if (vb + ub >= kMostGroups) return SEMMOE_EUNSUPPORTED;
+  return with_shrink_tiles(v.ad.rank, tt, [&](auto rt, auto t4) -> int32_t {
+    constexpr int RT = decltype(rt)::value, TT = decltype(t4)::value;
+    static std::atomic<uint64_t> allowed{0};
+    return launch_groups(shrink_both_kernel<F32, RT, TT>, &allowed, dim3(unsigned(vb + ub)), kShrinkLds<F32, RT, TT>, s, v, int(vb), u);
   });
 }
 
 template <bool F32, bool TR>
 static int32_t launch_expand(const ExpandArgs& a, int tt, long long tiles, hipStream_t s) {
-  return with_rank_tiles(a.ad.rank, [&](auto rt) {
+  const long long groups = tiles * cdiv(a.N, a.chunks * kExpandCols);
+  if (groups <= 0) return SEMMOE_OK;
+  if (groups >= kMostGroups) return SEMMOE_EUNSUPPORTED;
+  return with_rank_tiles(a.ad.rank, [&](auto rt) -> int32_t {
     return with_token_tiles(tt, [&](auto t4) -> int32_t {
       constexpr int RT = decltype(rt)::value, TT = decltype(t4)::value;
       using E = Elem<F32>;
-      auto kern = expand_kernel<F32, RT, TT, TR>;
-      const size_t rp = (16 * RT + E::kStep - 1) / E::kStep * E::kStep;
-      const size_t lds = pre_bytes(a.ad.n_adapters) + size_t(16 * TT) * (kExpandCols + 4) * 4 + size_t(16 * TT) * (rp + E::kPer16) * E::kSize;
+      constexpr size_t rows = (16 * RT + E::kStep - 1) / E::kStep * E::kStep;
       static std::atomic<uint64_t> allowed{0};
-      return launch_groups(kern, &allowed, tiles * cdiv(a.N, kExpandCols), lds, s, a);
+      return launch_groups(expand_kernel<F32, RT, TT, TR>, &allowed, dim3(unsigned(groups)), TR ? 4 * rows * 32 * E::kSize : 0, s, a);
     });
   });
 }
 
-template <bool F32, bool SWAP>
-static int32_t launch_outer(const OuterArgs& a, size_t items, hipStream_t s) {
-  const int32_t st = with_rank_tiles(a.ad.rank, [&](auto rt) -> int32_t {
+template <bool F32>
+static int32_t launch_outer(const OuterArgs& da, const OuterArgs& db, hipStream_t s) {
+  constexpr int NC = kOuterCols<F32>;
+  const long long items = da.max_items, ab = da.dF ? items * cdiv(da.C, NC) : 0, bb = db.dF ? items * cdiv(db.C, NC) : 0;
+  if (ab + bb >= kMostGroups) return SEMMOE_EUNSUPPORTED;
+  const int32_t st = with_rank_tiles(da.ad.rank, [&](auto rt) -> int32_t {
     constexpr int RT = decltype(rt)::value;
     using E = Elem<F32>;
-    auto kern = outer_kernel<F32, RT, SWAP>;
-    const size_t lds = pre_bytes(a.ad.n_adapters) + size_t(kOuterTok) * (kOuterCols + E::kPer16 + 16 * RT + E::kPer16) * E::kSize;
     static std::atomic<uint64_t> allowed{0};
-    return launch_groups(kern, &allowed, (long long)items * cdiv(a.C, kOuterCols), lds, s, a);
+    return launch_groups(outer_kernel<F32, RT>, &allowed, dim3(unsigned(ab + bb)), kOuterTok * (256 + 16 * RT * E::kSize + 16), s, da, int(ab), db);
   });
-  if (st != SEMMOE_OK) return st;
-  if (a.ad.T <= a.seg) return SEMMOE_OK;  // no adapter has a second segment
-  const size_t size = size_t(a.ad.rank) * a.C;
-  const unsigned gx = unsigned((size + 4095) / 4096);
-  hipLaunchKernelGGL((outer_join_kernel<F32>), dim3(gx, a.ad.n_adapters), dim3(256), pre_bytes(a.ad.n_adapters), s, a);
-  SEMMOE_LAUNCH_CHECK();
-  return SEMMOE_OK;
+  if (st != SEMMOE_OK || da.ad.T <= da.seg) return st;  // no adapter has a second segment
+  const int ja = da.dF ? int((size_t(da.ad.rank) * da.C + 1023) / 1024) : 0, jb = db.dF ? int((size_t(db.ad.rank) * db.C + 1023) / 1024) : 0;
+  static std::atomic<uint64_t> allowed{0};
+  return launch_groups(outer_join_kernel<F32>, &allowed, dim3(ja + jb, da.ad.n_adapters), 0, s, da, ja, db);
 }
 
 template <bool F32>
 static int32_t run_adapters(const semmoe_config* cfg, const semmoe_adapter_shape* sh, const AdapterPlan& p, hipStream_t s,
                             const void* X, const AdapterArgs& ad, const void* A, const void* B, const float* scale,
                             const void* Y_base, void* Y, float* U, size_t ldx, size_t ld_base, size_t ldo) {
-  ShrinkArgs sa{ad, X, ldx, A, scale, sh->d_in, p.part_k_in, p.parts_in, U};
-  const int32_t st = launch_shrink<F32, false>(sa, p.shrink_tt, p.tiles(p.shrink_tt, cfg->T, sh->n_adapters), s);
+  const ShrinkArgs sa{ad, X, ldx, A, scale, sh->d_in, p.part_k_in, p.parts_in, U};
+  const int32_t st = launch_shrink<F32>(sa, p.shrink_tt, p.tiles(p.shrink_tt, cfg->T, sh->n_adapters), s);
   if (st != SEMMOE_OK) return st;
-  ExpandArgs ea{ad, U, p.parts_in, B, sh->d_out, Y_base, ld_base, Y, ldo};
+  const ExpandArgs ea{ad, U, p.parts_in, B, sh->d_out, p.chunks_out, Y_base, ld_base, Y, ldo};
   return launch_expand<F32, false>(ea, p.expand_tt, p.tiles(p.expand_tt, cfg->T, sh->n_adapters + 1), s);
 }
 
@@ -675,34 +870,21 @@ template <bool F32>
 static int32_t run_adapters_grad(const semmoe_config* cfg, const semmoe_adapter_shape* sh, const AdapterPlan& p, hipStream_t s,
                                  const void* X, const void* dY, const AdapterArgs& ad, const void* A, const void* B,
                                  const float* scale, const void* dX_base, void* dX, void* dA, void* dB, float* U, float* V,
-                                 float* partial, size_t ldx, size_t ldy, size_t ld_base, size_t ldo) {
-  const long long tiles = p.tiles(p.shrink_tt, cfg->T, sh->n_adapters);
-  const size_t items = partial_items(cfg, sh, p);
-  int32_t st;
-  if (dX || dA) {
-    ShrinkArgs sa{ad, dY, ldy, B, scale, sh->d_out, p.part_k_out, p.parts_out, V};
-    st = launch_shrink<F32, true>(sa, p.shrink_tt, tiles, s);
-    if (st != SEMMOE_OK) return st;
-  }
+                                 float* partial_a, float* partial_b, size_t ldx, size_t ldy, size_t ld_base, size_t ldo) {
+  const ShrinkArgs va{ad, dY, ldy, B, scale, sh->d_out, p.part_k_out, p.parts_out, V};
+  const ShrinkArgs ua{ad, X, ldx, A, scale, sh->d_in, p.part_k_in, p.parts_in, U};
+  int32_t st = launch_shrink_both<F32>(va, ua, dX || dA, dB, p.shrink_tt, p.tiles(p.shrink_tt, cfg->T, sh->n_adapters), s);
+  if (st != SEMMOE_OK) return st;
   if (dX) {
-    ExpandArgs ea{ad, V, p.parts_out, A, sh->d_in, dX_base, ld_base, dX, ldo};
+    const ExpandArgs ea{ad, V, p.parts_out, A, sh->d_in, p.chunks_in, dX_base, ld_base, dX, ldo};
     st = launch_expand<F32, true>(ea, p.expand_tt, p.tiles(p.expand_tt, cfg->T, sh->n_adapters + 1), s);
     if (st != SEMMOE_OK) return st;
   }
-  if (dA) {
-    OuterArgs oa{ad, V, p.parts_out, X, ldx, sh->d_in, p.seg, int(items), partial, dA};
-    st = launch_outer<F32, false>(oa, items, s);
-    if (st != SEMMOE_OK) return st;
-  }
-  if (dB) {
-    ShrinkArgs sa{ad, X, ldx, A, scale, sh->d_in, p.part_k_in, p.parts_in, U};
-    st = launch_shrink<F32, false>(sa, p.shrink_tt, tiles, s);  // nothing to launch where T is 0
-    if (st != SEMMOE_OK) return st;
-    OuterArgs oa{ad, U, p.parts_in, dY, ldy, sh->d_out, p.seg, int(items), partial, dB};
-    st = launch_outer<F32, true>(oa, items, s);
-    if (st != SEMMOE_OK) return st;
-  }
-  return SEMMOE_OK;
+  if (!dA && !dB) return SEMMOE_OK;
+  const int items = int(partial_items(cfg, sh, p));
+  const OuterArgs oa{ad, V, p.parts_out, X, ldx, sh->d_in, p.seg, items, partial_a, dA};
+  const OuterArgs ob{ad, U, p.parts_in, dY, ldy, sh->d_out, p.seg, items, partial_b, dB};
+  return launch_outer<F32>(oa, ob, s);
 }
 
 }  // namespace semmoe
@@ -734,9 +916,8 @@ extern "C" int32_t semmoe_adapter_workspace_bytes(const semmoe_config* cfg, cons
   const int32_t st = check_shape(cfg, shape);
   if (st != SEMMOE_OK) return st;
   const AdapterPlan p = plan_of(cfg, shape);
-  const size_t widest = size_t(shape->d_in > shape->d_out ? shape->d_in : shape->d_out);
   *bytes_out = align_up(u_floats(cfg, shape, p.parts_in) * 4, 256) + align_up(u_floats(cfg, shape, p.parts_out) * 4, 256) +
-               (cfg->T > p.seg ? align_up(partial_items(cfg, shape, p) * shape->rank * widest * 4, 256) : 0) + 256;
+               align_up(partial_floats(cfg, shape, p, shape->d_in) * 4, 256) + partial_floats(cfg, shape, p, shape->d_out) * 4 + 256;
   return SEMMOE_OK;
 }
 
@@ -778,14 +959,14 @@ extern "C" int32_t semmoe_adapters_grad(const semmoe_config* cfg, void* stream, 
     return SEMMOE_ESHAPE;
   if (dX && dX_base == dX && ld_base != ldo) return SEMMOE_ESHAPE;
   const AdapterPlan p = plan_of(cfg, shape);
-  const size_t widest = size_t(shape->d_in > shape->d_out ? shape->d_in : shape->d_out);
   Carver c(ws, ws_bytes);
   float* U = c.take<float>(u_floats(cfg, shape, p.parts_in));
   float* V = c.take<float>(u_floats(cfg, shape, p.parts_out));
-  float* partial = c.take<float>(cfg->T > p.seg ? partial_items(cfg, shape, p) * shape->rank * widest : 0);
+  float* partial_a = c.take<float>(partial_floats(cfg, shape, p, shape->d_in));
+  float* partial_b = c.take<float>(partial_floats(cfg, shape, p, shape->d_out));
   if (!c.ok) return SEMMOE_EWORKSPACE;
   const AdapterArgs ad{order, adapter_offsets, cfg->T, shape->n_adapters, shape->rank};
   auto* const run = cfg->dtype == SEMMOE_BF16 ? run_adapters_grad<false> : run_adapters_grad<true>;
-  return run(cfg, shape, p, static_cast<hipStream_t>(stream), X, dY, ad, A, B, scale, dX_base, dX, dA, dB, U, V, partial, ldx,
+  return run(cfg, shape, p, static_cast<hipStream_t>(stream), X, dY, ad, A, B, scale, dX_base, dX, dA, dB, U, V, partial_a, partial_b, ldx,
              ldy, ld_base, ldo);
 }
