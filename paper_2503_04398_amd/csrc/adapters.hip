@@ -271,9 +271,10 @@ __global__ __launch_bounds__(256) void shrink_both_kernel(const ShrinkArgs v, in
 // TR = false: F_a = B_a [N][rank].  TR = true: F_a = A_a [rank][N].  Group n_adapters: Out = Base.
 //
 // Streams rows of Base in and rows of Out out.  A wave keeps the fragments of u for its 16 TT tokens and walks over 32 columns at a
-// time (its workgroup over 128), the next columns' Base and factor requested before the present ones are multiplied.  The
-// columns of a factor are dealt to the two MFMA tiles so that a lane ends with whole 16-byte pieces of a row: no LDS, no
-// barrier.  A_a's columns go through LDS of the wave's own and are read across.
+// time (its workgroup over 128), the next columns' Base and factor requested before the present ones are multiplied.  Loads and
+// stores are as memory lies: four neighbouring lanes a 64-byte segment of a row, the factor as runs; its fragments and the products
+// change places in LDS of the wave's own, no barrier.  (Fragments loaded and products stored as the matrix instruction has them, a
+// segment's pieces 16 lanes apart, kept the address units busy for 74 % of 134 us: 16384 tokens, 7168 columns, rank 64.)
 struct ExpandArgs {
   AdapterArgs ad;
   const float* U;
@@ -294,9 +295,10 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
   using elem = typename E::type;
   constexpr int BT = 16 * TT;
   constexpr int KS = (16 * RT + E::kStep - 1) / E::kStep;
-  constexpr int NP = F32 ? 2 : 1;             // 16-byte pieces a lane has of a token's 32 columns
-  constexpr int RB = 32 * E::kSize;           // TR: bytes of a row in LDS
-  constexpr int LPR = RB / 16, NF = TR ? (RT * 16 * LPR + 63) / 64 : 2 * KS;  // lanes of a row; loads of a step's factor
+  constexpr int LPR = 2 * E::kSize, NP = 16 * LPR / 64;  // lanes of a token's 32 columns, 16 bytes each; pieces a lane has of 16 tokens
+  constexpr int RB = 32 * E::kSize;                      // TR: bytes of a factor's row in LDS
+  constexpr int NF = RT * E::kSize / 2;                  // loads of a step's factor, 32 * 16 RT numbers
+  constexpr int kDelta = 16 * 144;                       // 16 tokens x 32 products, rows padded against bank conflicts
   extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
   const int n_ad = a.ad.n_adapters, r = a.ad.rank;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
@@ -312,21 +314,21 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
   int c0 = cut * a.chunks * kExpandCols + wave * 32;
   if (c0 >= c_hi) return;  // no barrier below
 
-  // column of row m of MFMA tile i: a lane's results 4 g4 + 0..3 of the two tiles are pieces of a row
-  auto col_of = [](int m, int i) { return F32 ? 16 * i + m : 8 * (m >> 2) + 4 * i + (m & 3); };
-  auto piece_col = [&](int q) { return F32 ? 16 * q + 4 * g4 : 8 * g4; };
-
-  const elem* base_row[TT];
-  elem* out_row[TT];
-  bool there[TT];
+  const int l_col = (lane % LPR) * E::kPer16;  // this lane's piece of a row's 32 columns
+  const elem* base_row[TT][NP];
+  elem* out_row[TT][NP];
+  bool there[TT][NP];
 #pragma unroll
-  for (int t = 0; t < TT; ++t) {
-    const int tok = t * 16 + l16 < n_tok ? a.ad.order[p0 + t * 16 + l16] : -1;
-    there[t] = unsigned(tok) < unsigned(a.ad.T);
-    const size_t row = there[t] ? tok : 0;
-    base_row[t] = static_cast<const elem*>(a.Base) + row * a.ld_base;
-    out_row[t] = static_cast<elem*>(a.Out) + row * a.ldo;
-  }
+  for (int t = 0; t < TT; ++t)
+#pragma unroll
+    for (int q = 0; q < NP; ++q) {
+      const int at = t * 16 + q * (64 / LPR) + lane / LPR;
+      const int tok = at < n_tok ? a.ad.order[p0 + at] : -1;
+      there[t][q] = unsigned(tok) < unsigned(a.ad.T);
+      const size_t row = there[t][q] ? tok : 0;
+      base_row[t][q] = static_cast<const elem*>(a.Base) + row * a.ld_base + l_col;
+      out_row[t][q] = static_cast<elem*>(a.Out) + row * a.ldo + l_col;
+    }
   const u32x4_t zero = {0, 0, 0, 0};
   u32x4_t u[KS][TT];
   {
@@ -367,46 +369,49 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
   }
 
   const elem* F = static_cast<const elem*>(a.F) + size_t(none ? 0 : it.g) * r * a.N;
+  unsigned char* const delta = lds_raw + wave * kDelta;
+  unsigned char* const stg = lds_raw + 4 * kDelta + wave * (TR ? KS * E::kStep * RB : 32 * (16 * RT + E::kPer16) * E::kSize);
+  // where the lane's pieces of the factor come from and go to.  TR: rows of 32 columns.  Else the 32 columns' runs of r numbers are
+  // one run; in LDS a piece's width apart, so that 16 of them start in different banks.
+  int f_row[NF], f_col[NF], f_put[NF];
+#pragma unroll
+  for (int i = 0; i < NF; ++i) {
+    const int n = i * 64 + lane, per_row = TR ? LPR : r / E::kPer16;
+    f_row[i] = n / per_row;
+    f_col[i] = (n - f_row[i] * per_row) * E::kPer16;
+    f_put[i] = TR ? n * 16 : (f_row[i] * (r + E::kPer16) + f_col[i]) * E::kSize;
+  }
   u32x4_t fb[NF], bs[TT][NP];
   auto fetch = [&](int c) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < TT; ++t)
 #pragma unroll
-      for (int q = 0; q < NP; ++q)
-        bs[t][q] = a.Base && there[t] && c + piece_col(q) < c_hi ? load_piece(base_row[t] + c + piece_col(q)) : zero;
+      for (int q = 0; q < NP; ++q) bs[t][q] = a.Base && there[t][q] && c + l_col < c_hi ? load_piece(base_row[t][q] + c) : zero;
     if (none) return;
 #pragma unroll
     for (int i = 0; i < NF; ++i) {
-      if constexpr (TR) {
-        const int row = (i * 64 + lane) / LPR, n = c + (lane % LPR) * E::kPer16;
-        fb[i] = row < r && n < c_hi ? load_piece(F + size_t(row) * a.N + n) : zero;
-      } else {
-        const int k = (i >> 1) * E::kStep + g4 * E::kPer16, n = min(c + col_of(l16, i & 1), a.N - 1);
-        fb[i] = k < r ? load_piece(F + size_t(n) * r + k) : zero;
-      }
+      if constexpr (TR) fb[i] = f_row[i] < r && c + f_col[i] < c_hi ? load_piece(F + size_t(f_row[i]) * a.N + c + f_col[i]) : zero;
+      else fb[i] = f_row[i] < 32 && c + f_row[i] < c_hi ? load_piece(F + size_t(c + f_row[i]) * r + f_col[i]) : zero;
     }
   };
-  unsigned char* const stg = lds_raw + wave * KS * E::kStep * RB;  // TR
   if constexpr (TR) {  // rows that no load fills
     for (int i = NF * 64 + lane; i < KS * E::kStep * LPR; i += 64) *reinterpret_cast<u32x4_t*>(stg + i * 16) = zero;
   }
 
   fetch(c0);
   for (; c0 < c_hi; c0 += kExpandCols) {
-    u32x4_t now[TT][NP], f_now[NF];
+    u32x4_t now[TT][NP];
 #pragma unroll
     for (int t = 0; t < TT; ++t)
 #pragma unroll
       for (int q = 0; q < NP; ++q) now[t][q] = bs[t][q];
-#pragma unroll
-    for (int i = 0; i < NF; ++i) f_now[i] = fb[i];
-    if constexpr (TR) {
-      lds_fence();
+    lds_fence();
+    if (!none) {
 #pragma unroll
       for (int i = 0; i < NF; ++i)
-        if (NF * 64 <= KS * E::kStep * LPR || i * 64 + lane < KS * E::kStep * LPR) *reinterpret_cast<u32x4_t*>(stg + (i * 64 + lane) * 16) = f_now[i];
-      lds_fence();
+        if (TR || f_row[i] < 32) *reinterpret_cast<u32x4_t*>(stg + f_put[i]) = fb[i];
     }
+    lds_fence();
     if (c0 + kExpandCols < c_hi) fetch(c0 + kExpandCols);
     f32x4_t acc[2][TT];
 #pragma unroll
@@ -419,31 +424,41 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           u32x4_t f;
-          // read across: lane i of 16 points at the columns 4 (i % 4) .. of the 16 that its tile holds
-          if constexpr (TR) f = column_piece<F32>(lane, [&](int row, int col) { return stg + (ks * E::kStep + row) * RB + col_of(col, i) * E::kSize; });
-          else f = f_now[ks * 2 + i];
+          if constexpr (TR) {
+            f = column_piece<F32>(lane, [&](int row, int col) { return stg + (ks * E::kStep + row) * RB + (i * 16 + col) * E::kSize; });
+          } else {
+            const int k = ks * E::kStep + g4 * E::kPer16;
+            f = k < r ? *reinterpret_cast<const u32x4_t*>(stg + ((i * 16 + l16) * (r + E::kPer16) + k) * E::kSize) : zero;
+          }
 #pragma unroll
           for (int t = 0; t < TT; ++t) acc[i][t] = piece_mfma<F32>(f, u[ks][t], acc[i][t]);
         }
     }
 #pragma unroll
-    for (int t = 0; t < TT; ++t)
+    for (int t = 0; t < TT; ++t) {
+      lds_fence();
+#pragma unroll
+      for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4_t*>(delta + l16 * 144 + (i * 16 + g4 * 4) * 4) = acc[i][t];
+      lds_fence();
 #pragma unroll
       for (int q = 0; q < NP; ++q) {
-        const int n = c0 + piece_col(q);
-        if (!there[t] || n >= c_hi) continue;
+        const float* d = reinterpret_cast<const float*>(delta + (q * (64 / LPR) + lane / LPR) * 144) + l_col;
         u32x4_t v = now[t][q];
+        const f32x4_t lo = *reinterpret_cast<const f32x4_t*>(d);
         if constexpr (F32) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + acc[q][t][e]);
+          for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + lo[e]);
         } else {
+          const f32x4_t hi = *reinterpret_cast<const f32x4_t*>(d + 4);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            v[e] = pack_bf16x2(__uint_as_float(v[e] << 16) + acc[e >> 1][t][(e & 1) * 2],
-                               __uint_as_float(v[e] & 0xffff0000u) + acc[e >> 1][t][(e & 1) * 2 + 1]);
+          for (int e = 0; e < 4; ++e) {
+            const f32x4_t& two = e < 2 ? lo : hi;
+            v[e] = pack_bf16x2(__uint_as_float(v[e] << 16) + two[(e & 1) * 2], __uint_as_float(v[e] & 0xffff0000u) + two[(e & 1) * 2 + 1]);
+          }
         }
-        *reinterpret_cast<u32x4_t*>(out_row[t] + n) = v;
+        if (there[t][q] && c0 + l_col < c_hi) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(out_row[t][q] + c0));
       }
+    }
   }
 }
 
@@ -702,6 +717,7 @@ static void cut_k(int K, int es, long long tiles, int* part_k, int* parts) {
 static int cut_columns(int N, int tt, long long tiles) {
   const int steps = cdiv(N, kExpandCols);
   long long cuts = tiles > 0 ? (tt <= 2 ? 896 : 2048) / tiles : 1;
+  if (cuts >= 6) cuts = (cuts + 2) / 8 * 8;
   cuts = cuts < 1 ? 1 : (cuts > steps ? steps : cuts);
   return cdiv(steps, int(cuts));
 }
@@ -713,7 +729,7 @@ static AdapterPlan plan_of(const semmoe_config* cfg, const semmoe_adapter_shape*
   AdapterPlan p;
   const int T = cfg->T, es = int(act_bytes(cfg));
   const int mean = T / s->n_adapters, most = mean <= 24 ? 1 : (mean <= 48 ? 2 : 4);
-  const int shrink_tt = (long long)T * s->rank >= 8192 * 64 || T >= 8192 ? 2 : 1, expand_tt = T >= 8192 ? 4 : (T >= 2048 ? 2 : 1);
+  const int shrink_tt = (long long)T * s->rank >= 16384 * 64 && s->rank <= 64 ? 4 : ((long long)T * s->rank >= 8192 * 64 || T >= 8192 ? 2 : 1), expand_tt = T >= 8192 ? 4 : (T >= 2048 ? 2 : 1);
   p.shrink_tt = shrink_tt < most ? shrink_tt : most;
   p.expand_tt = expand_tt < most ? expand_tt : most;
   const long long tiles = p.tiles(p.shrink_tt, T, s->n_adapters), e_tiles = p.tiles(p.expand_tt, T, s->n_adapters + 1);
@@ -795,6 +811,8 @@ template <typename F>
 static int32_t with_shrink_tiles(int rank, int tt, F f) {
   return with_rank_tiles(rank, [&](auto rt) -> int32_t {
     if (tt <= 1) return f(rt, std::integral_constant<int, 1>{});
+    if constexpr (decltype(rt)::value == 4)  // the one rank where 64 tokens pay (see plan_of)
+      if (tt >= 4) return f(rt, std::integral_constant<int, 4>{});
     return f(rt, std::integral_constant<int, 2>{});
   });
 }
@@ -832,8 +850,9 @@ static int32_t launch_expand(const ExpandArgs& a, int tt, long long tiles, hipSt
       constexpr int RT = decltype(rt)::value, TT = decltype(t4)::value;
       using E = Elem<F32>;
       constexpr size_t rows = (16 * RT + E::kStep - 1) / E::kStep * E::kStep;
+      constexpr size_t factor = TR ? rows * 32 * E::kSize : 32 * (16 * RT + E::kPer16) * E::kSize;
       static std::atomic<uint64_t> allowed{0};
-      return launch_groups(expand_kernel<F32, RT, TT, TR>, &allowed, dim3(unsigned(groups)), TR ? 4 * rows * 32 * E::kSize : 0, s, a);
+      return launch_groups(expand_kernel<F32, RT, TT, TR>, &allowed, dim3(unsigned(groups)), 4 * (16 * 144 + factor), s, a);
     });
   });
 }

@@ -70,17 +70,32 @@ static int32_t launch_nn_split(const GemmArgs& a, int max_rows, hipStream_t s) {
   return SEMMOE_OK;
 }
 
-template <int MODE, int TT>
-static int32_t launch_nn_f32(const GemmArgs& a, int max_rows, hipStream_t s) {
-  const long long bound = (long long)(max_rows / (32 * TT) + a.nq) * cdiv(a.N, 128);
-  hipLaunchKernelGGL((gemm_nn_f32_kernel<MODE, TT>), dim3(nn_grid(bound, 2)), dim3(256), 0, s, a);
+template <int MODE, int TT, int NW>
+static int32_t launch_nn_f32_as(const GemmArgs& a, int max_rows, hipStream_t s) {
+  const long long bound = (long long)(max_rows / (16 * TT) + a.nq) * cdiv(a.N, 64);
+  hipLaunchKernelGGL((gemm_nn_f32_kernel<MODE, TT, NW>), dim3(nn_grid(bound, NW == 8 ? 1 : 2)), dim3(64 * NW), 0, s, a);
   SEMMOE_LAUNCH_CHECK();
   return SEMMOE_OK;
 }
 
+template <int MODE, int TT>
+static int32_t launch_nn_f32(const GemmArgs& a, int max_rows, int est, hipStream_t s) {
+  DeviceInfo d;
+  const int32_t st = device_info(&d);
+  if (st != SEMMOE_OK) return st;
+  // eight waves while the tiles (a ragged group's last one half full) have a compute unit each and K repays the sum over them: 16
+  // experts of 32 rows, K 2048, 192 tiles 31 us, 34 with four waves; K 512, 384 tiles 23 and 17
+  const long long tiles = (long long)a.nq * (2 * est / (16 * TT) + 1) * cdiv(a.N, 64) / 2;
+  if (tiles <= d.num_cu && a.K >= 1024) return launch_nn_f32_as<MODE, TT, 8>(a, max_rows, s);
+  return launch_nn_f32_as<MODE, TT, 4>(a, max_rows, s);
+}
+
 template <int MODE>
 static int32_t launch_nn_f32(const GemmArgs& a, int max_rows, int est, hipStream_t s) {
-  return est <= 32 ? launch_nn_f32<MODE, 1>(a, max_rows, s) : launch_nn_f32<MODE, 2>(a, max_rows, s);
+  if (64ull * a.ldx >= (1ull << 31)) return SEMMOE_EUNSUPPORTED;  // 32-bit offsets of a tile's rows
+  if (est <= 16) return launch_nn_f32<MODE, 1>(a, max_rows, est, s);
+  if (est <= 48) return launch_nn_f32<MODE, 2>(a, max_rows, est, s);
+  return launch_nn_f32<MODE, 4>(a, max_rows, est, s);
 }
 
 // Tile shapes.  Means of rows an expert, 8 shapes of 1 to 128 experts (d 1024 to 7168, F 512 to 2880), groups spread lognormally

@@ -499,82 +499,85 @@ __global__ __launch_bounds__(256, 1) void gemm_nn_split_kernel(GemmArgs head, Ge
 }
 
 // ------------------------------------------------------------------------------------------------
-// fp32 (v_mfma_f32_16x16x4_f32: full fp32 products and sums).  128 weight columns x 32 TT tokens, four waves as 2 x 2.  A lane
-// reads 16 bytes of a weight row: four consecutive columns, which are row l16 of four MFMA tiles (tile i has the columns
-// 4 m + i), and 16 bytes of a token row: the k of four MFMAs in turn.  So a lane ends with four consecutive columns of a token.
+// fp32 (v_mfma_f32_16x16x4_f32: full fp32 products and sums).  64 weight columns x 16 TT tokens; NW waves cut K between them, 16
+// weight rows at a time: four, or eight where the tiles do not fill the chip.  A lane's 16 bytes of a weight row are four consecutive columns, which are row l16 of four MFMA tiles (tile
+// i has the columns 4 m + i), and its 16 bytes of a token row the k of four MFMAs in turn, so the operands come from memory as
+// they are used, a weight row in runs of 256 bytes, AHEAD steps ahead and without a barrier; a lane ends with four consecutive columns.
+// What bounds it: few rows, the weights' stream; many, the matrix pipe, 32 cycles each of these.  (As 128 x 32 tiles that share LDS
+// slices 16 experts of 32 rows, d 512, F 1024 had 64 workgroups: 62 us for K 2048.)
 // ------------------------------------------------------------------------------------------------
-template <int MODE, int TT>
-__global__ __launch_bounds__(256) void gemm_nn_f32_kernel(GemmArgs a) {
-  constexpr int BW = 128, BT = 32 * TT, BK = 32, LDX = BK + 4;
-  __shared__ __attribute__((aligned(16))) float Ws[BK * BW];
-  __shared__ __attribute__((aligned(16))) float Xs[BT * LDX];
+template <int MODE, int TT, int NW>
+__global__ __launch_bounds__(64 * NW) void gemm_nn_f32_kernel(GemmArgs a) {
+  constexpr int BW = 64, BT = 16 * TT, AHEAD = TT <= 2 ? 4 : 2;
+  __shared__ f32x4_t red[NW * 4 * 64];  // [wave][tile][lane]
   __shared__ int pre[520];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wf = wave & 1, wt = wave >> 1;
-  const int l16 = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const TileWalk walk = make_walk(a, pre, BT, BW);
   const ItemWalk my = xcd_share(walk.total);
+  const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int r = 0; r < my.count; ++r) {
     TileAt at;
-    if (!walk_tile(a, walk, pre, my.item(r), BT, BW, &at)) continue;
+    if (!walk_tile(a, walk, pre, my.item(r), BT, BW, &at)) continue;  // uniform: no barrier is skipped
     const int widx = a.group_to_weight ? a.group_to_weight[a.q_lo + at.q] : (a.q_lo + at.q);
-    const float* Wg = static_cast<const float*>(a.W) + size_t(widx) * a.w_group_stride + min(at.f0 + (tid & 31) * 4, a.N - 4);
-    const float* Xg = static_cast<const float*>(a.X) + size_t(at.row_lo) * a.ldx;
+    const float* Wg = static_cast<const float*>(a.W) + size_t(widx) * a.w_group_stride + size_t(g * 4) * a.ldw + min(at.f0 + l16 * 4, a.N - 4);
+    const float* Xg = static_cast<const float*>(a.X) + size_t(at.row_lo) * a.ldx + g * 4;
+    uint32_t x_at[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) x_at[t] = uint32_t(min(t * 16 + l16, at.n_tok - 1)) * uint32_t(a.ldx);
     f32x4_t acc[4][TT];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int t = 0; t < TT; ++t) acc[i][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    f32x4_t w[4], x[TT];
-    const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
-    auto fetch = [&](int k0) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int k = k0 + i * 8 + (tid >> 5);
-        w[i] = k < a.K ? *reinterpret_cast<const f32x4_t*>(Wg + size_t(k) * a.ldw) : zero;
-      }
-#pragma unroll
-      for (int t = 0; t < TT; ++t) {
-        const int row = min(t * 32 + (tid >> 3), at.n_tok - 1), k = k0 + (tid & 7) * 4;
-        x[t] = k < a.K ? *reinterpret_cast<const f32x4_t*>(Xg + size_t(row) * a.ldx + k) : zero;
-      }
+      for (int t = 0; t < TT; ++t) acc[i][t] = zero;
+    struct Step {
+      f32x4_t w[4], x[TT];
     };
-    fetch(0);
-    for (int k0 = 0; k0 < a.K; k0 += BK) {
-      __syncthreads();
+    auto fetch = [&](int k0, Step& s) __attribute__((always_inline)) {
+      const bool in = k0 + g * 4 < a.K;  // K % 8 == 0: four rows of a lane are there or not
 #pragma unroll
-      for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4_t*>(Ws + (i * 8 + (tid >> 5)) * BW + (tid & 31) * 4) = w[i];
+      for (int e = 0; e < 4; ++e) s.w[e] = in ? *reinterpret_cast<const f32x4_t*>(Wg + size_t(k0 + e) * a.ldw) : zero;
 #pragma unroll
-      for (int t = 0; t < TT; ++t) *reinterpret_cast<f32x4_t*>(Xs + (t * 32 + (tid >> 3)) * LDX + (tid & 7) * 4) = x[t];
-      __syncthreads();
-      if (k0 + BK < a.K) fetch(k0 + BK);
+      for (int t = 0; t < TT; ++t) s.x[t] = in ? *reinterpret_cast<const f32x4_t*>(Xg + x_at[t] + k0) : zero;
+    };
+    auto multiply = [&](const Step& s) __attribute__((always_inline)) {
 #pragma unroll
-      for (int h = 0; h < BK / 16; ++h) {
-        f32x4_t xf[TT];
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
-          xf[t] = *reinterpret_cast<const f32x4_t*>(Xs + ((wt * TT + t) * 16 + l16) * LDX + h * 16 + g * 4);
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          const f32x4_t wv = *reinterpret_cast<const f32x4_t*>(Ws + (h * 16 + g * 4 + s) * BW + wf * 64 + l16 * 4);
+          for (int t = 0; t < TT; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(s.w[e][i], s.x[t][e], acc[i][t], 0, 0, 0);
+    };
+    Step s[AHEAD];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < AHEAD; ++i) fetch((wave + i * NW) * 16, s[i]);
+    for (int k0 = wave * 16; k0 < a.K; k0 += AHEAD * NW * 16) {
 #pragma unroll
-            for (int t = 0; t < TT; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(wv[i], xf[t][s], acc[i][t], 0, 0, 0);
-        }
+      for (int i = 0; i < AHEAD; ++i) {
+        multiply(s[i]);  // zeros where the wave has no such step
+        fetch(k0 + (AHEAD + i) * NW * 16, s[i]);
       }
     }
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
-      const int tok = (wt * TT + t) * 16 + l16;
-      if (tok >= at.n_tok) continue;
+      __syncthreads();  // what was read of the tokens before
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int feat = at.f0 + wf * 64 + g * 16 + e * 4;
-        const size_t row = size_t(at.row_lo) + tok;
-        if (feat < a.N)
-          *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + (MODE == kNnSums ? quad_at(a.N, int(row), feat) : row * a.ldo + feat)) =
-              f32x4_t{acc[0][t][e], acc[1][t][e], acc[2][t][e], acc[3][t][e]};
+      for (int i = 0; i < 4; ++i) red[(wave * 4 + i) * 64 + lane] = acc[i][t];
+      __syncthreads();
+      f32x4_t v = zero;
+      if (wave < 4) {  // tile `wave`
+#pragma unroll
+        for (int w = 0; w < NW; ++w) v += red[(w * 4 + wave) * 64 + lane];
       }
+      __syncthreads();
+      if (wave < 4) red[wave * 64 + lane] = v;
+      __syncthreads();
+      if (wave >= 4) continue;
+      const float* rs = reinterpret_cast<const float*>(red) + lane * 4 + wave;  // row 4 g + `wave` of the four tiles
+      const f32x4_t o = {rs[0], rs[256], rs[512], rs[768]};
+      const int tok = t * 16 + l16, feat = at.f0 + g * 16 + wave * 4, row = at.row_lo + tok;
+      if (tok < at.n_tok && feat < a.N)
+        *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + (MODE == kNnSums ? quad_at(a.N, row, feat) : size_t(row) * a.ldo + feat)) = o;
     }
   }
 }
