@@ -494,7 +494,7 @@ class SemMoE:
     # -- low-rank adapters
     def adapter_index(self, req_offsets, adapter_of_req, n_adapters, order, adapter_offsets):
         """the batch is order's length; requests are adapter_of_req's"""
-        c = self._cfg(T=order.shape[0])
+        c = self._cfg() if order.shape[0] == self.cfg.T else self._cfg(T=order.shape[0])
         n_req = adapter_of_req.shape[0]
         if req_offsets.shape[0] != n_req + 1 or adapter_offsets.shape[0] != int(n_adapters) + 1:
             raise SemMoEError("adapter_index: shapes must be req_offsets[n_req+1], adapter_of_req[n_req], "

@@ -185,9 +185,7 @@ __device__ __forceinline__ void shrink_body(const ShrinkArgs& a, int block, unsi
   auto fetch = [&](int k0) __attribute__((always_inline)) {
     const bool in = k0 + l_k < k_hi;
 #pragma unroll
-    for (int i = 0; i < 2 * TT; ++i) xb[i] = in ? load_piece(x_row[i] + k0 + l_k) : zero;
-#pragma unroll
-    for (int i = 0; i < 2 * RT; ++i) {
+    for (int i = 0; i < 2 * RT; ++i) {  // the factor first: the first step's rows wait for the order
       if constexpr (TR) {
         const int at = (i * 64 + lane) * E::kPer16;
         fb[i] = at < min(KSL, k_hi - k0) * r ? load_piece(F + size_t(k0) * r + at) : zero;
@@ -195,6 +193,8 @@ __device__ __forceinline__ void shrink_body(const ShrinkArgs& a, int block, unsi
         fb[i] = in ? load_piece(F + size_t(min(i * 8 + l_row, r - 1)) * a.K + k0 + l_k) : zero;
       }
     }
+#pragma unroll
+    for (int i = 0; i < 2 * TT; ++i) xb[i] = in ? load_piece(x_row[i] + k0 + l_k) : zero;
   };
 
   unsigned char* const stg = lds_raw + wave * (TT + RT) * 2048;
@@ -314,22 +314,42 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
   int c0 = cut * a.chunks * kExpandCols + wave * 32;
   if (c0 >= c_hi) return;  // no barrier below
 
-  const int l_col = (lane % LPR) * E::kPer16;  // this lane's piece of a row's 32 columns
-  const elem* base_row[TT][NP];
-  elem* out_row[TT][NP];
-  bool there[TT][NP];
+  // what does not wait for the tokens' numbers is requested while they are on their way
+  int tok[TT][NP];
 #pragma unroll
   for (int t = 0; t < TT; ++t)
 #pragma unroll
     for (int q = 0; q < NP; ++q) {
       const int at = t * 16 + q * (64 / LPR) + lane / LPR;
-      const int tok = at < n_tok ? a.ad.order[p0 + at] : -1;
-      there[t][q] = unsigned(tok) < unsigned(a.ad.T);
-      const size_t row = there[t][q] ? tok : 0;
-      base_row[t][q] = static_cast<const elem*>(a.Base) + row * a.ld_base + l_col;
-      out_row[t][q] = static_cast<elem*>(a.Out) + row * a.ldo + l_col;
+      tok[t][q] = at < n_tok ? a.ad.order[p0 + at] : -1;
     }
   const u32x4_t zero = {0, 0, 0, 0};
+  const elem* F = static_cast<const elem*>(a.F) + size_t(none ? 0 : it.g) * r * a.N;
+  unsigned char* const delta = lds_raw + wave * kDelta;
+  unsigned char* const stg = lds_raw + 4 * kDelta + wave * (TR ? KS * E::kStep * RB : 32 * (16 * RT + E::kPer16) * E::kSize);
+  // where the lane's pieces of the factor come from and go to.  TR: rows of 32 columns.  Else the 32 columns' runs of r numbers are
+  // one run; in LDS a piece's width apart, so that 16 of them start in different banks.
+  int f_row[NF], f_col[NF], f_put[NF];
+#pragma unroll
+  for (int i = 0; i < NF; ++i) {
+    const int n = i * 64 + lane, per_row = TR ? LPR : r / E::kPer16;
+    f_row[i] = n / per_row;
+    f_col[i] = (n - f_row[i] * per_row) * E::kPer16;
+    f_put[i] = TR ? n * 16 : (f_row[i] * (r + E::kPer16) + f_col[i]) * E::kSize;
+  }
+  u32x4_t fb[NF], bs[TT][NP];
+  auto fetch_factor = [&](int c) __attribute__((always_inline)) {
+    if (none) return;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      if constexpr (TR) fb[i] = f_row[i] < r && c + f_col[i] < c_hi ? load_piece(F + size_t(f_row[i]) * a.N + c + f_col[i]) : zero;
+      else fb[i] = f_row[i] < 32 && c + f_row[i] < c_hi ? load_piece(F + size_t(c + f_row[i]) * r + f_col[i]) : zero;
+    }
+  };
+  fetch_factor(c0);
+  if constexpr (TR) {  // rows that no load fills
+    for (int i = NF * 64 + lane; i < KS * E::kStep * LPR; i += 64) *reinterpret_cast<u32x4_t*>(stg + i * 16) = zero;
+  }
   u32x4_t u[KS][TT];
   {
     // all numbers of a part, up to 16 loads, on their way together; the parts in order
@@ -367,38 +387,26 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
             u[ks][t][x] = pack_bf16x2(f[(ks * TT + t) * 2 + (x >> 1)][(x & 1) * 2], f[(ks * TT + t) * 2 + (x >> 1)][(x & 1) * 2 + 1]);
         }
   }
-
-  const elem* F = static_cast<const elem*>(a.F) + size_t(none ? 0 : it.g) * r * a.N;
-  unsigned char* const delta = lds_raw + wave * kDelta;
-  unsigned char* const stg = lds_raw + 4 * kDelta + wave * (TR ? KS * E::kStep * RB : 32 * (16 * RT + E::kPer16) * E::kSize);
-  // where the lane's pieces of the factor come from and go to.  TR: rows of 32 columns.  Else the 32 columns' runs of r numbers are
-  // one run; in LDS a piece's width apart, so that 16 of them start in different banks.
-  int f_row[NF], f_col[NF], f_put[NF];
+  const int l_col = (lane % LPR) * E::kPer16;  // this lane's piece of a row's 32 columns
+  const elem* base_row[TT][NP];
+  elem* out_row[TT][NP];
+  bool there[TT][NP];
 #pragma unroll
-  for (int i = 0; i < NF; ++i) {
-    const int n = i * 64 + lane, per_row = TR ? LPR : r / E::kPer16;
-    f_row[i] = n / per_row;
-    f_col[i] = (n - f_row[i] * per_row) * E::kPer16;
-    f_put[i] = TR ? n * 16 : (f_row[i] * (r + E::kPer16) + f_col[i]) * E::kSize;
-  }
-  u32x4_t fb[NF], bs[TT][NP];
-  auto fetch = [&](int c) __attribute__((always_inline)) {
+  for (int t = 0; t < TT; ++t)
+#pragma unroll
+    for (int q = 0; q < NP; ++q) {
+      there[t][q] = unsigned(tok[t][q]) < unsigned(a.ad.T);
+      const size_t row = there[t][q] ? tok[t][q] : 0;
+      base_row[t][q] = static_cast<const elem*>(a.Base) + row * a.ld_base + l_col;
+      out_row[t][q] = static_cast<elem*>(a.Out) + row * a.ldo + l_col;
+    }
+  auto fetch_base = [&](int c) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < TT; ++t)
 #pragma unroll
       for (int q = 0; q < NP; ++q) bs[t][q] = a.Base && there[t][q] && c + l_col < c_hi ? load_piece(base_row[t][q] + c) : zero;
-    if (none) return;
-#pragma unroll
-    for (int i = 0; i < NF; ++i) {
-      if constexpr (TR) fb[i] = f_row[i] < r && c + f_col[i] < c_hi ? load_piece(F + size_t(f_row[i]) * a.N + c + f_col[i]) : zero;
-      else fb[i] = f_row[i] < 32 && c + f_row[i] < c_hi ? load_piece(F + size_t(c + f_row[i]) * r + f_col[i]) : zero;
-    }
   };
-  if constexpr (TR) {  // rows that no load fills
-    for (int i = NF * 64 + lane; i < KS * E::kStep * LPR; i += 64) *reinterpret_cast<u32x4_t*>(stg + i * 16) = zero;
-  }
-
-  fetch(c0);
+  fetch_base(c0);
   for (; c0 < c_hi; c0 += kExpandCols) {
     u32x4_t now[TT][NP];
 #pragma unroll
@@ -412,7 +420,10 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
         if (TR || f_row[i] < 32) *reinterpret_cast<u32x4_t*>(stg + f_put[i]) = fb[i];
     }
     lds_fence();
-    if (c0 + kExpandCols < c_hi) fetch(c0 + kExpandCols);
+    if (c0 + kExpandCols < c_hi) {
+      fetch_factor(c0 + kExpandCols);
+      fetch_base(c0 + kExpandCols);
+    }
     f32x4_t acc[2][TT];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -507,7 +518,8 @@ __device__ __forceinline__ void outer_body(const OuterArgs& a, int block, unsign
   const int l_row = tid >> 4, l_col = (tid & 15) * E::kPer16;
   const u32x4_t zero = {0, 0, 0, 0};
   u32x4_t xb[4];
-  f32x4_t ub[NU];
+  constexpr int UP = RT <= 2 ? 4 : (RT == 4 ? 2 : 1);  // planes of the numbers that are under way with the rows
+  f32x4_t ub[NU][UP];
   int tok[4];
   auto tokens = [&](int p) __attribute__((always_inline)) {
 #pragma unroll
@@ -521,8 +533,10 @@ __device__ __forceinline__ void outer_body(const OuterArgs& a, int block, unsign
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
       const int t = (i * 256 + tid) / (RT * 4), j = (i * 256 + tid) % (RT * 4) * 4;
-      ub[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-      if (p + t < p1 && j < r) ub[i] = sum_parts(a.U + size_t(p + t) * r + j, size_t(a.ad.T) * r, a.parts);
+#pragma unroll
+      for (int x = 0; x < UP; ++x)
+        ub[i][x] = p + t < p1 && j < r && x < a.parts
+                       ? *reinterpret_cast<const f32x4_t*>(a.U + (size_t(x) * a.ad.T + p + t) * r + j) : f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     }
   };
 
@@ -540,9 +554,15 @@ __device__ __forceinline__ void outer_body(const OuterArgs& a, int block, unsign
     for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4_t*>(r_at(i * 16 + l_row, (tid & 15) * 16)) = xb[i];
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-      unsigned char* const o = Us + (i * 256 + tid) / (RT * 4) * RBU + (i * 256 + tid) % (RT * 4) * 4 * E::kSize;
-      if constexpr (F32) *reinterpret_cast<f32x4_t*>(o) = ub[i];
-      else *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(ub[i][0], ub[i][1]), pack_bf16x2(ub[i][2], ub[i][3]));
+      const int t = (i * 256 + tid) / (RT * 4), j = (i * 256 + tid) % (RT * 4) * 4;
+      f32x4_t v = ub[i][0];
+#pragma unroll
+      for (int x = 1; x < UP; ++x) v += ub[i][x];
+      if (a.parts > UP && p + t < p1 && j < r)
+        v += sum_parts(a.U + (size_t(UP) * a.ad.T + p + t) * r + j, size_t(a.ad.T) * r, a.parts - UP);
+      unsigned char* const o = Us + t * RBU + j * E::kSize;
+      if constexpr (F32) *reinterpret_cast<f32x4_t*>(o) = v;
+      else *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     }
     __syncthreads();
     if (p + KT < p1) {
@@ -737,8 +757,13 @@ static AdapterPlan plan_of(const semmoe_config* cfg, const semmoe_adapter_shape*
   cut_k(s->d_out, es, tiles, &p.part_k_out, &p.parts_out);
   p.chunks_in = cut_columns(s->d_in, p.expand_tt, e_tiles);
   p.chunks_out = cut_columns(s->d_out, p.expand_tt, e_tiles);
-  const int seg = cdiv(cdiv(T, 8), kOuterTok) * kOuterTok;
-  p.seg = seg < 1024 ? 1024 : (seg > 8192 ? 8192 : seg);
+  // Segments until there are some 512 workgroups; a slice of 64 tokens takes one 1 to 3 us, a segment more a launch that joins (862 tokens of
+  // 3 adapters, 336 and 976 columns, rank 48: 32 us as whole adapters, 14 slices long).  Adapters of few tokens stay whole where the
+  // batch is short: no launch that joins.
+  const int cols = es == 2 ? kOuterCols<false> : kOuterCols<true>;
+  const int wanted = 512 / (cdiv(s->d_in, cols) + cdiv(s->d_out, cols));
+  const int seg = cdiv(cdiv(T, wanted < 1 ? 1 : wanted), kOuterTok) * kOuterTok, least = mean <= 192 ? 1024 : 128;
+  p.seg = seg < least ? least : (seg > 8192 ? 8192 : seg);
   return p;
 }
 

@@ -93,9 +93,13 @@ static int32_t launch_nn_f32(const GemmArgs& a, int max_rows, int est, hipStream
 template <int MODE>
 static int32_t launch_nn_f32(const GemmArgs& a, int max_rows, int est, hipStream_t s) {
   if (64ull * a.ldx >= (1ull << 31)) return SEMMOE_EUNSUPPORTED;  // 32-bit offsets of a tile's rows
-  if (est <= 16) return launch_nn_f32<MODE, 1>(a, max_rows, est, s);
-  if (est <= 48) return launch_nn_f32<MODE, 2>(a, max_rows, est, s);
-  return launch_nn_f32<MODE, 4>(a, max_rows, est, s);
+  DeviceInfo d;
+  const int32_t st = device_info(&d);
+  if (st != SEMMOE_OK) return st;
+  // 64 tokens where the tiles have a compute unit each (16 experts of 61 rows, K 1280, 376 columns, 96 tiles: 33 us, 22 as 16-token tiles)
+  if (est > 48 && (long long)a.nq * cdiv(est, 64) * cdiv(a.N, 64) >= d.num_cu) return launch_nn_f32<MODE, 4>(a, max_rows, est, s);
+  if (est > 16) return launch_nn_f32<MODE, 2>(a, max_rows, est, s);
+  return launch_nn_f32<MODE, 1>(a, max_rows, est, s);
 }
 
 // Tile shapes.  Means of rows an expert, 8 shapes of 1 to 128 experts (d 1024 to 7168, F 512 to 2880), groups spread lognormally
