@@ -121,7 +121,10 @@ __global__ __launch_bounds__(64 * NWF * NWT, 1) void gemm_nn_ring_kernel(GemmArg
       if (s < nk) issue(s, s);
     int stage = 0;
     for (int it = 0; it < nk; ++it) {
-      const int younger = min(NSTAGE - 2, nk - 1 - it);
+      // slices issued after this one may stay in flight.  Of a partial slice a wave may have no load at all (its rows lie past K), so
+      // that the loads behind this slice's are fewer than they are counted: once it has been issued, all of them are waited for.
+      const bool counted = k_tail == BK || it + NSTAGE - 2 < nk - 1;
+      const int younger = counted ? min(NSTAGE - 2, nk - 1 - it) : 0;
       if (younger >= 2) wait_vmcnt<2 * C::IPW>();
       else if (younger == 1) wait_vmcnt<1 * C::IPW>();
       else wait_vmcnt<0>();

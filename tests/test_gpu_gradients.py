@@ -147,7 +147,8 @@ def _ffn(rows, d, F, dtype, D=1, rank=-1, seed=0, alias=None):
     if alias:
         dX = x if alias == "X" else dy
     m._workspace("expert_ffn_grad", m._ffn_grad_bytes(P))
-    m._own_ws["expert_ffn_grad"].fill_(0xff)  # NaN: what nobody writes does not pass for what another call left
+    for ws in m._own_ws.values():
+        ws.fill_(0xff)  # NaN: what nobody writes does not pass for what another call left
     m.expert_ffn_grad(rank, x, dy, torch.from_numpy(off).to(DEV), torch.from_numpy(of_phys).to(DEV), W_gu.to(DEV), W_dn.to(DEV), dX)
     torch.cuda.synchronize()
     lo, hi = (0, E) if rank < 0 else (rank * (E // D), (rank + 1) * (E // D))
@@ -191,6 +192,31 @@ def test_ffn_grad(rows, d, F, dtype):
     ((250, 200, 300, 190) * 8, 1016, 776), ((130,) * 40, 312, 1016), ((1100, 1400, 900, 1300) * 2, 568, 1160)])
 def test_ffn_grad_with_partial_slices(rows, d, F):
     _ffn(rows, d, F, "bf16", seed=d + len(rows))
+
+
+@pytest.mark.parametrize("d,F", [(72, 40), (136, 72), (200, 96), (8, 8)])
+def test_short_products_give_the_same_bits_every_time(d, F):
+    """K of one to three slices, the last with a few rows: nothing is read before its loads have landed"""
+    r = np.random.default_rng(d)
+    rows, E = (40, 100, 7, 129, 64, 300, 2, 31) * 8, 64
+    P = sum(rows)
+    m = _layer(P, 1, d, "bf16", E=E, F=F)
+    x, dy = _rand(r, (P, d), "bf16").to(DEV), _rand(r, (P, d), "bf16").to(DEV)
+    W_gu, W_dn = _rand(r, (E, 2 * F, d), "bf16", d ** -0.5).to(DEV), _rand(r, (E, d, F), "bf16", F ** -0.5).to(DEV)
+    off = torch.tensor(np.concatenate([[0], np.cumsum(rows)]), dtype=torch.int32, device=DEV)
+    of = torch.arange(E, dtype=torch.int32, device=DEV)
+    other = torch.randn(64 << 20, device=DEV)
+    want = None
+    for _ in range(12):
+        dX = torch.full((P, d), 512.0, dtype=torch.bfloat16, device=DEV)
+        other.mul_(-1.0)  # what the caches held goes
+        m.expert_ffn_grad(-1, x, dy, off, of, W_gu, W_dn, dX)
+        want = dX if want is None else want
+        assert torch.equal(dX, want)
+    args = [_np(t) for t in (x[:40], dy[:40], W_gu[0], W_dn[0])]
+    ref = G.swiglu_ffn_grad(*args)
+    err = np.linalg.norm(_np(want)[:40] - ref, axis=1) / np.linalg.norm(ref, axis=1)
+    assert (err <= _ffn_tolerance(*args, "bf16")).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
@@ -352,7 +378,8 @@ def test_gradients_replay_in_a_graph():
     for _ in range(3):
         for t in (dY, dw, dXp, dX):
             t.fill_(9.0)
-        m._own_ws["expert_ffn_grad"].fill_(0xff)
+        for ws in m._own_ws.values():
+            ws.fill_(0xff)
         graph.replay()
         torch.cuda.synchronize()
         for got, x in zip((dY, dw, dXp, dX), want):
