@@ -174,7 +174,7 @@ def _ptr(t):
 
 def _row_distance(t, n_cols: int, name: str) -> int:
     """distance of rows, in elements, of a matrix whose rows are runs of n_cols numbers, however far apart"""
-    if t.dim() != 2 or t.shape[1] != n_cols or t.stride(1) != 1:
+    if t.dim() != 2 or t.shape[1] != n_cols or (t.shape[0] and t.stride(1) != 1):
         raise ValueError("%s must be a matrix of rows of %d numbers, each row one run of memory" % (name, n_cols))
     if t.shape[0] <= 1:
         return n_cols
@@ -197,7 +197,10 @@ class SemMoE:
     """One config + one workspace; methods mirror the C entry points one to one."""
 
     def __init__(self, cfg: Config, device="cuda:0", allocate_workspace: bool = True):
+        import torch
         self.lib = load_library()
+        self._torch = torch
+        self._types = torch._C._cuda_getDevice, torch.int32, torch.float32, (torch.float32, torch.bfloat16)
         self.cfg = cfg
         self.device = device
         self.ws = None
@@ -208,7 +211,6 @@ class SemMoE:
         self._old_ws = []   # smaller ones before them: a captured graph may still hold their addresses
         self._c_config = None  # (values, C struct of them)
         if allocate_workspace:
-            import torch
             self.ws_bytes = self.workspace_bytes()
             self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
 
@@ -232,14 +234,31 @@ class SemMoE:
         return c
 
     def _workspace(self, call: str, need: int):
-        """(pointer, bytes) of a workspace that only `call` uses, of at least `need` bytes: kept from call to call"""
-        t = self._own_ws.get(call)
+        """(pointer, bytes) of a workspace that only `call` on the present stream uses, of at least `need` bytes: kept from call
+        to call, so that calls on two streams may overlap"""
+        key = (call, _stream())
+        t = self._own_ws.get(key)
         if t is None or t.numel() < need:
             import torch
             if t is not None:
                 self._old_ws.append(t)
-            self._own_ws[call] = t = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+            self._own_ws[key] = t = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
         return t.data_ptr(), t.numel()
+
+    def _fit(self, call: str, args):
+        """Refuses tensors that the library would read or write past their end, or as numbers of another type, or that lie on
+        another device than the current one.  args: (tensor or None, type, least numbers); the type None is the config's
+        activation type.  The calls of a few microseconds ask the same of their tensors in one expression first (a tuple and
+        a loop cost them 2 us more) and come here for what is wrong."""
+        torch = self._torch
+        dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
+        act = torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32
+        for t, dtype, least in args:
+            if t is not None and (t.dtype is not (dtype or act) or t.numel() < least or t.get_device() != dev):
+                size = t.numel() < least
+                raise SemMoEError("%s: %d numbers of %s on %s where %s%s on the current device (%d) are needed" % (
+                    call, t.numel(), t.dtype, t.device, "at least %d of " % least if least else "", dtype or act, dev),
+                    -2 if size else -1)
 
     def workspace_bytes(self) -> int:
         n = C.c_size_t(0)
@@ -465,11 +484,38 @@ class SemMoE:
     # -- gradients of the layer's steps
     def combine_grad(self, dOut, Y, slot_of_pair, topk_w, dY, dtopk_w):
         """dY or dtopk_w may be None (then topk_w or Y may be, too); dY may be Y itself"""
+        T, d, P = self.cfg.T, self.cfg.d, self.cfg.T * self.cfg.k
+        if T == 0:
+            return
+        here, i32, f32, acts = self._types
+        dev, act = dOut.get_device(), acts[self.cfg.dtype == BF16]
+        if dev < 0 or dev != here() or not (
+                act is dOut.dtype and i32 is slot_of_pair.dtype and dev == slot_of_pair.get_device() and dOut.numel() >= T * d
+                and slot_of_pair.numel() >= P
+                and (Y is None or (act is Y.dtype and dev == Y.get_device() and Y.numel() >= P * d))
+                and (dY is None or (act is dY.dtype and dev == dY.get_device() and dY.numel() >= P * d))
+                and (topk_w is None or (f32 is topk_w.dtype and dev == topk_w.get_device() and topk_w.numel() >= P))
+                and (dtopk_w is None or (f32 is dtopk_w.dtype and dev == dtopk_w.get_device() and dtopk_w.numel() >= P))):
+            self._fit("combine_grad", ((dOut, None, T * d), (Y, None, P * d), (slot_of_pair, i32, P),
+                    (topk_w, f32, P), (dY, None, P * d), (dtopk_w, f32, P)))
         c = self._cfg()
         self._check("semmoe_combine_grad", self.lib.semmoe_combine_grad(
             C.byref(c), _stream(), _ptr(dOut), _ptr(Y), _ptr(slot_of_pair), _ptr(topk_w), _ptr(dY), _ptr(dtopk_w)))
 
     def dispatch_grad(self, dX_perm, slot_of_pair, dX, dX_add=None):
+        """dX_add may be dX itself"""
+        T, d, P = self.cfg.T, self.cfg.d, self.cfg.T * self.cfg.k
+        if T == 0:
+            return
+        here, i32, _, acts = self._types
+        dev, act = dX.get_device(), acts[self.cfg.dtype == BF16]
+        if dev < 0 or dev != here() or not (
+                act is dX.dtype is dX_perm.dtype and i32 is slot_of_pair.dtype
+                and dev == dX_perm.get_device() == slot_of_pair.get_device() and dX.numel() >= T * d
+                and dX_perm.numel() >= P * d and slot_of_pair.numel() >= P
+                and (dX_add is None or (act is dX_add.dtype and dev == dX_add.get_device() and dX_add.numel() >= T * d))):
+            self._fit("dispatch_grad", ((dX_perm, None, P * d), (slot_of_pair, i32, P),
+                    (dX, None, T * d), (dX_add, None, T * d)))
         c = self._cfg()
         self._check("semmoe_dispatch_grad", self.lib.semmoe_dispatch_grad(
             C.byref(c), _stream(), _ptr(dX_perm), _ptr(slot_of_pair), _ptr(dX_add), _ptr(dX)))
@@ -478,48 +524,76 @@ class SemMoE:
         return self.cfg.F * ((rows + 31) // 32 * 128 + rows * (4 if self.cfg.dtype == BF16 else 8)) + 768
 
     def expert_ffn_grad(self, rank, X_perm, dY, expert_offsets, expert_of_phys, W_gu, W_down, dX_perm):
+        """dX_perm may be X_perm or dY itself.  W_gu and W_down hold every expert that expert_of_phys names for the rank."""
+        torch = self._torch
+        d, F, E, P = self.cfg.d, self.cfg.F, self.cfg.E, self.cfg.T * self.cfg.k
+        if P == 0:
+            return
+        self._fit("expert_ffn_grad", ((X_perm, None, P * d), (dY, None, P * d),
+                  (expert_offsets, torch.int32, E + 1), (expert_of_phys, torch.int32, E),
+                  (W_gu, None, 2 * F * d), (W_down, None, F * d), (dX_perm, None, P * d)))
         c = self._cfg()
-        ws, n = self._workspace("expert_ffn_grad", self._ffn_grad_bytes(self.cfg.T * self.cfg.k))
+        ws, n = self._workspace("expert_ffn_grad", self._ffn_grad_bytes(P))
         self._check("semmoe_expert_ffn_grad", self.lib.semmoe_expert_ffn_grad(
             C.byref(c), _stream(), int(rank), _ptr(X_perm), _ptr(dY), _ptr(expert_offsets), _ptr(expert_of_phys),
             _ptr(W_gu), _ptr(W_down), _ptr(dX_perm), ws, n))
 
     def shared_ffn_grad(self, X, dY, n_tokens, W_gu_sh, W_down_sh, dX):
-        """has a workspace of its own, as shared_ffn does, so that it may run on another stream beside the routed path's"""
+        """dX may be X or dY itself"""
+        d, F, n = self.cfg.d, self.cfg.F, int(n_tokens)
+        if n == 0:
+            return
+        self._fit("shared_ffn_grad", ((X, None, n * d), (dY, None, n * d), (W_gu_sh, None, 2 * F * d),
+                  (W_down_sh, None, F * d), (dX, None, n * d)))
         c = self._cfg()
-        ws, n = self._workspace("shared_ffn_grad", self._ffn_grad_bytes(max(int(n_tokens), 0)))
+        ws, size = self._workspace("shared_ffn_grad", self._ffn_grad_bytes(max(n, 0)))
         self._check("semmoe_shared_ffn_grad", self.lib.semmoe_shared_ffn_grad(
-            C.byref(c), _stream(), _ptr(X), _ptr(dY), int(n_tokens), _ptr(W_gu_sh), _ptr(W_down_sh), _ptr(dX), ws, n))
+            C.byref(c), _stream(), _ptr(X), _ptr(dY), n, _ptr(W_gu_sh), _ptr(W_down_sh), _ptr(dX), ws, size))
 
     # -- low-rank adapters
     def adapter_index(self, req_offsets, adapter_of_req, n_adapters, order, adapter_offsets):
         """the batch is order's length; requests are adapter_of_req's"""
-        c = self._cfg() if order.shape[0] == self.cfg.T else self._cfg(T=order.shape[0])
-        n_req = adapter_of_req.shape[0]
+        n_req, T = adapter_of_req.shape[0], order.shape[0]
         if req_offsets.shape[0] != n_req + 1 or adapter_offsets.shape[0] != int(n_adapters) + 1:
             raise SemMoEError("adapter_index: shapes must be req_offsets[n_req+1], adapter_of_req[n_req], "
                               "adapter_offsets[n_adapters+1]", -2)
+        here, i32, _, _ = self._types
+        dev = order.get_device()
+        if dev < 0 or dev != here() or not (
+                i32 is req_offsets.dtype is adapter_of_req.dtype is order.dtype is adapter_offsets.dtype
+                and dev == req_offsets.get_device() == adapter_of_req.get_device() == adapter_offsets.get_device()):
+            self._fit("adapter_index", ((req_offsets, i32, 1), (adapter_of_req, i32, 0),
+                    (order, i32, 0), (adapter_offsets, i32, 1)))
+        if T == 0:
+            adapter_offsets.zero_()
+            return
+        c = self._cfg() if T == self.cfg.T else self._cfg(T=T)
         self._check("semmoe_adapter_index", self.lib.semmoe_adapter_index(
             C.byref(c), _stream(), _ptr(req_offsets), int(n_req), _ptr(adapter_of_req), int(n_adapters), _ptr(order),
             _ptr(adapter_offsets)))
 
-    def _adapter_call(self, call, X, order, adapter_offsets, A, B, scale, *rows):
+    def _adapter_call(self, call, X, order, adapter_offsets, A, B, scale, dY, base, out):
         """(config, shape, workspace bytes) of an adapter call: made and checked once for shapes and distances of rows, which a
         serving step repeats for every layer; the call itself then costs the host as much as its kernels take.
-        rows: (tensor or None, columns of the call's d_in (0) or d_out (1), field of the shape, name)"""
-        key = (call, _config_values(self.cfg), X.shape, order.shape, adapter_offsets.shape, A.shape, B.shape,
-               scale is None or scale.shape, *((None if t is None else (t.shape, t.stride())) for t, _, _, _ in rows))
+        dY: None in the forward call, whose base and out have d_out columns; with it they have d_in."""
+        key = (call, _config_values(self.cfg), X.shape, X.stride(), order.shape, adapter_offsets.shape, A.shape, B.shape,
+               None if scale is None else scale.shape, None if dY is None else (dY.shape, dY.stride()),
+               None if base is None else (base.shape, base.stride()), None if out is None else (out.shape, out.stride()))
         made = self._adapter_calls.get(key)
         if made is not None:
             return made
+        if A.dim() != 3:
+            raise SemMoEError("%s: A is [n_adapters, rank, d_in]" % call, -2)
         n_ad, rank, d_in = A.shape
         if B.dim() != 3 or B.shape[0] != n_ad or B.shape[2] != rank or tuple(adapter_offsets.shape) != (n_ad + 1,) \
                 or tuple(order.shape) != (X.shape[0],) or (scale is not None and tuple(scale.shape) != (n_ad,)):
             raise SemMoEError("%s: shapes must be A[n,r,d_in], B[n,d_out,r], adapter_offsets[n+1], order[T], scale[n]" % call, -2)
         c, s = self._cfg(T=X.shape[0]), _CAdapterShape(n_ad, rank, d_in, B.shape[1], 0, 0, 0, 0)
-        for t, wide, field, name in rows:
+        n_out = s.d_out if dY is None else d_in
+        for t, field, n_cols, name in ((X, "ldx", d_in, "X"), (dY, "ldy", s.d_out, "dY"), (base, "ld_base", n_out, "the base"),
+                                       (out, "ld_out", n_out, "the result")):
             if t is not None:
-                setattr(s, field, _row_distance(t, s.d_out if wide else s.d_in, name))
+                setattr(s, field, _row_distance(t, n_cols, name))
                 if t.shape[0] != X.shape[0]:
                     raise SemMoEError("%s: all row tensors have X's rows" % call, -2)
         n = C.c_size_t(0)
@@ -532,19 +606,39 @@ class SemMoE:
 
     def adapters(self, X, order, adapter_offsets, A, B, Y, Y_base=None, scale=None):
         """Y = Y_base + scale * B (A x) by each token's adapter; Y_base=None adds to nothing, Y_base=Y adds in place"""
-        c, s, need = self._adapter_call("adapters", X, order, adapter_offsets, A, B, scale, (X, 0, "ldx", "X"),
-                                        (Y_base, 1, "ld_base", "Y_base"), (Y, 1, "ld_out", "Y"))
+        c, s, need = self._adapter_call("adapters", X, order, adapter_offsets, A, B, scale, None, Y_base, Y)
+        here, i32, f32, acts = self._types
+        dev, act = X.get_device(), acts[self.cfg.dtype == BF16]
+        if dev < 0 or dev != here() or not (
+                act is X.dtype is A.dtype is B.dtype is Y.dtype and i32 is order.dtype is adapter_offsets.dtype
+                and dev == order.get_device() == adapter_offsets.get_device() == A.get_device() == B.get_device() == Y.get_device()
+                and (scale is None or (f32 is scale.dtype and dev == scale.get_device()))
+                and (Y_base is None or (act is Y_base.dtype and dev == Y_base.get_device()))):
+            self._fit("adapters", ((X, None, 0), (order, i32, 0), (adapter_offsets, i32, 1),
+                    (A, None, 0), (B, None, 0), (scale, f32, 0), (Y_base, None, 0),
+                    (Y, None, 0)))
+        if X.shape[0] == 0:
+            return
         ws, n = self._workspace("adapters", need)
         self._check("semmoe_adapters", self.lib.semmoe_adapters(
             C.byref(c), _stream(), C.byref(s), X.data_ptr(), _ptr(order), _ptr(adapter_offsets), _ptr(A), _ptr(B), _ptr(scale),
             None if Y_base is None else Y_base.data_ptr(), Y.data_ptr(), ws, n))
 
     def adapters_grad(self, X, dY, order, adapter_offsets, A, B, dX=None, dA=None, dB=None, dX_base=None, scale=None):
-        """each of dX, dA, dB may be left out; dX_base=dX adds in place"""
-        c, s, need = self._adapter_call("adapters_grad", X, order, adapter_offsets, A, B, scale, (X, 0, "ldx", "X"),
-                                        (dY, 1, "ldy", "dY"), (dX_base, 0, "ld_base", "dX_base"), (dX, 0, "ld_out", "dX"))
+        """each of dX, dA, dB may be left out; dX_base=dX adds in place; dX may be X or dY itself"""
+        torch = self._torch
+        c, s, need = self._adapter_call("adapters_grad", X, order, adapter_offsets, A, B, scale, dY, dX_base, dX)
         if (dA is not None and dA.shape != A.shape) or (dB is not None and dB.shape != B.shape):
             raise SemMoEError("adapters_grad: dA and dB have the shapes of A and B", -2)
+        self._fit("adapters_grad", ((X, None, 0), (dY, None, 0), (order, torch.int32, 0),
+                  (adapter_offsets, torch.int32, 1), (A, None, 0), (B, None, 0),
+                  (scale, torch.float32, 0), (dX_base, None, 0), (dX, None, 0), (dA, None, 0),
+                  (dB, None, 0)))
+        if X.shape[0] == 0:
+            for t in (dA, dB):
+                if t is not None:
+                    t.zero_()
+            return
         ws, n = self._workspace("adapters", need)
         self._check("semmoe_adapters_grad", self.lib.semmoe_adapters_grad(
             C.byref(c), _stream(), C.byref(s), X.data_ptr(), dY.data_ptr(), _ptr(order), _ptr(adapter_offsets), _ptr(A), _ptr(B),

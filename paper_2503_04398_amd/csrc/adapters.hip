@@ -919,16 +919,16 @@ static int32_t run_adapters_grad(const semmoe_config* cfg, const semmoe_adapter_
   const ShrinkArgs ua{ad, X, ldx, A, scale, sh->d_in, p.part_k_in, p.parts_in, U};
   int32_t st = launch_shrink_both<F32>(va, ua, dX || dA, dB, p.shrink_tt, p.tiles(p.shrink_tt, cfg->T, sh->n_adapters), s);
   if (st != SEMMOE_OK) return st;
-  if (dX) {
-    const ExpandArgs ea{ad, V, p.parts_out, A, sh->d_in, p.chunks_in, dX_base, ld_base, dX, ldo};
-    st = launch_expand<F32, true>(ea, p.expand_tt, p.tiles(p.expand_tt, cfg->T, sh->n_adapters + 1), s);
+  if (dA || dB) {
+    const int items = int(partial_items(cfg, sh, p));
+    const OuterArgs oa{ad, V, p.parts_out, X, ldx, sh->d_in, p.seg, items, partial_a, dA};
+    const OuterArgs ob{ad, U, p.parts_in, dY, ldy, sh->d_out, p.seg, items, partial_b, dB};
+    st = launch_outer<F32>(oa, ob, s);
     if (st != SEMMOE_OK) return st;
   }
-  if (!dA && !dB) return SEMMOE_OK;
-  const int items = int(partial_items(cfg, sh, p));
-  const OuterArgs oa{ad, V, p.parts_out, X, ldx, sh->d_in, p.seg, items, partial_a, dA};
-  const OuterArgs ob{ad, U, p.parts_in, dY, ldy, sh->d_out, p.seg, items, partial_b, dB};
-  return launch_outer<F32>(oa, ob, s);
+  if (!dX) return SEMMOE_OK;  // last: dX may take the place of X or dY
+  const ExpandArgs ea{ad, V, p.parts_out, A, sh->d_in, p.chunks_in, dX_base, ld_base, dX, ldo};
+  return launch_expand<F32, true>(ea, p.expand_tt, p.tiles(p.expand_tt, cfg->T, sh->n_adapters + 1), s);
 }
 
 }  // namespace semmoe

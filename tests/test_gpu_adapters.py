@@ -273,6 +273,76 @@ def test_an_order_that_says_nonsense_stays_in_bounds():
             assert (t[:n] == 7.0).all() and (t[-n:] == 7.0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,n,rank,d_in,d_out", [
+    ([7] * 100, 130, 16, 72, 136),      # more adapters than a wave has lanes
+    ([2] * 40, 1000, 8, 64, 40),        # far more than tokens
+    ([700, 3, 900, 5, 640], 200, 24, 136, 72),  # long segments behind many empty adapters
+])
+def test_many_adapters(lens, n, rank, d_in, d_out, dtype):
+    _both(Batch(lens, [i * 37 % n for i in range(len(lens))][::-1], n, rank, d_in, d_out, dtype, pad=3, seed=n))
+
+
+@pytest.mark.parametrize("T", [2048, 8200])
+def test_larger_tiles(T):
+    """the token tiles of long batches: 32 in the first kernel, 32 and 64 in the second; 64 in both at rank 64"""
+    b = Batch([T // 3, T // 3, T - 2 * (T // 3)], [0, 1, 0], 2, 64 if T < 8192 else 16, 72, 136, "bf16", seed=T)
+    _both(b)
+
+
+def test_largest_tiles():
+    T = 16384
+    _both(Batch([9000, T - 9000 - 5], [0, 1], 2, 64, 136, 72, "bf16", pad=5, seed=3))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_gradient_in_the_place_of_its_inputs(dtype):
+    b = Batch([40, 300, 7], [0, 1, -1], 2, 16, 136, 136, dtype, pad=2, seed=16)
+    want = _gradient(b)
+    for place in ("X", "dY"):
+        X, dY, order, starts, A, B, scale, dXb = b.dev("X", "dY", "order", "starts", "A", "B", "scale", "dXb")
+        dX, dA, dB = (X if place == "X" else dY), torch.empty_like(A), torch.empty_like(B)
+        b.m.adapters_grad(X, dY, order, starts, A, B, dX=dX, dA=dA, dB=dB, dX_base=dXb, scale=scale)
+        for got, w in zip((dX[:347], dA, dB), (want[0][:347], want[1], want[2])):
+            assert torch.equal(got, w), place
+
+
+def test_calls_on_two_streams_at_once():
+    """each stream has a workspace of its own"""
+    a, c = Batch([500, 700], [0, 1], 2, 32, 1032, 1032, "bf16", seed=17), Batch([900, 300], [1, 0], 2, 32, 1032, 1032, "bf16", seed=18)
+    c.m = a.m
+    want = [_forward(a), _forward(c), *_gradient(a), *_gradient(c)]
+    ins = [x.dev("X", "dY", "order", "starts", "A", "B", "scale", "Yb", "dXb") for x in (a, c)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = [None, None]
+        for i, s in enumerate(streams):
+            X, dY, order, starts, A, B, scale, Yb, dXb = ins[i]
+            with torch.cuda.stream(s):
+                out = [torch.empty_like(Yb), torch.empty_like(X), torch.empty_like(A), torch.empty_like(B)]
+                for _ in range(4):
+                    a.m.adapters(X, order, starts, A, B, out[0], Y_base=Yb, scale=scale)
+                    a.m.adapters_grad(X, dY, order, starts, A, B, dX=out[1], dA=out[2], dB=out[3], dX_base=dXb, scale=scale)
+                got[i] = out
+        torch.cuda.synchronize()
+        assert torch.equal(got[0][0], want[0]) and torch.equal(got[1][0], want[1])
+        for x, y in zip(got[0][1:] + got[1][1:], want[2:]):
+            assert torch.equal(x, y)
+
+
+def test_no_tokens_through_the_binding():
+    b = Batch([], [], 2, 8, 16, 24, "bf16")
+    X, dY, order, starts, A, B = b.dev("X", "dY", "order", "starts", "A", "B")
+    starts.fill_(9)
+    b.m.adapter_index(torch.zeros(1, dtype=torch.int32, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV), 2, order, starts)
+    assert (starts == 0).all()
+    b.m.adapters(X, order, starts, A, B, dY)
+    dA, dB = torch.ones_like(A), torch.ones_like(B)
+    b.m.adapters_grad(X, dY, order, starts, A, B, dX=X, dA=dA, dB=dB)
+    assert (dA == 0).all() and (dB == 0).all()
+
+
 def test_no_tokens():
     b = Batch([], [], 2, 8, 16, 24, "bf16")
     m, lib = b.m, b.m.lib

@@ -146,3 +146,50 @@ def test_binding_refuses_shapes_that_do_not_fit():
         m.adapters_grad(X, Y, order, off, A, Bm, dA=torch.zeros(2, 8, 8))
     with pytest.raises(S.SemMoEError):
         m.adapter_index(torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), 2, order, off)
+
+
+def test_binding_refuses_tensors_of_other_types_and_places():
+    """host tensors and numbers of another type are refused before they reach a kernel"""
+    m = S.SemMoE(S.Config(T=8, d=16, E=4, k=2, F=8, D=2, cap=4, dtype="bf16"), allocate_workspace=False)
+    bf, i32 = dict(dtype=torch.bfloat16), dict(dtype=torch.int32)
+    X, P = torch.zeros(8, 16, **bf), torch.zeros(16, 16, **bf)
+    slots, w = torch.zeros(16, **i32), torch.zeros(8, 2)
+    for bad in (dict(Y=P.float()), dict(Y=P[:15]), dict(slots=slots.long()), dict(w=w.double()), dict(dOut=X[:7])):
+        a = dict(dOut=X, Y=P, slots=slots, w=w)
+        a.update(bad)
+        with pytest.raises(S.SemMoEError):
+            m.combine_grad(a["dOut"], a["Y"], a["slots"], a["w"], P.clone(), w.clone())
+    with pytest.raises(S.SemMoEError, match="device"):
+        m.combine_grad(X, P, slots, w, P.clone(), w.clone())
+    with pytest.raises(S.SemMoEError, match="device"):
+        m.dispatch_grad(P, slots, X)
+    off, of = torch.zeros(5, **i32), torch.zeros(4, **i32)
+    gu, dn = torch.zeros(4, 16, 16, **bf), torch.zeros(4, 16, 8, **bf)
+    with pytest.raises(S.SemMoEError, match="needed"):
+        m.expert_ffn_grad(0, P, P, off[:4], of, gu, dn, P)
+    with pytest.raises(S.SemMoEError, match="device"):
+        m.expert_ffn_grad(0, P, P, off, of, gu, dn, P)
+    with pytest.raises(S.SemMoEError, match="device"):
+        m.shared_ffn_grad(X, X, 8, gu[0], dn[0], X)
+    with pytest.raises(S.SemMoEError, match="needed"):
+        m.shared_ffn_grad(X, X, 9, gu[0], dn[0], X)
+    A, Bm = torch.zeros(2, 8, 16, **bf), torch.zeros(2, 24, 8, **bf)
+    order, starts, Y = torch.zeros(8, **i32), torch.zeros(3, **i32), torch.zeros(8, 24, **bf)
+    with pytest.raises(S.SemMoEError, match="device"):
+        m.adapters(X, order, starts, A, Bm, Y)
+    with pytest.raises(S.SemMoEError, match="needed"):
+        m.adapters(X, order, starts, A, Bm, Y.float())
+    with pytest.raises(S.SemMoEError, match="needed"):
+        m.adapters_grad(X, Y, order.long(), starts, A, Bm, dA=A.clone())
+    with pytest.raises(S.SemMoEError, match="device"):
+        m.adapter_index(torch.zeros(3, **i32), torch.zeros(2, **i32), 2, order, starts)
+
+
+def test_nothing_to_do_is_no_call():
+    """batches without a token: no address to hand over and no kernel to run"""
+    m = S.SemMoE(S.Config(T=0, d=16, E=4, k=2, F=8, D=2, cap=1, dtype="fp32"), allocate_workspace=False)
+    e = torch.empty(0, 16)
+    m.combine_grad(e, e, e, e, e, e)
+    m.dispatch_grad(e, e, e)
+    m.expert_ffn_grad(0, e, e, e, e, e, e, e)
+    m.shared_ffn_grad(e, e, 0, e, e, e)
