@@ -206,9 +206,9 @@ class SemMoE:
         self.ws = None
         self.ws_bytes = 0
         self.ws_shared = None
-        self._own_ws = {}   # workspaces of the calls that name a size of their own, by call
+        self._own_ws = {}   # workspaces of the calls that name a size of their own, by call and stream
         self._adapter_calls = {}  # config, shape and workspace bytes of the adapter calls seen, by their shapes
-        self._old_ws = []   # smaller ones before them: a captured graph may still hold their addresses
+        self._capturing = torch._C._cuda_isCurrentStreamCapturing
         self._c_config = None  # (values, C struct of them)
         if allocate_workspace:
             self.ws_bytes = self.workspace_bytes()
@@ -234,16 +234,17 @@ class SemMoE:
         return c
 
     def _workspace(self, call: str, need: int):
-        """(pointer, bytes) of a workspace that only `call` on the present stream uses, of at least `need` bytes: kept from call
-        to call, so that calls on two streams may overlap"""
+        """(pointer, bytes, owner) of a workspace that only `call` on the present stream uses, of at least `need` bytes: kept from
+        call to call, so that calls on two streams may overlap.  While a graph is captured it is of the graph's own memory and
+        goes back there when the owner does, so that graphs may run beside each other and beside calls on any stream."""
+        if self._capturing():
+            t = self._torch.empty(max(need, 256), dtype=self._torch.uint8, device=self.device)
+            return t.data_ptr(), t.numel(), t
         key = (call, _stream())
         t = self._own_ws.get(key)
         if t is None or t.numel() < need:
-            import torch
-            if t is not None:
-                self._old_ws.append(t)
-            self._own_ws[key] = t = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
-        return t.data_ptr(), t.numel()
+            self._own_ws[key] = t = self._torch.empty(max(need, 256), dtype=self._torch.uint8, device=self.device)
+        return t.data_ptr(), t.numel(), t
 
     def _fit(self, call: str, args):
         """Refuses tensors that the library would read or write past their end, or as numbers of another type, or that lie on
@@ -533,7 +534,7 @@ class SemMoE:
                   (expert_offsets, torch.int32, E + 1), (expert_of_phys, torch.int32, E),
                   (W_gu, None, 2 * F * d), (W_down, None, F * d), (dX_perm, None, P * d)))
         c = self._cfg()
-        ws, n = self._workspace("expert_ffn_grad", self._ffn_grad_bytes(P))
+        ws, n, owner = self._workspace("expert_ffn_grad", self._ffn_grad_bytes(P))
         self._check("semmoe_expert_ffn_grad", self.lib.semmoe_expert_ffn_grad(
             C.byref(c), _stream(), int(rank), _ptr(X_perm), _ptr(dY), _ptr(expert_offsets), _ptr(expert_of_phys),
             _ptr(W_gu), _ptr(W_down), _ptr(dX_perm), ws, n))
@@ -546,7 +547,7 @@ class SemMoE:
         self._fit("shared_ffn_grad", ((X, None, n * d), (dY, None, n * d), (W_gu_sh, None, 2 * F * d),
                   (W_down_sh, None, F * d), (dX, None, n * d)))
         c = self._cfg()
-        ws, size = self._workspace("shared_ffn_grad", self._ffn_grad_bytes(max(n, 0)))
+        ws, size, owner = self._workspace("shared_ffn_grad", self._ffn_grad_bytes(max(n, 0)))
         self._check("semmoe_shared_ffn_grad", self.lib.semmoe_shared_ffn_grad(
             C.byref(c), _stream(), _ptr(X), _ptr(dY), n, _ptr(W_gu_sh), _ptr(W_down_sh), _ptr(dX), ws, size))
 
@@ -619,7 +620,7 @@ class SemMoE:
                     (Y, None, 0)))
         if X.shape[0] == 0:
             return
-        ws, n = self._workspace("adapters", need)
+        ws, n, owner = self._workspace("adapters", need)
         self._check("semmoe_adapters", self.lib.semmoe_adapters(
             C.byref(c), _stream(), C.byref(s), X.data_ptr(), _ptr(order), _ptr(adapter_offsets), _ptr(A), _ptr(B), _ptr(scale),
             None if Y_base is None else Y_base.data_ptr(), Y.data_ptr(), ws, n))
@@ -639,7 +640,7 @@ class SemMoE:
                 if t is not None:
                     t.zero_()
             return
-        ws, n = self._workspace("adapters", need)
+        ws, n, owner = self._workspace("adapters", need)
         self._check("semmoe_adapters_grad", self.lib.semmoe_adapters_grad(
             C.byref(c), _stream(), C.byref(s), X.data_ptr(), dY.data_ptr(), _ptr(order), _ptr(adapter_offsets), _ptr(A), _ptr(B),
             _ptr(scale), None if dX_base is None else dX_base.data_ptr(), None if dX is None else dX.data_ptr(), _ptr(dA),

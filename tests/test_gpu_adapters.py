@@ -417,6 +417,42 @@ def test_a_larger_call_leaves_the_workspace_of_a_captured_graph_alone():
         assert torch.equal(Y, want) and (other == 77).all()
 
 
+def test_graphs_beside_each_other():
+    """a captured graph has a workspace of its own, whatever stream it was captured on and whatever runs beside it"""
+    a, c = Batch([500, 700], [0, 1], 2, 32, 1032, 1032, "bf16", seed=19), Batch([900, 300], [1, 0], 2, 32, 1032, 1032, "bf16", seed=20)
+    c.m = a.m
+    want = [[_forward(x), *_gradient(x)] for x in (a, c)]
+    capture, streams, graphs, outs = torch.cuda.Stream(), [torch.cuda.Stream(), torch.cuda.Stream()], [], []
+    kept, held = dict(a.m._own_ws), []
+    for x in (a, c):
+        X, dY, order, starts, A, B, scale, Yb, dXb = ins = x.dev("X", "dY", "order", "starts", "A", "B", "scale", "Yb", "dXb")
+        out = [torch.empty_like(Yb), torch.empty_like(X), torch.empty_like(A), torch.empty_like(B)]
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=capture):
+            a.m.adapters(X, order, starts, A, B, out[0], Y_base=Yb, scale=scale)
+            a.m.adapters_grad(X, dY, order, starts, A, B, dX=out[1], dA=out[2], dB=out[3], dX_base=dXb, scale=scale)
+        held.append(ins)
+        graphs.append(graph)
+        outs.append(out)
+    assert a.m._own_ws.keys() == kept.keys() and all(a.m._own_ws[k] is kept[k] for k in kept)
+    for _ in range(3):
+        for out in outs:
+            for t in out:
+                t.fill_(9.0)
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for s, graph in zip(streams, graphs):
+                with torch.cuda.stream(s):
+                    graph.replay()
+        eager = _forward(a)
+        torch.cuda.synchronize()
+        assert torch.equal(eager, want[0][0])
+        for out, w in zip(outs, want):
+            for got, x in zip(out, w):
+                assert torch.equal(got, x)
+
+
 def test_offsets_past_32_bits():
     """rows of a wide tensor whose last ones lie more than 2^31 elements behind the first"""
     T, d, r, wide = 66000, 64, 8, 36864
