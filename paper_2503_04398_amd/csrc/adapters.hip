@@ -745,11 +745,15 @@ static int cut_columns(int N, int tt, long long tiles) {
 // Tokens of a tile.  A tile reads the whole of its adapter's factor, so many tokens want large tiles; few want many tiles: 16 / 32 / 64
 // tokens in both kernels, us: 1000 tokens of 8 adapters, 4096 x 4096, rank 64: 23 / 29 / 43; 16384 tokens of 4, 7168 x 7168, rank 16: 204 /
 // 191 / 179, with 32 in shrink and 64 in expand 177; 4096 of 64 adapters, 2880 x 2880, rank 128: 61 / 52 / 62.
+static bool shrink_has_64(int rank) { return rank > 32 && rank <= 64; }  // the ranks where 64-token tiles of shrink pay
+
 static AdapterPlan plan_of(const semmoe_config* cfg, const semmoe_adapter_shape* s) {
   AdapterPlan p;
   const int T = cfg->T, es = int(act_bytes(cfg));
   const int mean = T / s->n_adapters, most = mean <= 24 ? 1 : (mean <= 48 ? 2 : 4);
-  const int shrink_tt = (long long)T * s->rank >= 16384 * 64 && s->rank <= 64 ? 4 : ((long long)T * s->rank >= 8192 * 64 || T >= 8192 ? 2 : 1), expand_tt = T >= 8192 ? 4 : (T >= 2048 ? 2 : 1);
+  const long long work = (long long)T * s->rank;
+  const int shrink_tt = work >= 16384 * 64 && shrink_has_64(s->rank) ? 4 : (work >= 8192 * 64 || T >= 8192 ? 2 : 1);
+  const int expand_tt = T >= 8192 ? 4 : (T >= 2048 ? 2 : 1);
   p.shrink_tt = shrink_tt < most ? shrink_tt : most;
   p.expand_tt = expand_tt < most ? expand_tt : most;
   const long long tiles = p.tiles(p.shrink_tt, T, s->n_adapters), e_tiles = p.tiles(p.expand_tt, T, s->n_adapters + 1);
@@ -836,43 +840,45 @@ template <typename F>
 static int32_t with_shrink_tiles(int rank, int tt, F f) {
   return with_rank_tiles(rank, [&](auto rt) -> int32_t {
     if (tt <= 1) return f(rt, std::integral_constant<int, 1>{});
-    if constexpr (decltype(rt)::value == 4)  // the one rank where 64 tokens pay (see plan_of)
+    if constexpr (decltype(rt)::value == 4)  // shrink_has_64
       if (tt >= 4) return f(rt, std::integral_constant<int, 4>{});
     return f(rt, std::integral_constant<int, 2>{});
   });
 }
 
 template <bool F32>
-static int32_t launch_shrink(const ShrinkArgs& a, int tt, long long tiles, hipStream_t s) {
-  if (tiles <= 0) return SEMMOE_OK;
-  if (tiles * a.parts >= kMostGroups) return SEMMOE_EUNSUPPORTED;
+static int32_t launch_shrink(const ShrinkArgs& a, int tt, hipStream_t s) {
   return with_shrink_tiles(a.ad.rank, tt, [&](auto rt, auto t4) -> int32_t {
     constexpr int RT = decltype(rt)::value, TT = decltype(t4)::value;
+    const long long tiles = AdapterPlan::tiles(TT, a.ad.T, a.ad.n_adapters);
+    if (tiles <= 0) return SEMMOE_OK;
+    if (tiles * a.parts >= kMostGroups) return SEMMOE_EUNSUPPORTED;
     static std::atomic<uint64_t> allowed{0};
     return launch_groups(shrink_kernel<F32, RT, TT>, &allowed, dim3(unsigned(tiles * a.parts)), kShrinkLds<F32, RT, TT>, s, a);
   });
 }
 
 template <bool F32>
-static int32_t launch_shrink_both(const ShrinkArgs& v, const ShrinkArgs& u, bool want_v, bool want_u, int tt, long long tiles, hipStream_t s) {
-  const long long vb = want_v ? tiles * v.parts : 0, ub = want_u ? tiles * u.parts : 0;
-  if (vb + ub <= 0) return SEMMOE_OK;
-  if (vb + ub >= kMostGroups) return SEMMOE_EUNSUPPORTED;
+static int32_t launch_shrink_both(const ShrinkArgs& v, const ShrinkArgs& u, bool want_v, bool want_u, int tt, hipStream_t s) {
   return with_shrink_tiles(v.ad.rank, tt, [&](auto rt, auto t4) -> int32_t {
     constexpr int RT = decltype(rt)::value, TT = decltype(t4)::value;
+    const long long tiles = AdapterPlan::tiles(TT, v.ad.T, v.ad.n_adapters);
+    const long long vb = want_v ? tiles * v.parts : 0, ub = want_u ? tiles * u.parts : 0;
+    if (vb + ub <= 0) return SEMMOE_OK;
+    if (vb + ub >= kMostGroups) return SEMMOE_EUNSUPPORTED;
     static std::atomic<uint64_t> allowed{0};
     return launch_groups(shrink_both_kernel<F32, RT, TT>, &allowed, dim3(unsigned(vb + ub)), kShrinkLds<F32, RT, TT>, s, v, int(vb), u);
   });
 }
 
 template <bool F32, bool TR>
-static int32_t launch_expand(const ExpandArgs& a, int tt, long long tiles, hipStream_t s) {
-  const long long groups = tiles * cdiv(a.N, a.chunks * kExpandCols);
-  if (groups <= 0) return SEMMOE_OK;
-  if (groups >= kMostGroups) return SEMMOE_EUNSUPPORTED;
+static int32_t launch_expand(const ExpandArgs& a, int tt, hipStream_t s) {
   return with_rank_tiles(a.ad.rank, [&](auto rt) -> int32_t {
     return with_token_tiles(tt, [&](auto t4) -> int32_t {
       constexpr int RT = decltype(rt)::value, TT = decltype(t4)::value;
+      const long long groups = AdapterPlan::tiles(TT, a.ad.T, a.ad.n_adapters + 1) * cdiv(a.N, a.chunks * kExpandCols);
+      if (groups <= 0) return SEMMOE_OK;
+      if (groups >= kMostGroups) return SEMMOE_EUNSUPPORTED;
       using E = Elem<F32>;
       constexpr size_t rows = (16 * RT + E::kStep - 1) / E::kStep * E::kStep;
       constexpr size_t factor = TR ? rows * 32 * E::kSize : 32 * (16 * RT + E::kPer16) * E::kSize;
@@ -904,10 +910,10 @@ static int32_t run_adapters(const semmoe_config* cfg, const semmoe_adapter_shape
                             const void* X, const AdapterArgs& ad, const void* A, const void* B, const float* scale,
                             const void* Y_base, void* Y, float* U, size_t ldx, size_t ld_base, size_t ldo) {
   const ShrinkArgs sa{ad, X, ldx, A, scale, sh->d_in, p.part_k_in, p.parts_in, U};
-  const int32_t st = launch_shrink<F32>(sa, p.shrink_tt, p.tiles(p.shrink_tt, cfg->T, sh->n_adapters), s);
+  const int32_t st = launch_shrink<F32>(sa, p.shrink_tt, s);
   if (st != SEMMOE_OK) return st;
   const ExpandArgs ea{ad, U, p.parts_in, B, sh->d_out, p.chunks_out, Y_base, ld_base, Y, ldo};
-  return launch_expand<F32, false>(ea, p.expand_tt, p.tiles(p.expand_tt, cfg->T, sh->n_adapters + 1), s);
+  return launch_expand<F32, false>(ea, p.expand_tt, s);
 }
 
 template <bool F32>
@@ -917,7 +923,7 @@ static int32_t run_adapters_grad(const semmoe_config* cfg, const semmoe_adapter_
                                  float* partial_a, float* partial_b, size_t ldx, size_t ldy, size_t ld_base, size_t ldo) {
   const ShrinkArgs va{ad, dY, ldy, B, scale, sh->d_out, p.part_k_out, p.parts_out, V};
   const ShrinkArgs ua{ad, X, ldx, A, scale, sh->d_in, p.part_k_in, p.parts_in, U};
-  int32_t st = launch_shrink_both<F32>(va, ua, dX || dA, dB, p.shrink_tt, p.tiles(p.shrink_tt, cfg->T, sh->n_adapters), s);
+  int32_t st = launch_shrink_both<F32>(va, ua, dX || dA, dB, p.shrink_tt, s);
   if (st != SEMMOE_OK) return st;
   if (dA || dB) {
     const int items = int(partial_items(cfg, sh, p));
@@ -928,7 +934,7 @@ static int32_t run_adapters_grad(const semmoe_config* cfg, const semmoe_adapter_
   }
   if (!dX) return SEMMOE_OK;  // last: dX may take the place of X or dY
   const ExpandArgs ea{ad, V, p.parts_out, A, sh->d_in, p.chunks_in, dX_base, ld_base, dX, ldo};
-  return launch_expand<F32, true>(ea, p.expand_tt, p.tiles(p.expand_tt, cfg->T, sh->n_adapters + 1), s);
+  return launch_expand<F32, true>(ea, p.expand_tt, s);
 }
 
 }  // namespace semmoe

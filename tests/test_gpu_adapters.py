@@ -295,6 +295,12 @@ def test_largest_tiles():
     _both(Batch([9000, T - 9000 - 5], [0, 1], 2, 64, 136, 72, "bf16", pad=5, seed=3))
 
 
+@pytest.mark.parametrize("T,rank", [(65600, 16), (32800, 32), (40000, 40), (16400, 128), (131100, 8)])
+def test_long_batches_of_every_rank(T, rank):
+    """T * rank past every line of the tiles' choice, where only some ranks have the largest tiles"""
+    _both(Batch([T // 2 + 11, 3, T - T // 2 - 30], [1, 2, 0], 3, rank, 40, 72, "bf16", pad=16, seed=rank))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_gradient_in_the_place_of_its_inputs(dtype):
     b = Batch([40, 300, 7], [0, 1, -1], 2, 16, 136, 136, dtype, pad=2, seed=16)
