@@ -180,6 +180,8 @@ __global__ __launch_bounds__(64 * NWF * NWT, 1) void gemm_nn_ring_kernel(GemmArg
 // 128 TI bytes, its rows advance by 64 ldw a slice, and a weight fragment is two transposing reads of 8 bytes a lane.
 // Where K is no multiple of 64 the last slice is the last 64 rows of K once more in part: what the slice before held is masked out of
 // its fragments (K % 8 == 0: whole halves of a wave).  Needs more than NSTAGE slices.
+// Measured, 16 experts of 1300 rows, d 2048, F 768, 256 x 128 tiles and pieces: dh (K 2048) 94 to 105 us, 0.62 to 0.70 PFLOP/s; dX (K
+// 1536) 142 to 158 us, 0.83 to 0.93.  128 experts of 62 rows, 128 x 128: 104 and 173 us, 4.4 and 5.0 TB/s of weights, rows and sums.
 // ------------------------------------------------------------------------------------------------
 template <int TI, int TJ, int NSTAGE>
 struct NnW4Cfg {
@@ -503,11 +505,13 @@ __global__ __launch_bounds__(256, 1) void gemm_nn_split_kernel(GemmArgs head, Ge
 
 // ------------------------------------------------------------------------------------------------
 // fp32 (v_mfma_f32_16x16x4_f32: full fp32 products and sums).  64 weight columns x 16 TT tokens; NW waves cut K between them, 16
-// weight rows at a time: four, or eight where the tiles do not fill the chip.  A lane's 16 bytes of a weight row are four consecutive columns, which are row l16 of four MFMA tiles (tile
-// i has the columns 4 m + i), and its 16 bytes of a token row the k of four MFMAs in turn, so the operands come from memory as
-// they are used, a weight row in runs of 256 bytes, AHEAD steps ahead and without a barrier; a lane ends with four consecutive columns.
-// What bounds it: few rows, the weights' stream; many, the matrix pipe, 32 cycles each of these.  (As 128 x 32 tiles that share LDS
-// slices 16 experts of 32 rows, d 512, F 1024 had 64 workgroups: 62 us for K 2048.)
+// weight rows at a time: four, or eight where the tiles do not fill the chip.  A lane's 16 bytes of a weight row are four
+// consecutive columns, which are row l16 of four MFMA tiles (tile i has the columns 4 m + i), and its 16 bytes of a token row the
+// k of four MFMAs in turn, so the operands come from memory as they are used, a weight row in runs of 256 bytes, AHEAD steps
+// ahead and without a barrier; a lane ends with four consecutive columns.
+// What bounds it: the matrix pipe, 32 cycles an instruction, on tiles that ragged groups half fill, and with few rows the walk's
+// start and end.  Measured, 16 experts of 32 rows, d 512, F 1024: K 512 18 us, K 2048 31 us, of which the products are 14.  (As 128 x 32
+// tiles that share LDS slices that was 64 workgroups: 62 us for K 2048.)
 // ------------------------------------------------------------------------------------------------
 template <int MODE, int TT, int NW>
 __global__ __launch_bounds__(64 * NW) void gemm_nn_f32_kernel(GemmArgs a) {

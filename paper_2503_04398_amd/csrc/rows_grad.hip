@@ -4,7 +4,8 @@
 //
 // Both stream: combine's gradient reads P + T rows and writes P, one workgroup a token, a 16-byte piece a thread and pass, the
 // k rows of a piece requested before the first is used.  The k dot products are kept in registers over the walk and meet once
-// at its end, in a fixed order.
+// at its end, in a fixed order.  Y is read past the caches: it comes once, and dY is what the next kernel reads.
+// Measured, bf16, 16384 tokens of 7168, 8 rows each: 4.0 GB in 767 to 775 us, 5.2 TB/s where a copy of that size reaches 4.8.
 #include "common.hpp"
 
 namespace semmoe {

@@ -231,7 +231,7 @@ def test_ffn_grad_in_place(alias):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("n,d,F", [(1, 64, 64), (31, 264, 72), (200, 512, 384), (777, 192, 640)])
+@pytest.mark.parametrize("n,d,F", [(1, 64, 64), (31, 264, 72), (200, 512, 384), (777, 192, 640), (9000, 520, 1160)])
 def test_shared_ffn_grad(n, d, F, dtype):
     r = np.random.default_rng(n)
     m = _layer(n, 1, d, dtype, F=F)
