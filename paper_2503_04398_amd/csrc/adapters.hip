@@ -119,20 +119,6 @@ __device__ __forceinline__ bool find_item(const AdapterArgs& a, int n_groups, in
   return false;
 }
 
-// The sum over the parts of four numbers of u: four loads in flight at a time, added in order.
-__device__ __forceinline__ f32x4_t sum_parts(const float* p, size_t plane, int parts) {
-  f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int q = 0; q < parts; q += 4) {
-    f32x4_t v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const f32x4_t*>(p + plane * min(q + i, parts - 1));
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (q + i < parts) s += v[i];
-  }
-  return s;
-}
-
 // ---- shrink: U[part][position][j] = s_a * sum over the part's k of R[token, k] F_a(j, k) ------------------------------
 // TR = false: F_a = A_a [rank][K], rows along k.  TR = true: F_a = B_a [K][rank].
 //
@@ -562,12 +548,29 @@ __device__ __forceinline__ void outer_body(const OuterArgs& a, int block, unsign
     for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4_t*>(r_at(i * 16 + l_row, (tid & 15) * 16)) = xb[i];
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-      const int t = (i * 256 + tid) / (RT * 4), j = (i * 256 + tid) % (RT * 4) * 4;
-      f32x4_t v = ub[i][0];
 #pragma unroll
-      for (int x = 1; x < UP; ++x) v += ub[i][x];
-      if (a.parts > UP && p + t < p1 && j < r)
-        v += sum_parts(a.U + (size_t(UP) * a.ad.T + p + t) * r + j, size_t(a.ad.T) * r, a.parts - UP);
+      for (int x = 1; x < UP; ++x) ub[i][0] += ub[i][x];
+    }
+    // the planes behind them, all numbers of two at a time
+    for (int x0 = UP; x0 < a.parts; x0 += 2) {
+      f32x4_t more[2][NU];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < NU; ++i) {
+          const int t = (i * 256 + tid) / (RT * 4), j = (i * 256 + tid) % (RT * 4) * 4;
+          more[x][i] = p + t < p1 && j < r && x0 + x < a.parts
+                           ? *reinterpret_cast<const f32x4_t*>(a.U + (size_t(x0 + x) * a.ad.T + p + t) * r + j) : f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < NU; ++i) ub[i][0] += more[x][i];
+    }
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      const int t = (i * 256 + tid) / (RT * 4), j = (i * 256 + tid) % (RT * 4) * 4;
+      const f32x4_t v = ub[i][0];
       unsigned char* const o = Us + t * RBU + j * E::kSize;
       if constexpr (F32) *reinterpret_cast<f32x4_t*>(o) = v;
       else *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
