@@ -731,14 +731,16 @@ struct AdapterPlan {
   static long long tiles(int tt, int T, int groups) { return T / (16 * tt) + (groups < T ? groups : T); }
 };
 
-// K cut into parts until there are some 400 workgroups.  Every part is a plane that each reader of u adds: 4096 x 4096, rank 16 on 256
-// tokens of 8 adapters (24 tiles) 8.7 us with 8 parts, 10.1 with 16; 512 tokens (36 tiles) 10.1 / 11.6 / 15.2 with 5 / 10 / 16; 2048
-// tokens (132 tiles) 21.6 / 18.9 / 17.3 with 1 / 2 / 5.
-static void cut_k(int K, int es, long long tiles, int* part_k, int* parts) {
+// K cut into parts until there are some 400 workgroups, 140 to 280 of ranks past 64, whose steps are longer; at most 4: every part is a
+// plane that each reader of u adds, a few at a time.  4096 x 4096, us as captured graphs, with 1 / 2 / 3 / 4 / 6 / 8 parts: forward of 500 tokens of 8
+// adapters, rank 64 (39 tiles) 24.4 / 17.8 / 18.0 / 16.3 / 21.0 / 20.9, gradient 35.1 / 29.1 / 28.6 / 27.2 / 30.6 / 31.1; 256 tokens of
+// 64, rank 16 forward 12.9 / 10.9 / 10.5 / 10.1 / 10.1 / 10.1; 1000 tokens of 8, 2880 columns, rank 128 (70 tiles), gradient 63.0 / 62.1 /
+// 67.5 / 72.7 / 73.1 / 73.5, 2000 tokens (133 tiles), 4096 columns, forward 40.8 / 32.5 / 36.3 / 36.4; but fp32, 79 tokens of one, 568 and 4808 columns, rank 128 (5 tiles) 92 / 58 / 50 / 45 / 44 / 43.
+static void cut_k(int K, int es, int rank, long long tiles, int* part_k, int* parts) {
   const int unit = 512 / es;  // a slice for each of the four waves
   const int units = cdiv(K, unit);
-  long long want = tiles > 0 ? 400 / tiles : 1;
-  want = want < 1 ? 1 : (want > 6 ? 6 : want);
+  long long want = tiles > 0 ? (rank > 64 ? (140 + tiles - 1) / tiles : 400 / tiles) : 1;
+  want = want < 1 ? 1 : (want > 4 ? 4 : want);
   const int per = cdiv(units, int(want < units ? want : units));
   *part_k = per * unit;
   *parts = cdiv(units, per);
@@ -769,8 +771,8 @@ static AdapterPlan plan_of(const semmoe_config* cfg, const semmoe_adapter_shape*
   p.shrink_tt = shrink_tt < most ? shrink_tt : most;
   p.expand_tt = expand_tt < most ? expand_tt : most;
   const long long tiles = p.tiles(p.shrink_tt, T, s->n_adapters), e_tiles = p.tiles(p.expand_tt, T, s->n_adapters + 1);
-  cut_k(s->d_in, es, tiles, &p.part_k_in, &p.parts_in);
-  cut_k(s->d_out, es, tiles, &p.part_k_out, &p.parts_out);
+  cut_k(s->d_in, es, s->rank, tiles, &p.part_k_in, &p.parts_in);
+  cut_k(s->d_out, es, s->rank, tiles, &p.part_k_out, &p.parts_out);
   p.chunks_in = cut_columns(s->d_in, p.expand_tt, e_tiles);
   p.chunks_out = cut_columns(s->d_out, p.expand_tt, e_tiles);
   // Segments until there are some 512 workgroups; a slice of 64 tokens takes one 1 to 3 us, a segment more a launch that joins (862 tokens of
