@@ -102,15 +102,15 @@ static int32_t launch_nn_f32(const GemmArgs& a, int max_rows, int est, hipStream
   return launch_nn_f32<MODE, 1>(a, max_rows, est, s);
 }
 
-// Tile shapes.  Means of rows an expert, 8 shapes of 1 to 128 experts (d 1024 to 7168, F 512 to 2880), groups spread lognormally
-// by 0.3; FFN gradients in us with one of the two products as 128 x 64 / 128 x 128 / 256 x 128 and pieces / 256 x 256 and pieces:
-//   * 128 columns x 64 tokens, ring of 4, while such tiles have a compute unit each: dh of 8 experts, d 7168, F 2048, 90 rows
-//     353 / 365 / 395 / 442, 130 rows 404 / 377; one expert of these, 900 rows 182 / 190, 1300 rows 317 / 278
-//   * 128 x 128 up to 80 rows, where the weights' stream is the time (128 experts of 40, d 2048, F 768: 414 / 407 / 411 / 427),
-//     and beyond while they have one each (16 experts of 90, d 4096, F 1536, dh: 279 / 263 / 283 / 312; 130 rows 310 / 327 / 314 / 341)
-//   * 256 x 256 from 192 rows on with five quarters of a round of them (8 experts of 400, d 7168, dx: 741 / 655 / 620 / 604; 600 rows of d
-//     2880, 273 tiles: 630 / 531 / 511 / 528), or, with groups of 1024 rows and more, three fifths (16 experts of 1300, d 2048, F
-//     768, dh: 456 / 437 / 428 / 422); 256 x 128 else
+// Tile shapes.  Means of rows an expert, groups spread lognormally by 0.3; FFN gradients in us with one of the two products as 128 x 128 /
+// 256 x 128 and pieces / 256 x 256 and pieces:
+//   * 128 x 128 up to 80 rows (128 experts of 40, d 2048, F 768: 407 / 411 / 427) and while they have a compute unit each (16
+//     experts of 90, d 4096, F 1536, dh: 263 / 283 / 312; 130 rows 327 / 314 / 341).  128 x 64 tiles are behind these even where they leave
+//     half the chip idle, 64 x 64 ones too: a slice costs a wave much the same (one expert of 64 rows, d 7168, F 2048, dh: 172, 187 as
+//     128 x 64, 170 as 64 x 64, dX 180 / 187 / 178; 8 of 90 rows, dX: 368 / 423; 16 of 48, d 2048, F 768, dX: 71 / 90 / 94)
+//   * 256 x 256 from 192 rows on with five quarters of a round of them (8 experts of 400, d 7168, dx: 655 / 620 / 604; 600 rows of d
+//     2880, 273 tiles: 531 / 511 / 528), or, with groups of 1024 rows and more, three fifths (16 experts of 1300, d 2048, F
+//     768, dh: 437 / 428 / 422); 256 x 128 else
 // Shapes whose K is shorter than a ring, or with more groups than the tables hold, take 128 x 64 tiles with a barrier a slice.
 template <int MODE>
 static int32_t launch_nn_bf16(const GemmArgs& a, int max_rows, int est, hipStream_t s) {
@@ -126,7 +126,6 @@ static int32_t launch_nn_bf16(const GemmArgs& a, int max_rows, int est, hipStrea
     const long long rows = !a.offsets ? 100ll * cdiv(est, bt) : (est * 2 <= bt ? 100ll : 100ll * est / bt + 50);
     return a.nq * rows * cdiv(a.N, bw);
   };
-  if (tiles(128, 64) <= 100 * cus && nn_w4_fits<2, 1, 4>(a)) return launch_nn_w4<MODE, 2, 1, 4, 1>(a, max_rows, s);
   if (nn_w4_fits<2, 2, 3>(a)) {
     if (est < 80 || tiles(128, 128) <= 110 * cus) return launch_nn_w4<MODE, 2, 2, 3, 1>(a, max_rows, s);
     const long long big = tiles(256, 256);

@@ -186,7 +186,7 @@ def test_ffn_grad(rows, d, F, dtype):
 
 
 # every tile shape with K in whole slices and with a last one that is half, barely or nearly full, columns that end inside a tile:
-# few tiles (128 x 64), few rows (128 x 128), 80 rows and more (256 x 128), 192 and more with many tiles (256 x 256)
+# few rows or few tiles (128 x 128), 80 rows and more (256 x 128), 192 and more with many tiles (256 x 256)
 @pytest.mark.parametrize("rows,d,F", [
     ((70, 20, 5), 520, 264), ((3, 40) * 20, 776, 648), ((90, 130, 100) * 16, 1032, 328), ((250, 200, 300, 190) * 14, 520, 712),
     ((250, 200, 300, 190) * 8, 1016, 776), ((130,) * 40, 312, 1016), ((1100, 1400, 900, 1300) * 2, 568, 1160)])
