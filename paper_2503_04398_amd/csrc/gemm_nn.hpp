@@ -180,8 +180,8 @@ __global__ __launch_bounds__(64 * NWF * NWT, 1) void gemm_nn_ring_kernel(GemmArg
 // 128 TI bytes, its rows advance by 64 ldw a slice, and a weight fragment is two transposing reads of 8 bytes a lane.
 // Where K is no multiple of 64 the last slice is the last 64 rows of K once more in part: what the slice before held is masked out of
 // its fragments (K % 8 == 0: whole halves of a wave).  Needs more than NSTAGE slices.
-// Measured, 16 experts of 1300 rows, d 2048, F 768, 256 x 128 tiles and pieces: dh (K 2048) 94 to 105 us, 0.62 to 0.70 PFLOP/s; dX (K
-// 1536) 142 to 158 us, 0.83 to 0.93.  128 experts of 62 rows, 128 x 128: 104 and 173 us, 4.4 and 5.0 TB/s of weights, rows and sums.
+// Measured, 16 experts of 1300 rows, d 2048, F 768, 256 x 256 tiles and pieces: dh (K 2048) 94 to 105 us, 0.62 to 0.70 PFLOP/s; dX (K
+// 1536) 142 to 160 us, 0.82 to 0.93.  128 experts of 62 rows, 128 x 128: 102 and 172 us at best, 4.5 and 5.0 TB/s of weights, rows and sums.
 // ------------------------------------------------------------------------------------------------
 template <int TI, int TJ, int NSTAGE>
 struct NnW4Cfg {
