@@ -206,7 +206,7 @@ class SemMoE:
         self.ws = None
         self.ws_bytes = 0
         self.ws_shared = None
-        self._own_ws = {}   # workspaces of the calls that name a size of their own, by call and stream
+        self._own_ws = {}   # workspaces of the calls that name a size of their own, by call, device and stream
         self._adapter_calls = {}  # config, shape and workspace bytes of the adapter calls seen, by their shapes
         self._capturing = torch._C._cuda_isCurrentStreamCapturing
         self._c_config = None  # (values, C struct of them)
@@ -235,15 +235,17 @@ class SemMoE:
 
     def _workspace(self, call: str, need: int):
         """(pointer, bytes, owner) of a workspace that only `call` on the present stream uses, of at least `need` bytes: kept from
-        call to call, so that calls on two streams may overlap.  While a graph is captured it is of the graph's own memory and
-        goes back there when the owner does, so that graphs may run beside each other and beside calls on any stream."""
+        call to call, so that calls on two streams may overlap.  It lies on the current device, where the call's tensors have
+        been found.  While a graph is captured it is of the graph's own memory and goes back there when the owner does, so that
+        graphs may run beside each other and beside calls on any stream."""
+        dev = self._types[0]()
         if self._capturing():
-            t = self._torch.empty(max(need, 256), dtype=self._torch.uint8, device=self.device)
+            t = self._torch.empty(max(need, 256), dtype=self._torch.uint8, device=dev)
             return t.data_ptr(), t.numel(), t
-        key = (call, _stream())
+        key = (call, dev, _stream())  # a default stream's handle is the same on every device
         t = self._own_ws.get(key)
         if t is None or t.numel() < need:
-            self._own_ws[key] = t = self._torch.empty(max(need, 256), dtype=self._torch.uint8, device=self.device)
+            self._own_ws[key] = t = self._torch.empty(max(need, 256), dtype=self._torch.uint8, device=dev)
         return t.data_ptr(), t.numel(), t
 
     def _fit(self, call: str, args):

@@ -193,3 +193,32 @@ def test_nothing_to_do_is_no_call():
     m.dispatch_grad(e, e, e)
     m.expert_ffn_grad(0, e, e, e, e, e, e, e)
     m.shared_ffn_grad(e, e, 0, e, e, e)
+
+
+def test_workspaces_of_devices_streams_and_graphs_are_apart(monkeypatch):
+    """a default stream has the same handle on every device, and a graph's workspace is no other's"""
+    m = S.SemMoE(S.Config(T=64, d=64, E=16, k=2, F=32, D=4, cap=16), allocate_workspace=False)
+    now, made = {"dev": 0, "stream": 0, "capturing": False}, []
+
+    class Torch:
+        uint8 = torch.uint8
+
+        @staticmethod
+        def empty(n, dtype, device):
+            made.append(device)
+            return torch.empty(n, dtype=dtype)
+    m._torch, m._capturing, m._types = Torch, lambda: now["capturing"], (lambda: now["dev"],) + m._types[1:]
+    monkeypatch.setattr(B, "_stream", lambda: now["stream"])
+
+    def get(call="adapters", need=1000, **at):
+        now.update({"dev": 0, "stream": 0, "capturing": False, **at})
+        p, n, owner = m._workspace(call, need)
+        assert n >= need and p == owner.data_ptr()
+        return owner
+    first = get()
+    others = [get(dev=1), get(stream=7), get("shared_ffn_grad"), get(capturing=True), get(capturing=True)]
+    assert made == [0, 1, 0, 0, 0, 0]
+    assert len({t.data_ptr() for t in [first] + others}) == 6
+    assert get(need=900) is first and get(dev=1) is others[0] and get(stream=7) is others[1]
+    larger = get(need=5000)
+    assert larger is not first and get() is larger and get(dev=1) is others[0]
