@@ -74,7 +74,8 @@ __global__ __launch_bounds__(512) void combine_grad_kernel(int k, int row_chunks
       }
 #pragma unroll
       for (int j = 0; j < G; ++j) {
-        if constexpr (DOTS) acc[g0 + j] = g.dot(Piece<BF16>(v[j]), acc[g0 + j]);
+        if constexpr (DOTS)  // zeros in the place of a missing row would be NaN beside an infinite number
+          if (sl[g0 + j] >= 0) acc[g0 + j] = g.dot(Piece<BF16>(v[j]), acc[g0 + j]);
         if constexpr (ROWS)
           if (sl[g0 + j] >= 0) dY[size_t(sl[g0 + j]) * row_chunks + c] = g.times(wt[g0 + j]);
       }

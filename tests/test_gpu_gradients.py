@@ -120,6 +120,28 @@ def test_infinite_and_missing_numbers_stay_in_their_rows():
     assert torch.equal(bad_dY[rows], dY[rows])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_a_pair_without_a_row_has_no_gradient_whatever_its_token_holds(bad, dtype):
+    """a slot outside [0,P) beside numbers of dOut that are not finite: dtopk_w is 0 there, as it is beside finite ones"""
+    r = np.random.default_rng(5)
+    T, k, d = 6, 3, 72
+    m = _layer(T, k, d, dtype)
+    dOut, Y = _rand(r, (T, d), dtype), _rand(r, (T * k, d), dtype).to(DEV)
+    dOut[1, 7], dOut[4] = bad, bad
+    slots = torch.from_numpy(r.permutation(T * k).astype(np.int32))
+    gone = [1 * k + 2, 2 * k, 4 * k, 4 * k + 1]
+    slots[gone] = torch.tensor([-1, T * k, T * k + 7, -2 ** 31], dtype=torch.int32)
+    w = torch.from_numpy(r.random((T, k), dtype=np.float32)).to(DEV)
+    for rows in (True, False):
+        dY, dw = torch.full_like(Y, 7.0), torch.full((T, k), 7.0, device=DEV)
+        m.combine_grad(dOut.to(DEV), Y, slots.to(DEV), w, dY if rows else None, dw)
+        got = dw.view(-1).cpu()
+        assert (got[gone] == 0.0).all(), got[gone]
+        there = [p for p in (1 * k, 1 * k + 1, 4 * k + 2)]
+        assert not torch.isfinite(got[there]).any()
+
+
 # ---- the expert FFN
 def _ffn_tolerance(x, dy, w_gu, w_dn, dtype):
     """see above; of rows x, dy of one expert"""
