@@ -20,11 +20,13 @@ __device__ __forceinline__ uint4 load_stream16(const uint4* p) {
 // 4 rows each: 179 -> 164.  A result that the memory-side cache can hold for its reader is stored as before.
 // WEIGHTED = false: weights of one, topk_w is not read (the gradient of dispatch: 2.35 GB of these rows and an addend in 473 to 480 us,
 // 4.9 TB/s).
+// Out may be Y_shared (dispatch_grad's dX in the place of dX_add), so neither is __restrict__: a thread reads each piece before it
+// writes it, and the machine code is the same.
 template <bool BF16, int KU, bool NTOUT, bool WEIGHTED>
 __global__ __launch_bounds__(512) void combine_kernel(int k, int row_chunks, int P, const uint4* __restrict__ Y,
                                                       const int32_t* __restrict__ slot_of_pair,
                                                       const float* __restrict__ topk_w,
-                                                      const uint4* __restrict__ Y_shared, uint4* __restrict__ Out) {
+                                                      const uint4* Y_shared, uint4* Out) {
   const int tok = blockIdx.x;
   auto put = [&](int c, uint4 v) {
     if constexpr (NTOUT)

@@ -1,5 +1,8 @@
 """CPU-only: the adapter and gradient calls check their arguments before they touch a GPU."""
 import ctypes as C
+import os
+import re
+import subprocess
 
 import numpy as np
 import pytest
@@ -7,6 +10,7 @@ import torch
 
 import paper_2503_04398_amd as S
 from paper_2503_04398_amd import binding as B
+from paper_2503_04398_amd import build as BLD
 
 EINVAL, ESHAPE, EWORKSPACE, EUNSUPPORTED = -1, -2, -3, -5
 
@@ -222,3 +226,22 @@ def test_workspaces_of_devices_streams_and_graphs_are_apart(monkeypatch):
     assert get(need=900) is first and get(dev=1) is others[0] and get(stream=7) is others[1]
     larger = get(need=5000)
     assert larger is not first and get() is larger and get(dev=1) is others[0]
+
+
+@pytest.mark.skipif(not os.path.exists(BLD.HIPCC), reason="needs the compiler")
+@pytest.mark.parametrize("source,kernel,may_coincide", [
+    ("combine.hip", "combine_kernel", (6, 7)),         # dispatch_grad: dX may be dX_add
+    ("rows_grad.hip", "combine_grad_kernel", (4, 7)),  # combine_grad: dY may be Y
+])
+def test_kernels_do_not_deny_that_a_result_lies_in_the_place_of_an_input(source, kernel, may_coincide):
+    """what the compiler was told of pointers that the header lets coincide: none of them is `noalias`"""
+    cmd = [BLD.HIPCC] + [f for f in BLD.HIP_FLAGS if f != "-fPIC"] + ["-O1", "--cuda-device-only", "-S", "-emit-llvm", "-o", "-",
+                                                                        os.path.join(BLD.CSRC, source)]
+    text = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True, check=True, timeout=120).stdout
+    heads = re.findall(r"^define [^\n]*amdgpu_kernel void @_ZN6semmoe\d+%sI\w+\((.*)\) \S*unnamed_addr" % kernel, text, re.M)
+    assert heads
+    for head in heads:
+        args = re.split(r", (?=ptr |i32 )", head)
+        for i in may_coincide:
+            assert args[i].startswith("ptr") and "noalias" not in args[i], args[i]
+        assert any("noalias" in a for a in args)  # the word means what the test takes it for
