@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import operator
 import os
+import threading
 from dataclasses import dataclass
 from typing import Optional
 
@@ -193,8 +194,18 @@ def _stream():
     return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
 
 
+class _OfThread(threading.local):
+    """what a thread keeps for itself; it goes when the thread ends"""
+
+    def __init__(self):
+        self.workspaces = {}
+
+
 class SemMoE:
-    """One config + one workspace; methods mirror the C entry points one to one."""
+    """One config + one workspace; methods mirror the C entry points one to one.
+
+    Calls that use the workspace of the config (`ws`, `ws_shared`) take their turns on one stream.  Those that name a size of their own
+    (the FFN gradients and the adapters) may be made from several threads and on several streams at once."""
 
     def __init__(self, cfg: Config, device="cuda:0", allocate_workspace: bool = True):
         import torch
@@ -206,7 +217,7 @@ class SemMoE:
         self.ws = None
         self.ws_bytes = 0
         self.ws_shared = None
-        self._own_ws = {}   # workspaces of the calls that name a size of their own, by call, device and stream
+        self._mine = _OfThread()
         self._adapter_calls = {}  # config, shape and workspace bytes of the adapter calls seen, by their shapes
         self._capturing = torch._C._cuda_isCurrentStreamCapturing
         self._c_config = None  # (values, C struct of them)
@@ -233,10 +244,15 @@ class SemMoE:
             setattr(c, k_, v)
         return c
 
+    @property
+    def _own_ws(self):
+        """this thread's workspaces of the calls that name a size of their own, by call, device and stream"""
+        return self._mine.workspaces
+
     def _workspace(self, call: str, need: int):
-        """(pointer, bytes, owner) of a workspace that only `call` on the present stream uses, of at least `need` bytes: kept from
-        call to call, so that calls on two streams may overlap.  It lies on the current device, where the call's tensors have
-        been found.  While a graph is captured it is of the graph's own memory and goes back there when the owner does, so that
+        """(pointer, bytes, owner) of a workspace that only `call` of this thread on the present stream uses, of at least `need`
+        bytes: kept from call to call, so that calls on two streams may overlap, and calls of two threads on one, whose launches may
+        come in turns.  It lies on the current device, where the call's tensors have been found.  While a graph is captured it is of the graph's own memory and goes back there when the owner does, so that
         graphs may run beside each other and beside calls on any stream."""
         dev = self._types[0]()
         if self._capturing():

@@ -7,6 +7,8 @@ r = u for bf16 rows (h is rounded once as an operand, Y once) and e for fp32, n_
 worst case of any order of adding).  dX is the same chain.  dA = sum over t tokens of v x^T has |v| |x| summed over the tokens
 in the place of |B| |h|, and so dB.  Each entry is held to that; and the whole, whose roundings do not all point the same
 way, to 2^-8 (bf16) or 2e-6 (fp32: e times the square root of the terms, thrice) of its norm."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -486,3 +488,34 @@ def test_offsets_past_32_bits():
         want = _np(B[a]) @ (_np(A[a]) @ _np(X[t]))
         # one rounding of h as an operand, one of the result
         assert np.linalg.norm(_np(Y[t]) - want) <= 2.0 ** -7 * np.linalg.norm(want)
+
+
+def test_calls_of_two_threads_on_one_stream():
+    """the launches of two threads' calls may come in turns: each thread has sums of its own"""
+    a, c = Batch([500, 700], [0, 1], 2, 32, 1032, 1032, "bf16", seed=21), Batch([900, 300], [1, 0], 2, 32, 1032, 1032, "bf16", seed=22)
+    want = [[_forward(x), *_gradient(x)] for x in (a, c)]
+    ins = [x.dev("X", "dY", "order", "starts", "A", "B", "scale", "Yb", "dXb") for x in (a, c)]
+    outs = [[torch.empty_like(t) for t in (i[7], i[0], i[4], i[5])] for i in ins]
+    torch.cuda.synchronize()
+    start, failed = threading.Barrier(2), []
+
+    def work(i):
+        X, dY, order, starts, A, B, scale, Yb, dXb = ins[i]
+        Y, dX, dA, dB = outs[i]
+        start.wait()
+        try:
+            for _ in range(100):
+                a.m.adapters(X, order, starts, A, B, Y, Y_base=Yb, scale=scale)
+                a.m.adapters_grad(X, dY, order, starts, A, B, dX=dX, dA=dA, dB=dB, dX_base=dXb, scale=scale)
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed
+    for out, w in zip(outs, want):
+        for got, x in zip(out, w):
+            assert torch.equal(got, x)

@@ -1,8 +1,11 @@
 """CPU-only: the adapter and gradient calls check their arguments before they touch a GPU."""
 import ctypes as C
+import gc
 import os
 import re
 import subprocess
+import threading
+import weakref
 
 import numpy as np
 import pytest
@@ -245,3 +248,35 @@ def test_kernels_do_not_deny_that_a_result_lies_in_the_place_of_an_input(source,
         for i in may_coincide:
             assert args[i].startswith("ptr") and "noalias" not in args[i], args[i]
         assert any("noalias" in a for a in args)  # the word means what the test takes it for
+
+
+def test_workspaces_of_threads_are_apart(monkeypatch):
+    """a call enqueues several launches, and those of two threads on one stream may come in turns: neither finds the other's sums"""
+    m = S.SemMoE(S.Config(T=64, d=64, E=16, k=2, F=32, D=4, cap=16), allocate_workspace=False)
+
+    class Torch:
+        uint8 = torch.uint8
+
+        @staticmethod
+        def empty(n, dtype, device):
+            return torch.empty(n, dtype=dtype)
+    m._torch, m._capturing, m._types = Torch, lambda: False, (lambda: 0,) + m._types[1:]
+    monkeypatch.setattr(B, "_stream", lambda: 0)
+    mine = m._workspace("adapters", 1000)[2]
+    both, theirs, gone = threading.Barrier(2), [], []
+
+    def work():
+        first = m._workspace("adapters", 1000)[2]
+        both.wait()
+        theirs.append(first.data_ptr())
+        assert m._workspace("adapters", 900)[2] is first
+        both.wait()  # neither has ended before the other's is seen
+        gone.append(weakref.ref(first))
+    threads = [threading.Thread(target=work) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len({mine.data_ptr(), *theirs}) == 3 and m._workspace("adapters", 1000)[2] is mine
+    gc.collect()
+    assert [r() for r in gone] == [None, None]  # a thread's workspaces go with it
