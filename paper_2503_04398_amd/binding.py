@@ -208,10 +208,7 @@ class SemMoE:
     (the FFN gradients and the adapters) may be made from several threads and on several streams at once."""
 
     def __init__(self, cfg: Config, device="cuda:0", allocate_workspace: bool = True):
-        import torch
         self.lib = load_library()
-        self._torch = torch
-        self._types = torch._C._cuda_getDevice, torch.int32, torch.float32, (torch.float32, torch.bfloat16)
         self.cfg = cfg
         self.device = device
         self.ws = None
@@ -219,13 +216,24 @@ class SemMoE:
         self.ws_shared = None
         self._mine = _OfThread()
         self._adapter_calls = {}  # config, shape and workspace bytes of the adapter calls seen, by their shapes
-        self._capturing = torch._C._cuda_isCurrentStreamCapturing
         self._c_config = None  # (values, C struct of them)
         if allocate_workspace:
+            import torch
             self.ws_bytes = self.workspace_bytes()
             self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
 
     # -- helpers
+    def __getattr__(self, name):
+        """What the calls on the GPU ask of torch, looked up by the first of them and kept: the host's calls need neither torch nor
+        one that knows a GPU."""
+        if name not in ("_torch", "_types", "_capturing"):
+            raise AttributeError("%s has no %s" % (type(self).__name__, name))
+        import torch
+        for n, v in (("_torch", torch), ("_capturing", torch._C._cuda_isCurrentStreamCapturing),
+                     ("_types", (torch._C._cuda_getDevice, torch.int32, torch.float32, (torch.float32, torch.bfloat16)))):
+            self.__dict__.setdefault(n, v)
+        return self.__dict__[name]
+
     def _check(self, name: str, st: int):
         if st != 0:
             raise SemMoEError(name, st, self.lib.semmoe_last_hip_error())

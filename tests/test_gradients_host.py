@@ -4,6 +4,7 @@ import gc
 import os
 import re
 import subprocess
+import sys
 import threading
 import weakref
 
@@ -280,3 +281,29 @@ def test_workspaces_of_threads_are_apart(monkeypatch):
     assert len({mine.data_ptr(), *theirs}) == 3 and m._workspace("adapters", 1000)[2] is mine
     gc.collect()
     assert [r() for r in gone] == [None, None]  # a thread's workspaces go with it
+
+
+HOST_ONLY = """
+import sys
+%s
+import numpy as np
+import paper_2503_04398_amd as S
+m = S.SemMoE(S.Config(T=8, d=8, E=4, k=2, F=8, D=2, cap=4), allocate_workspace=False)
+assert m.workspace_bytes() > 0
+e2r, phys, inv = m.place(np.array([4, 1, 1, 4]), np.zeros((4, 4)))
+assert sorted(phys.tolist()) == [0, 1, 2, 3]
+try:
+    m._no_such_name
+except AttributeError:
+    print("done")
+"""
+
+
+@pytest.mark.parametrize("torch_is", [
+    "sys.modules['torch'] = None  # not there",
+    "import torch; del torch._C._cuda_getDevice, torch._C._cuda_isCurrentStreamCapturing  # built without a GPU's support"])
+def test_host_calls_need_no_torch_that_knows_a_gpu(torch_is):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    p = subprocess.run([sys.executable, "-c", HOST_ONLY % torch_is], cwd=root, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True,
+                       timeout=120)
+    assert p.returncode == 0 and p.stdout.strip().endswith("done"), p.stdout
