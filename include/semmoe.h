@@ -538,6 +538,9 @@ int32_t semmoe_adapter_index(const semmoe_config* cfg, void* stream, const int32
 /* Workspace of semmoe_adapters and semmoe_adapters_grad for this config and shape (its ld* do not matter). */
 int32_t semmoe_adapter_workspace_bytes(const semmoe_config* cfg, const semmoe_adapter_shape* shape,
                                        size_t* bytes_out /*host*/);
+/* The part of it that semmoe_adapters uses: u, where the gradient holds v and sums over tokens, too. */
+int32_t semmoe_adapter_forward_workspace_bytes(const semmoe_config* cfg, const semmoe_adapter_shape* shape,
+                                               size_t* bytes_out /*host*/);
 
 /*
  * adapters - Y[i] = Y_base[i] + s_a B_a (A_a X[i]) for the tokens with an adapter, Y[i] = Y_base[i] for those without.

@@ -134,6 +134,7 @@ _SIGS = {
     "semmoe_shared_ffn_grad": ([_P] * 4 + [C.c_int32] + [_P] * 4 + [C.c_size_t], C.c_int32),
     "semmoe_adapter_index": ([_P, _P, _P, C.c_int32, _P, C.c_int32, _P, _P], C.c_int32),
     "semmoe_adapter_workspace_bytes": ([_P, _P, C.POINTER(C.c_size_t)], C.c_int32),
+    "semmoe_adapter_forward_workspace_bytes": ([_P, _P, C.POINTER(C.c_size_t)], C.c_int32),
     "semmoe_adapters": ([_P] * 12 + [C.c_size_t], C.c_int32),
     "semmoe_adapters_grad": ([_P] * 15 + [C.c_size_t], C.c_int32),
     "semmoe_probe_copy": ([_P, _P, _P, C.c_size_t], C.c_int32),
@@ -624,8 +625,8 @@ class SemMoE:
                 if t.shape[0] != X.shape[0]:
                     raise SemMoEError("%s: all row tensors have X's rows" % call, -2)
         n = C.c_size_t(0)
-        self._check("semmoe_adapter_workspace_bytes",
-                    self.lib.semmoe_adapter_workspace_bytes(C.byref(c), C.byref(s), C.byref(n)))
+        size = "semmoe_adapter_forward_workspace_bytes" if dY is None else "semmoe_adapter_workspace_bytes"
+        self._check(size, getattr(self.lib, size)(C.byref(c), C.byref(s), C.byref(n)))
         if len(self._adapter_calls) >= 256:
             self._adapter_calls.clear()
         self._adapter_calls[key] = made = (c, s, int(n.value))

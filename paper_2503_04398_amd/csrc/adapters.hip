@@ -469,6 +469,9 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
 // ---- outer: dF_a = sum over a's tokens of U[position][j] R[token][c] ---------------------------------------------------
 // SWAP = false: dF_a [rank][C] (c along a row).  SWAP = true: dF_a [C][rank].  An adapter's tokens are cut into segments;
 // one with several of them leaves fp32 sums, which `outer_join` adds in the order of the segments.
+// A segment that begins at position p has the place 2 (p / seg), or 2 (p / seg) + 1 if it isn't its adapter's first.  Adapters of
+// several segments are longer than one, so of all positions with the same p / seg at most one begins such an adapter and at
+// most one goes on with one: no place is taken twice, and there are two for every `seg` tokens, however many adapters there are.
 //
 // Both operands run along the tokens, so a slice of 64 rows x 256 bytes and the numbers of its tokens go to LDS and are read
 // across; the next slice's rows are on their way meanwhile.  Every row is read once, the numbers once for each 256 bytes of it.
@@ -480,10 +483,11 @@ struct OuterArgs {
   const void* R;
   size_t ldr;
   int C, seg;      // columns; tokens of a segment
-  int max_items;   // items that `partial` holds
-  float* partial;  // [max_items][rank * C]
+  float* partial;  // [partial_places][rank * C]
   void* dF;        // act [n_adapters][rank * C]
 };
+
+__device__ __forceinline__ int partial_place(int lo, int i, int seg) { return (lo / seg + i) * 2 + (i > 0); }  // i-th segment
 
 constexpr int kOuterTok = 64;
 template <bool F32>
@@ -606,7 +610,7 @@ __device__ __forceinline__ void outer_body(const OuterArgs& a, int block, unsign
       const size_t at = SWAP ? size_t(c) * r + jj : size_t(jj) * a.C + c;
       const f32x4_t v = acc[ct][j];
       if (it.count > 1) {
-        if (item < a.max_items) *reinterpret_cast<f32x4_t*>(a.partial + size_t(item) * r * a.C + at) = v;
+        *reinterpret_cast<f32x4_t*>(a.partial + size_t(partial_place(it.lo, item - it.first, a.seg)) * r * a.C + at) = v;
         continue;
       }
       elem* o = static_cast<elem*>(a.dF) + size_t(it.g) * r * a.C + at;
@@ -629,24 +633,13 @@ __global__ __launch_bounds__(256) void outer_join_kernel(const OuterArgs da, int
   const bool first = int(blockIdx.x) < da_blocks;
   const OuterArgs& a = first ? da : db;
   const int own = blockIdx.y;
-  auto segments = [&](int g) {
-    const int lo = min(max(a.ad.offsets[g], 0), a.ad.T), hi = min(max(a.ad.offsets[g + 1], lo), a.ad.T);
-    return max(1, (hi - lo + a.seg - 1) / a.seg);
-  };
-  const int n_seg = segments(own);
-  if (n_seg <= 1) return;
-  // its first segment's place: those of the adapters before it
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int g = lane; g < own; g += 64) before += segments(g);
-#pragma unroll
-  for (int off = 32; off; off >>= 1) before += __shfl_xor(before, off);
-  const int n = min(n_seg, a.max_items - before);
+  const int lo = min(max(a.ad.offsets[own], 0), a.ad.T), hi = min(max(a.ad.offsets[own + 1], lo), a.ad.T);
+  const int n = (hi - lo + a.seg - 1) / a.seg;
   const size_t size = size_t(a.ad.rank) * a.C;
   const size_t i = (size_t(first ? blockIdx.x : blockIdx.x - da_blocks) * 256 + threadIdx.x) * 4;
-  if (i >= size || n <= 0) return;
-  f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.partial + before * size + i);
-  for (int q = 1; q < n; ++q) v += *reinterpret_cast<const f32x4_t*>(a.partial + (before + q) * size + i);
+  if (n <= 1 || i >= size) return;
+  f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.partial + partial_place(lo, 0, a.seg) * size + i);
+  for (int q = 1; q < n; ++q) v += *reinterpret_cast<const f32x4_t*>(a.partial + partial_place(lo, q, a.seg) * size + i);
   elem* o = static_cast<elem*>(a.dF) + own * size + i;
   if constexpr (F32) *reinterpret_cast<f32x4_t*>(o) = v;
   else *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
@@ -788,11 +781,11 @@ static AdapterPlan plan_of(const semmoe_config* cfg, const semmoe_adapter_shape*
 static size_t u_floats(const semmoe_config* cfg, const semmoe_adapter_shape* s, int parts) {
   return size_t(parts) * cfg->T * s->rank;
 }
-static size_t partial_items(const semmoe_config* cfg, const semmoe_adapter_shape* s, const AdapterPlan& p) {
-  return size_t(cfg->T) / p.seg + s->n_adapters;
+static size_t partial_places(const semmoe_config* cfg, const AdapterPlan& p) {
+  return cfg->T > p.seg ? size_t(cdiv(cfg->T, p.seg)) * 2 : 0;  // else no adapter has a second segment
 }
 static size_t partial_floats(const semmoe_config* cfg, const semmoe_adapter_shape* s, const AdapterPlan& p, int width) {
-  return cfg->T > p.seg ? partial_items(cfg, s, p) * s->rank * width : 0;  // else no adapter has a second segment
+  return partial_places(cfg, p) * s->rank * width;
 }
 
 static int32_t check_shape(const semmoe_config* cfg, const semmoe_adapter_shape* s) {
@@ -905,7 +898,7 @@ static int32_t launch_expand(const ExpandArgs& a, int tt, hipStream_t s) {
 template <bool F32>
 static int32_t launch_outer(const OuterArgs& da, const OuterArgs& db, hipStream_t s) {
   constexpr int NC = kOuterCols<F32>;
-  const long long items = da.max_items, ab = da.dF ? items * cdiv(da.C, NC) : 0, bb = db.dF ? items * cdiv(db.C, NC) : 0;
+  const long long items = (long long)da.ad.T / da.seg + da.ad.n_adapters, ab = da.dF ? items * cdiv(da.C, NC) : 0, bb = db.dF ? items * cdiv(db.C, NC) : 0;
   if (ab + bb >= kMostGroups) return SEMMOE_EUNSUPPORTED;
   const int32_t st = with_rank_tiles(da.ad.rank, [&](auto rt) -> int32_t {
     constexpr int RT = decltype(rt)::value;
@@ -940,9 +933,8 @@ static int32_t run_adapters_grad(const semmoe_config* cfg, const semmoe_adapter_
   int32_t st = launch_shrink_both<F32>(va, ua, dX || dA, dB, p.shrink_tt, s);
   if (st != SEMMOE_OK) return st;
   if (dA || dB) {
-    const int items = int(partial_items(cfg, sh, p));
-    const OuterArgs oa{ad, V, p.parts_out, X, ldx, sh->d_in, p.seg, items, partial_a, dA};
-    const OuterArgs ob{ad, U, p.parts_in, dY, ldy, sh->d_out, p.seg, items, partial_b, dB};
+    const OuterArgs oa{ad, V, p.parts_out, X, ldx, sh->d_in, p.seg, partial_a, dA};
+    const OuterArgs ob{ad, U, p.parts_in, dY, ldy, sh->d_out, p.seg, partial_b, dB};
     st = launch_outer<F32>(oa, ob, s);
     if (st != SEMMOE_OK) return st;
   }
@@ -982,6 +974,15 @@ extern "C" int32_t semmoe_adapter_workspace_bytes(const semmoe_config* cfg, cons
   const AdapterPlan p = plan_of(cfg, shape);
   *bytes_out = align_up(u_floats(cfg, shape, p.parts_in) * 4, 256) + align_up(u_floats(cfg, shape, p.parts_out) * 4, 256) +
                align_up(partial_floats(cfg, shape, p, shape->d_in) * 4, 256) + partial_floats(cfg, shape, p, shape->d_out) * 4 + 256;
+  return SEMMOE_OK;
+}
+
+extern "C" int32_t semmoe_adapter_forward_workspace_bytes(const semmoe_config* cfg, const semmoe_adapter_shape* shape,
+                                                          size_t* bytes_out) {
+  if (!bytes_out) return SEMMOE_EINVAL;
+  const int32_t st = check_shape(cfg, shape);
+  if (st != SEMMOE_OK) return st;
+  *bytes_out = u_floats(cfg, shape, plan_of(cfg, shape).parts_in) * 4 + 256;
   return SEMMOE_OK;
 }
 

@@ -519,3 +519,38 @@ def test_calls_of_two_threads_on_one_stream():
     for out, w in zip(outs, want):
         for got, x in zip(out, w):
             assert torch.equal(got, x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,n", [
+    ([129, 257, 1, 300, 128, 2, 385], 7),   # adapters of one and of several segments of 128 tokens side by side
+    ([130] * 20, 20),                       # each just longer than a segment
+    ([1300, 1, 1100, 5, 2500, 1025, 7], 300)])
+def test_adapters_of_several_segments_side_by_side(lens, n, dtype):
+    _both(Batch(lens, list(range(len(lens))), n, 16, 72, 136, dtype, pad=3, seed=n))
+
+
+def test_the_sums_of_segments_stay_in_their_places():
+    """what lies behind the workspace that the library asks for is not written, whatever the lengths"""
+    import ctypes as C
+    from paper_2503_04398_amd import binding as Bn
+    for lens, n in (([129, 257, 1, 300, 128, 2, 385], 7), ([2600], 1), ([1000, 1040], 2), ([1] * 40 + [1500], 41)):
+        b = Batch(lens, list(range(n)), n, 16, 72, 136, "bf16", seed=n)
+        want, want_Y = _gradient(b), _forward(b)
+        X, dY, order, starts, A, B, scale, Yb, dXb = b.dev("X", "dY", "order", "starts", "A", "B", "scale", "Yb", "dXb")
+        c, s, size = b.m._cfg(T=b.T), Bn._CAdapterShape(n, 16, 72, 136, 0, 0, 0, 0), C.c_size_t(0)
+        dX, dA, dB, Y = torch.empty_like(X), torch.empty_like(A), torch.empty_like(B), torch.empty_like(Yb)
+        p = lambda *ts: [t.data_ptr() for t in ts]  # noqa: E731
+        assert b.m.lib.semmoe_adapter_workspace_bytes(C.byref(c), C.byref(s), C.byref(size)) == 0
+        ws = torch.full((size.value + 4096,), 0xa5, dtype=torch.uint8, device=DEV)
+        assert b.m.lib.semmoe_adapters_grad(C.byref(c), None, C.byref(s), *p(X, dY, order, starts, A, B, scale, dXb, dX, dA, dB, ws),
+                                            size.value) == 0
+        torch.cuda.synchronize()
+        assert (ws[size.value:] == 0xa5).all()
+        for got, w in zip((dX, dA, dB), want):
+            assert torch.equal(got, w)
+        assert b.m.lib.semmoe_adapter_forward_workspace_bytes(C.byref(c), C.byref(s), C.byref(size)) == 0
+        ws.fill_(0xa5)
+        assert b.m.lib.semmoe_adapters(C.byref(c), None, C.byref(s), *p(X, order, starts, A, B, scale, Yb, Y, ws), size.value) == 0
+        torch.cuda.synchronize()
+        assert (ws[size.value:] == 0xa5).all() and torch.equal(Y, want_Y)

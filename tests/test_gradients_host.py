@@ -307,3 +307,33 @@ def test_host_calls_need_no_torch_that_knows_a_gpu(torch_is):
     p = subprocess.run([sys.executable, "-c", HOST_ONLY % torch_is], cwd=root, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True,
                        timeout=120)
     assert p.returncode == 0 and p.stdout.strip().endswith("done"), p.stdout
+
+
+def _sizes(T, dtype="bf16", **kw):
+    lib = S.load_library()
+    c, s, n, f = S.Config(T=T, d=8, E=1, k=1, F=8, D=1, cap=max(T, 1), dtype=dtype).c(), _shape(**kw), C.c_size_t(0), C.c_size_t(0)
+    assert lib.semmoe_adapter_workspace_bytes(C.byref(c), C.byref(s), C.byref(n)) == 0
+    assert lib.semmoe_adapter_forward_workspace_bytes(C.byref(c), C.byref(s), C.byref(f)) == 0
+    return n.value, f.value
+
+
+@pytest.mark.parametrize("n_adapters", [1, 4, 64, 1024])
+def test_adapter_workspaces_follow_the_tokens_and_not_the_adapters(n_adapters):
+    """u and v: at most four planes of T x rank each; the sums over tokens: two places of rank x width for every segment (of no fewer than
+    `seg` tokens for these widths), however many adapters there are"""
+    for T, rank, d_in, d_out, seg in ((32768, 128, 4096, 4096, 4096), (9000, 64, 8192, 256, 1024), (500, 16, 64, 64, 128), (0, 8, 64, 64, 1)):
+        both, forward = _sizes(T, n_adapters=n_adapters, rank=rank, d_in=d_in, d_out=d_out)
+        planes, places = 4 * T * rank * 4, 2 * -(-T // seg)
+        assert forward <= planes + 256
+        assert both <= 2 * planes + places * rank * (d_in + d_out) * 4 + 1024
+        assert forward <= both
+
+
+def test_the_forward_call_asks_for_its_own_part():
+    m = S.SemMoE(S.Config(T=3000, d=16, E=1, k=1, F=8, D=1, cap=3000, dtype="fp32"), allocate_workspace=False)
+    X, Y, A, Bm = torch.zeros(3000, 16), torch.zeros(3000, 24), torch.zeros(2, 8, 16), torch.zeros(2, 24, 8)
+    order, off = torch.zeros(3000, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    both, forward = _sizes(3000, "fp32", n_adapters=2, rank=8, d_in=16, d_out=24)
+    assert m._adapter_call("adapters", X, order, off, A, Bm, None, None, None, Y)[2] == forward < both
+    assert m._adapter_call("adapters_grad", X, order, off, A, Bm, None, Y, None, X)[2] == both
+    assert m.lib.semmoe_adapter_forward_workspace_bytes(None, None, None) == EINVAL
