@@ -42,11 +42,6 @@ struct Elem<false> {
   static constexpr int kSize = 2, kPer16 = 8, kStep = 32;
 };
 
-template <bool F32>
-__device__ __forceinline__ typename Elem<F32>::type to_act(float f) {
-  if constexpr (F32) return f; else return f32_to_bf16(f);
-}
-
 __device__ __forceinline__ u32x4_t load_piece(const void* p) { return *reinterpret_cast<const u32x4_t*>(p); }
 
 // the compiler keeps LDS accesses on both sides in place; a wave's own LDS operations complete in order
@@ -377,7 +372,7 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
         for (int x = 0; x < 4; ++x) {
           if constexpr (F32) u[ks][t][x] = __float_as_uint(f[ks * TT + t][x]);
           else  // the operand's rounding
-            u[ks][t][x] = pack_bf16x2(f[(ks * TT + t) * 2 + (x >> 1)][(x & 1) * 2], f[(ks * TT + t) * 2 + (x >> 1)][(x & 1) * 2 + 1]);
+            u[ks][t][x] = cvt_pk_bf16(f[(ks * TT + t) * 2 + (x >> 1)][(x & 1) * 2], f[(ks * TT + t) * 2 + (x >> 1)][(x & 1) * 2 + 1]);
         }
   }
   const int l_col = (lane % LPR) * E::kPer16;  // this lane's piece of a row's 32 columns
@@ -457,7 +452,7 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const f32x4_t& two = e < 2 ? lo : hi;
-            v[e] = pack_bf16x2(__uint_as_float(v[e] << 16) + two[(e & 1) * 2], __uint_as_float(v[e] & 0xffff0000u) + two[(e & 1) * 2 + 1]);
+            v[e] = cvt_pk_bf16(__uint_as_float(v[e] << 16) + two[(e & 1) * 2], __uint_as_float(v[e] & 0xffff0000u) + two[(e & 1) * 2 + 1]);
           }
         }
         if (there[t][q] && c0 + l_col < c_hi) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(out_row[t][q] + c0));
@@ -577,7 +572,7 @@ __device__ __forceinline__ void outer_body(const OuterArgs& a, int block, unsign
       const f32x4_t v = ub[i][0];
       unsigned char* const o = Us + t * RBU + j * E::kSize;
       if constexpr (F32) *reinterpret_cast<f32x4_t*>(o) = v;
-      else *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      else *reinterpret_cast<uint2*>(o) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
     }
     __syncthreads();
     if (p + KT < p1) {
@@ -615,7 +610,7 @@ __device__ __forceinline__ void outer_body(const OuterArgs& a, int block, unsign
       }
       elem* o = static_cast<elem*>(a.dF) + size_t(it.g) * r * a.C + at;
       if constexpr (F32) *reinterpret_cast<f32x4_t*>(o) = v;
-      else *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      else *reinterpret_cast<uint2*>(o) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
     }
 }
 
@@ -642,7 +637,7 @@ __global__ __launch_bounds__(256) void outer_join_kernel(const OuterArgs da, int
   for (int q = 1; q < n; ++q) v += *reinterpret_cast<const f32x4_t*>(a.partial + partial_place(lo, q, a.seg) * size + i);
   elem* o = static_cast<elem*>(a.dF) + own * size + i;
   if constexpr (F32) *reinterpret_cast<f32x4_t*>(o) = v;
-  else *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  else *reinterpret_cast<uint2*>(o) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
 }
 
 // ---- index ---------------------------------------------------------------------------------------------------------------

@@ -110,6 +110,17 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return static_cast<uint32_t>(f32_to_bf16(lo)) | (static_cast<uint32_t>(f32_to_bf16(hi)) << 16);
 }
 
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+
+// hardware conversion (v_cvt_pk_bf16_f32, round to nearest even), of any number: NaN stays NaN whatever its bits, where the carry of
+// f32_to_bf16 makes 0 of 0xffffffff
+__device__ __forceinline__ uint32_t cvt_pk_bf16(float lo, float hi) {
+  f32x2_t v = {lo, hi};
+  bf16x2_t b = __builtin_convertvector(v, bf16x2_t);
+  return *reinterpret_cast<uint32_t*>(&b);
+}
+
 // The k expert ids of a token: KU >= k registers, positions from k on repeat earlier ids (map_ids masks them).  No load sits
 // behind a branch, so they all go out together.  quads (k a multiple of four, rows 16-byte aligned): a quarter of the
 // instructions; a wave's 64 rows lie anywhere, and each 4-byte instruction costs the address unit as much as a 16-byte one.

@@ -26,16 +26,6 @@
 
 namespace semmoe {
 
-typedef __attribute__((ext_vector_type(2))) float f32x2_t;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
-
-// hardware conversion (v_cvt_pk_bf16_f32, round to nearest even)
-__device__ __forceinline__ uint32_t cvt_pk_bf16(float lo, float hi) {
-  f32x2_t v = {lo, hi};
-  bf16x2_t b = __builtin_convertvector(v, bf16x2_t);
-  return *reinterpret_cast<uint32_t*>(&b);
-}
-
 // A pointer the program knows to be uniform, moved to scalar registers even where the compiler parked it in
 // vector registers.
 template <typename T>

@@ -31,7 +31,7 @@ struct Piece {  // 16 bytes as floats
   __device__ __forceinline__ u32x4_t times(float w) const {
     u32x4_t v;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) v[x] = BF16 ? pack_bf16x2(w * f[2 * x], w * f[2 * x + 1]) : __float_as_uint(w * f[x]);
+    for (int x = 0; x < 4; ++x) v[x] = BF16 ? cvt_pk_bf16(w * f[2 * x], w * f[2 * x + 1]) : __float_as_uint(w * f[x]);
     return v;
   }
   __device__ __forceinline__ float dot(const Piece& o, float s) const {

@@ -554,3 +554,26 @@ def test_the_sums_of_segments_stay_in_their_places():
         assert b.m.lib.semmoe_adapters(C.byref(c), None, C.byref(s), *p(X, order, starts, A, B, scale, Yb, Y, ws), size.value) == 0
         torch.cuda.synchronize()
         assert (ws[size.value:] == 0xa5).all() and torch.equal(Y, want_Y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bits", [-1, 0x7fffffff, 0x7fc00000, 0x7f800001, -4194304])
+def test_a_scale_that_is_no_number(bits, dtype):
+    """NaN of any bits (0xffffffff is what memory filled with ones holds) reaches all that the adapter adds to, and nothing else"""
+    b = Batch([20, 3, 300], [0, 1, 0], 2, 16, 64, 40, dtype, seed=31)
+    clean, clean_grad = _forward(b), _gradient(b)
+    b.scale[0] = torch.tensor([bits], dtype=torch.int32).view(torch.float32)[0]
+    Y, (dX, dA, dB) = _forward(b), _gradient(b)
+    for got, want in ((Y, clean), (dX, clean_grad[0])):
+        assert torch.isnan(got[:20]).all() and torch.isnan(got[23:]).all() and torch.equal(got[20:23], want[20:23])
+    for got, want in ((dA, clean_grad[1]), (dB, clean_grad[2])):
+        assert torch.isnan(got[0]).all() and torch.equal(got[1], want[1])
+
+
+def test_infinite_products_stay_infinite():
+    """an infinity in a row is one in what its token gets, and no NaN"""
+    b = Batch([20, 3], [0, 1], 2, 16, 64, 40, "bf16", seed=31)
+    b.A[0], b.B[0], b.X[:20] = 1.0, 1.0, 1.0
+    b.X[4, 9] = float("inf")
+    Y = _forward(b)
+    assert (Y[4] == float("inf")).all() and torch.isfinite(Y[:4].float()).all() and torch.isfinite(Y[5:].float()).all()

@@ -142,6 +142,24 @@ def test_a_pair_without_a_row_has_no_gradient_whatever_its_token_holds(bad, dtyp
         assert not torch.isfinite(got[there]).any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bits", [-1, 0x7fffffff, 0x7fc00000, 0x7f800001])
+def test_weights_that_are_no_numbers(bits, dtype):
+    """NaN of any bits in topk_w (0xffffffff is what memory filled with ones holds) is NaN in that pair's row, and in no other"""
+    r = np.random.default_rng(6)
+    T, k, d = 5, 2, 72
+    m = _layer(T, k, d, dtype)
+    dOut, Y = _rand(r, (T, d), dtype).to(DEV), _rand(r, (T * k, d), dtype).to(DEV)
+    w = torch.from_numpy(r.random((T, k), dtype=np.float32))
+    w[3, 1] = torch.tensor([bits], dtype=torch.int32).view(torch.float32)[0]
+    slots = torch.from_numpy(r.permutation(T * k).astype(np.int32))
+    dY, dw = torch.full_like(Y, 7.0), torch.full((T, k), 7.0, device=DEV)
+    m.combine_grad(dOut, Y, slots.to(DEV), w.to(DEV), dY, dw)
+    bad = int(slots[3 * k + 1])
+    assert torch.isnan(dY[bad]).all() and torch.isfinite(dY[[i for i in range(T * k) if i != bad]].float()).all()
+    assert torch.isfinite(dw).all()
+
+
 # ---- the expert FFN
 def _ffn_tolerance(x, dy, w_gu, w_dn, dtype):
     """see above; of rows x, dy of one expert"""
