@@ -544,7 +544,7 @@ int32_t semmoe_adapter_forward_workspace_bytes(const semmoe_config* cfg, const s
 
 /*
  * adapters - Y[i] = Y_base[i] + s_a B_a (A_a X[i]) for the tokens with an adapter, Y[i] = Y_base[i] for those without.
- * Sums in fp32; s_a A_a x is rounded to the act type once (an operand of the second product), Y once.
+ * Sums in fp32, Y rounded once; of s_a A_a x the second product takes 16 bits or more (bf16: two parts).
  * dev in : X[T,d_in]; order, adapter_offsets of semmoe_adapter_index; A, B, scale; Y_base[T,d_out] act or NULL (zero).
  * dev out: Y[T,d_out] act; may be Y_base itself (with the same ld), then rows without an adapter are not touched, or X.
  */
@@ -557,7 +557,7 @@ int32_t semmoe_adapters(const semmoe_config* cfg, void* stream, const semmoe_ada
  * u_i = s_a A_a X[i]:
  *   dX[i] = dX_base[i] + A_a^T v_i (dX_base[i] alone without an adapter);
  *   dA_a = sum over a's tokens of v_i X[i]^T;   dB_a = sum of dY[i] u_i^T  (zero for an adapter without tokens).
- * Sums in fp32 in a fixed order; u and v are rounded to the act type once, the results once.
+ * Sums in fp32 in a fixed order, the results rounded once; of u and v the products take 16 bits or more (bf16: two parts).
  * dev in : X[T,d_in], dY[T,d_out]; order, adapter_offsets; A, B, scale; dX_base[T,d_in] act or NULL (zero).
  * dev out: dX[T,d_in] (may be dX_base, with the same ld, or X or dY itself), dA and dB (as A and B, and not in their place)
  *          act; each may be NULL, not all.

@@ -6,7 +6,9 @@
 //   dA_a = sum over a's tokens of v x^T        dB_a = sum of dY u^T
 // so everything is made of three kernels over the ordered tokens: `shrink` (rows times a factor, down to rank numbers),
 // `expand` (rank numbers times a factor, added to rows) and `outer` (sums over tokens).  u and v are fp32 sums in the
-// workspace; as operands of the matrix instructions of bf16 rows they are rounded to bf16 once, as the rows and factors are.
+// workspace.  As operands of the matrix instructions of bf16 rows they are taken in two parts, the nearest bf16 and what that leaves,
+// 16 bits between them: half a step of the result's type is then the whole error, where one rounding of u would add as much again
+// (8192 tokens x 4096, rank 16, against 64 bits: 1.66e-3, and 2.35e-3 with u and v in bf16).
 //
 // A 16-byte piece of a row is the unit throughout: eight bf16 (v_mfma_f32_16x16x32_bf16) or four fp32 (four times
 // v_mfma_f32_16x16x4_f32, a lane's four numbers in turn: any order of k will do as long as both operands use it).
@@ -41,6 +43,17 @@ struct Elem<false> {
   using type = bf16_t;
   static constexpr int kSize = 2, kPer16 = 8, kStep = 32;
 };
+
+// operands made of fp32 numbers: the numbers themselves, or parts of them
+template <bool F32>
+constexpr int kParts = F32 ? 1 : 2;
+
+// a and b as bf16 in hi, what these leave in lo; beside an infinity or NaN nothing is left
+__device__ __forceinline__ void two_parts(float a, float b, uint32_t* hi, uint32_t* lo) {
+  *hi = cvt_pk_bf16(a, b);
+  const float ra = a - __uint_as_float(*hi << 16), rb = b - __uint_as_float(*hi & 0xffff0000u);
+  *lo = cvt_pk_bf16(fabsf(ra) <= fabsf(a) ? ra : 0.0f, fabsf(rb) <= fabsf(b) ? rb : 0.0f);
+}
 
 __device__ __forceinline__ u32x4_t load_piece(const void* p) { return *reinterpret_cast<const u32x4_t*>(p); }
 
@@ -338,7 +351,7 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
   if constexpr (TR) {  // rows that no load fills
     for (int i = NF * 64 + lane; i < KS * E::kStep * LPR; i += 64) *reinterpret_cast<u32x4_t*>(stg + i * 16) = zero;
   }
-  u32x4_t u[KS][TT];
+  u32x4_t u[kParts<F32>][KS][TT];
   {
     // all numbers of a part, up to 16 loads, on their way together; the parts in order
     constexpr int NV = KS * TT * (E::kPer16 / 4);
@@ -370,9 +383,15 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
       for (int t = 0; t < TT; ++t)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          if constexpr (F32) u[ks][t][x] = __float_as_uint(f[ks * TT + t][x]);
-          else  // the operand's rounding
-            u[ks][t][x] = cvt_pk_bf16(f[(ks * TT + t) * 2 + (x >> 1)][(x & 1) * 2], f[(ks * TT + t) * 2 + (x >> 1)][(x & 1) * 2 + 1]);
+          if constexpr (F32) {
+            u[0][ks][t][x] = __float_as_uint(f[ks * TT + t][x]);
+          } else {
+            const f32x4_t& four = f[(ks * TT + t) * 2 + (x >> 1)];
+            uint32_t hi, lo;
+            two_parts(four[(x & 1) * 2], four[(x & 1) * 2 + 1], &hi, &lo);
+            u[0][ks][t][x] = hi;
+            u[1][ks][t][x] = lo;
+          }
         }
   }
   const int l_col = (lane % LPR) * E::kPer16;  // this lane's piece of a row's 32 columns
@@ -430,7 +449,9 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
             f = k < r ? *reinterpret_cast<const u32x4_t*>(stg + ((i * 16 + l16) * (r + E::kPer16) + k) * E::kSize) : zero;
           }
 #pragma unroll
-          for (int t = 0; t < TT; ++t) acc[i][t] = piece_mfma<F32>(f, u[ks][t], acc[i][t]);
+          for (int h = 0; h < kParts<F32>; ++h)
+#pragma unroll
+            for (int t = 0; t < TT; ++t) acc[i][t] = piece_mfma<F32>(f, u[h][ks][t], acc[i][t]);
         }
     }
 #pragma unroll
@@ -496,7 +517,7 @@ __device__ __forceinline__ void outer_body(const OuterArgs& a, int block, unsign
   constexpr int RBU = 16 * RT * E::kSize + 16;                       // bytes of a token's numbers in LDS
   constexpr int NU = KT * RT * 4 / 256;                              // their loads a thread
   unsigned char* const Rs = lds_raw;               // [KT][256 bytes], 32-byte pairs of pieces swapped about by the row
-  unsigned char* const Us = lds_raw + KT * 256;    // [KT][RBU]
+  unsigned char* const Us = lds_raw + KT * 256;    // [parts][KT][RBU]
   const int r = a.ad.rank;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -572,7 +593,13 @@ __device__ __forceinline__ void outer_body(const OuterArgs& a, int block, unsign
       const f32x4_t v = ub[i][0];
       unsigned char* const o = Us + t * RBU + j * E::kSize;
       if constexpr (F32) *reinterpret_cast<f32x4_t*>(o) = v;
-      else *reinterpret_cast<uint2*>(o) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
+      else {
+        uint2 hi, lo;
+        two_parts(v[0], v[1], &hi.x, &lo.x);
+        two_parts(v[2], v[3], &hi.y, &lo.y);
+        *reinterpret_cast<uint2*>(o) = hi;
+        *reinterpret_cast<uint2*>(o + KT * RBU) = lo;
+      }
     }
     __syncthreads();
     if (p + KT < p1) {
@@ -586,11 +613,13 @@ __device__ __forceinline__ void outer_body(const OuterArgs& a, int block, unsign
       for (int c = 0; c < CT; ++c)
         x[c] = column_piece<F32>(lane, [&](int row, int col) { return r_at(ks * E::kStep + row, ((wave * CT + c) * 16 + col) * E::kSize); });
 #pragma unroll
-      for (int j = 0; j < RT; ++j) {
-        const u32x4_t u = column_piece<F32>(lane, [&](int row, int col) { return Us + (ks * E::kStep + row) * RBU + (j * 16 + col) * E::kSize; });
+      for (int j = 0; j < RT; ++j)
 #pragma unroll
-        for (int c = 0; c < CT; ++c) acc[c][j] = SWAP ? piece_mfma<F32>(u, x[c], acc[c][j]) : piece_mfma<F32>(x[c], u, acc[c][j]);
-      }
+        for (int h = 0; h < kParts<F32>; ++h) {
+          const u32x4_t u = column_piece<F32>(lane, [&](int row, int col) { return Us + (h * KT + ks * E::kStep + row) * RBU + (j * 16 + col) * E::kSize; });
+#pragma unroll
+          for (int c = 0; c < CT; ++c) acc[c][j] = SWAP ? piece_mfma<F32>(u, x[c], acc[c][j]) : piece_mfma<F32>(x[c], u, acc[c][j]);
+        }
     }
   }
 
@@ -899,7 +928,7 @@ static int32_t launch_outer(const OuterArgs& da, const OuterArgs& db, hipStream_
     constexpr int RT = decltype(rt)::value;
     using E = Elem<F32>;
     static std::atomic<uint64_t> allowed{0};
-    return launch_groups(outer_kernel<F32, RT>, &allowed, dim3(unsigned(ab + bb)), kOuterTok * (256 + 16 * RT * E::kSize + 16), s, da, int(ab), db);
+    return launch_groups(outer_kernel<F32, RT>, &allowed, dim3(unsigned(ab + bb)), kOuterTok * (256 + kParts<F32> * (16 * RT * E::kSize + 16)), s, da, int(ab), db);
   });
   if (st != SEMMOE_OK || da.ad.T <= da.seg) return st;  // no adapter has a second segment
   const int ja = da.dF ? int((size_t(da.ad.rank) * da.C + 1023) / 1024) : 0, jb = db.dF ? int((size_t(db.ad.rank) * db.C + 1023) / 1024) : 0;

@@ -577,3 +577,55 @@ def test_infinite_products_stay_infinite():
     b.X[4, 9] = float("inf")
     Y = _forward(b)
     assert (Y[4] == float("inf")).all() and torch.isfinite(Y[:4].float()).all() and torch.isfinite(Y[5:].float()).all()
+
+
+# ---- one rounding: u and v are operands in two parts that hold 16 bits between them, the results are rounded once
+def _once(got, want, parts, dtype, what):
+    """parts: |B| |h| and the like, what a relative error of h is carried over by.  Entries: half a step of the result, 2^-16 of the
+    parts (the second half of h is within 2^-8 of what the first leaves, which is 2^-8 of h) and the sums' fp32.  Whole: the
+    errors of the rounding lie anywhere within half a step, so their mean square is a third of its square; an eighth allowed for."""
+    got, (h, mag, n) = _np(got), parts
+    assert np.isfinite(got).all(), what
+    off, u = np.abs(got - want), R[dtype]
+    bound = u * np.abs(want) + (1.0 + u) * ((2.0 ** -16 if dtype == "bf16" else 0.0) * h + E32 * n * mag)
+    at = (off - bound).argmax()
+    assert (off <= bound).all(), "%s: off by %.3e where %.3e is allowed" % (what, off.flat[at], bound.flat[at])
+    if want.size >= 2048 and dtype == "bf16":
+        e = np.floor(np.log2(np.maximum(np.abs(want), 2.0 ** -100)))
+        allowed = 1.125 * np.sqrt(((u * 2.0 ** e) ** 2 / 3.0).sum()) / np.linalg.norm(want)
+        rel = np.linalg.norm(off) / np.linalg.norm(want)
+        assert rel <= allowed, "%s: |a-b|/|b| = %.3e, %.3e allowed" % (what, rel, allowed)
+
+
+def _both_once(b):
+    X, dY, A, B = _np(b.X), _np(b.dY), _np(b.A), _np(b.B)
+    s = np.ones(b.n) if b.scale is None else _np(b.scale)
+    rank, d_in, d_out = A.shape[1], A.shape[2], B.shape[1]
+    zero = lambda t: np.zeros(t.shape)  # noqa: E731
+    Y, Yh, Ym = (np.zeros((b.T, d_out)) for _ in range(3))
+    (dX, Xh, Xm), (dA, Ah, Am), (dB, Bh, Bm) = ([zero(t) for _ in range(3)] for t in (X, A, B))
+    for a in range(b.n):
+        t = np.flatnonzero(b.of == a)
+        u, v, um, vm = s[a] * X[t] @ A[a].T, s[a] * dY[t] @ B[a], s[a] * np.abs(X[t]) @ np.abs(A[a]).T, s[a] * np.abs(dY[t]) @ np.abs(B[a])
+        for out, h, m_, left, hi, mag in ((Y, Yh, Ym, B[a].T, u, um), (dX, Xh, Xm, A[a], v, vm)):
+            out[t], h[t], m_[t] = hi @ left, np.abs(hi) @ np.abs(left), mag @ np.abs(left)
+        dA[a], Ah[a], Am[a] = v.T @ X[t], np.abs(v).T @ np.abs(X[t]), vm.T @ np.abs(X[t])
+        dB[a], Bh[a], Bm[a] = dY[t].T @ u, np.abs(dY[t]).T @ np.abs(u), np.abs(dY[t]).T @ um
+    longest = max([int((b.of == a).sum()) for a in range(b.n)] + [rank])
+    got = _forward(b, base=False)
+    own = b.of >= 0
+    _once(got[torch.from_numpy(own).to(DEV)], Y[own], (Yh[own], Ym[own], d_in + rank + 4), b.dtype, "Y")
+    g = _gradient(b, base=False)
+    _once(g[0][torch.from_numpy(own).to(DEV)], dX[own], (Xh[own], Xm[own], d_out + rank + 4), b.dtype, "dX")
+    _once(g[1], dA, (Ah, Am, d_out + longest + 4), b.dtype, "dA")
+    _once(g[2], dB, (Bh, Bm, d_in + longest + 4), b.dtype, "dB")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,ads,n,rank,d_in,d_out", [
+    ([1], [0], 1, 8, 64, 40), ([3, 0, 2], [0, 0, 5], 4, 24, 136, 264), ([64, 65, 1, 130], [1, 0, -1, 2], 3, 32, 512, 520),
+    ([700, 30, 800], [0, 2, 0], 3, 16, 264, 72), ([5, 9, 4, 70, 3], [1, 0, 1, 1, 0], 2, 64, 328, 640),
+    ([90, 100], [0, 1], 2, 128, 1032, 392), ([1] * 50, [i % 17 - 1 for i in range(50)], 16, 8, 2048, 136),
+    ([1300, 1200], [0, 1], 2, 72, 136, 72), ([5000, 3300], [0, 1], 2, 64, 72, 40)])
+def test_results_are_rounded_once(lens, ads, n, rank, d_in, d_out, dtype):
+    _both_once(Batch(lens, ads, n, rank, d_in, d_out, dtype, seed=rank + 3))
