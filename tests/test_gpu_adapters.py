@@ -629,3 +629,47 @@ def _both_once(b):
     ([1300, 1200], [0, 1], 2, 72, 136, 72), ([5000, 3300], [0, 1], 2, 64, 72, 40)])
 def test_results_are_rounded_once(lens, ads, n, rank, d_in, d_out, dtype):
     _both_once(Batch(lens, ads, n, rank, d_in, d_out, dtype, seed=rank + 3))
+
+
+# ---- the token tiles of long batches in fp32, and results in the place of X
+@pytest.mark.parametrize("T,n,rank,d_in,d_out", [
+    (2048, 2, 16, 72, 136), (2100, 3, 64, 136, 72), (4200, 2, 128, 136, 264), (8200, 2, 16, 72, 40), (8250, 3, 32, 40, 136),
+    (8192, 2, 64, 264, 72), (8300, 2, 128, 72, 136), (16400, 2, 64, 136, 72), (16500, 1, 40, 40, 72), (16400, 2, 128, 40, 72), (131100, 2, 8, 40, 24)])
+def test_wide_tiles_in_fp32(T, n, rank, d_in, d_out):
+    """32 and 64 tokens in `expand`, 32 and (ranks 33 to 64) 64 in `shrink`, with tiles that end inside a request"""
+    lens = [T // 2 + 11, 3, T - T // 2 - 30]
+    _both(Batch(lens, [(i + 1) % n if n > 1 else 0 for i in range(3)] if n > 2 else [0, n - 1, 0], n, rank, d_in, d_out, "fp32", pad=16, seed=rank + T))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,rank", [(40, 16), (2100, 64), (8300, 128)])
+def test_result_in_the_place_of_x(T, rank, dtype):
+    b = Batch([T // 2, T - T // 2 - 5, 3], [0, 1, -1], 2, rank, 136, 136, dtype, pad=2, seed=T)
+    want, none = _forward(b), _forward(b, base=False)
+    for base, w in ((True, want), (False, none)):
+        X, order, starts, A, B, scale, Yb = b.dev("X", "order", "starts", "A", "B", "scale", "Yb")
+        b.m.adapters(X, order, starts, A, B, X, Y_base=Yb if base else None, scale=scale)
+        assert torch.equal(X[:T - 2], w[:T - 2]) and torch.equal(X[T - 2:], b.X[T - 2:].to(DEV))
+    # X as base, too: Y = X + scale B (A X)
+    X, order, starts, A, B, scale = b.dev("X", "order", "starts", "A", "B", "scale")
+    apart = torch.full_like(X, 7.0)
+    b.m.adapters(X, order, starts, A, B, apart, Y_base=X, scale=scale)
+    b.m.adapters(X, order, starts, A, B, X, Y_base=X, scale=scale)
+    assert torch.equal(X[:T - 2], apart[:T - 2])
+
+
+# ---- the index at the ends of its range
+@pytest.mark.parametrize("n_req,n,longest", [(65536, 1024, 1), (65536, 1, 3), (4097, 1024, 40), (20000, 77, 2)])
+def test_index_of_the_most_requests(n_req, n, longest):
+    r = np.random.default_rng(n)
+    lens = r.integers(0, longest + 1, n_req)
+    ads = r.integers(-1, n + 1, n_req).astype(np.int32)
+    off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    T = int(off[-1]) + 3
+    key = np.repeat(np.where((ads < 0) | (ads >= n), n, ads), lens)
+    want = np.concatenate([np.argsort(key, kind="stable"), np.full(3, -1)]).astype(np.int32)
+    m = S.SemMoE(S.Config(T=T, d=8, E=1, k=1, F=8, D=1, cap=T), device=DEV)
+    order, starts = torch.empty(T, dtype=torch.int32, device=DEV), torch.empty(n + 1, dtype=torch.int32, device=DEV)
+    m.adapter_index(torch.from_numpy(off).to(DEV), torch.from_numpy(ads).to(DEV), n, order, starts)
+    assert (order.cpu().numpy() == want).all()
+    assert (starts.cpu().numpy() == np.searchsorted(np.sort(key), np.arange(n + 1))).all()
