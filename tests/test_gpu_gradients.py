@@ -305,6 +305,85 @@ def test_large_gate_values(dtype):
     assert np.allclose(got[:, 1], [F * x0[0], 0, F * x0[2], 0], rtol=2.0 ** -7, atol=1e-30)  # sum over F of du
 
 
+# ---- the expert FFN, held to the roundings that the kernels make
+def _rounding_var(x, dtype):
+    """mean square of the error of rounding x to the act type: x lies in [2^e, 2^(e+1)), its error anywhere within half a step"""
+    half = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}[dtype]
+    e = np.floor(np.log2(np.maximum(np.abs(x), 2.0 ** -100)))
+    return (half * 2.0 ** e) ** 2 / 3.0
+
+
+def _ffn_check(got, x, dy, w_gu, w_dn, dtype):
+    """Two roundings to the act type: [dg | du], an operand of the last product, and dX.  g, u and dh are fp32 sums.
+    Whole: these roundings are independent, so the square of the error's norm is the sum of their mean squares, those of [dg | du]
+        carried over by the squares of the weights, an eighth allowed for (each sum has thousands of terms).  fp32: its roundings are
+        those of the sums too, sqrt(n) e for each of the three products of n terms.
+    Entries: half a step of each, all pointing the same way, and e (n + 4) of what a sum of n terms adds up, through the
+        derivatives of silu; the hardware's exp2 and reciprocal are within 4 e."""
+    F, r = w_dn.shape[1], R[dtype]
+    d = x.shape[1]
+    g, u, dh = x @ w_gu[:F].T, x @ w_gu[F:].T, dy @ w_dn
+    sig = 1.0 / (1.0 + np.exp(-g))
+    d1 = sig + g * sig * (1.0 - sig)
+    d2 = sig * (1.0 - sig) * (2.0 + g * (1.0 - 2.0 * sig))
+    dgu = np.concatenate([dh * u * d1, dh * g * sig], 1)
+    want = dgu @ w_gu
+    e = E32 * (d + 4)
+    mg, mu, mh = e * np.abs(x) @ np.abs(w_gu[:F]).T, e * np.abs(x) @ np.abs(w_gu[F:]).T, e * np.abs(dy) @ np.abs(w_dn)
+    slack = 12 * E32
+    off_g = mh * np.abs(u * d1) + mu * np.abs(dh * d1) + mg * np.abs(dh * u * d2) + slack * np.abs(dh * u) * sig * (1.0 + np.abs(g))
+    off_u = mh * np.abs(g * sig) + mg * np.abs(dh * d1) + slack * np.abs(dh * g) * sig * (1.0 + np.abs(g))
+    off = np.concatenate([off_g, off_u], 1)
+    bound = (r * np.abs(dgu) + (1.0 + r) * off) @ np.abs(w_gu) + E32 * (2 * F + 4) * np.abs(dgu) @ np.abs(w_gu)
+    bound = bound + r * (np.abs(want) + bound)
+    err = np.abs(got - want)
+    at = (err - bound).argmax()
+    assert (err <= bound).all(), "an entry is off by %.3e, %.3e allowed" % (err.flat[at], bound.flat[at])
+    if want.size >= 2048:
+        square = (_rounding_var(dgu, dtype) @ (w_gu * w_gu)).sum() + _rounding_var(want, dtype).sum()
+        sums = E32 * np.sqrt(2.0 * d + 2.0 * F) * 2.0
+        rel = np.linalg.norm(err) / np.linalg.norm(want)
+        allowed = 1.125 * np.sqrt(square) / np.linalg.norm(want) + sums
+        assert rel <= allowed, "|a-b|/|b| = %.3e, %.3e allowed" % (rel, allowed)
+
+
+# every family of tiles: streamed rows, 128 x 128, 256 x 128 and pieces, 256 x 256 and pieces, staged ones for widths that are no multiple
+# of 64, short K
+TIGHT = [
+    ((1, 2, 15, 16, 17, 33), 256, 512), ((3,) * 8, 1024, 768), ((40,) * 16, 512, 1024), ((70, 20, 5), 520, 264), ((64, 65, 130), 72, 40),
+    ((90, 130, 100) * 16, 1024, 320), ((250, 200, 300, 190) * 14, 512, 704), ((1100, 1400), 576, 1160), ((700,), 2048, 136)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,d,F", TIGHT)
+def test_ffn_grad_rounds_what_it_says_and_nothing_else(rows, d, F, dtype):
+    r = np.random.default_rng(d + F)
+    E, P = len(rows), int(sum(rows))
+    X, dY = _rand(r, (P, d), dtype), _rand(r, (P, d), dtype)
+    W_gu, W_dn = _rand(r, (E, 2 * F, d), dtype, d ** -0.5), _rand(r, (E, d, F), dtype, F ** -0.5)
+    off = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+    m = _layer(P, 1, d, dtype, E=E, F=F)
+    dX = torch.full((P, d), 512.0, dtype=_act(dtype), device=DEV)
+    m.expert_ffn_grad(-1, X.to(DEV), dY.to(DEV), torch.from_numpy(off).to(DEV), torch.arange(E, dtype=torch.int32, device=DEV),
+                      W_gu.to(DEV), W_dn.to(DEV), dX)
+    got = _np(dX)
+    for q in list(range(E))[:6]:
+        at = slice(off[q], off[q + 1])
+        _ffn_check(got[at], *(_np(t) for t in (X[at], dY[at], W_gu[q], W_dn[q])), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,d,F", [(1, 64, 64), (256, 1032, 384), (777, 192, 640)])
+def test_shared_ffn_grad_rounds_what_it_says_and_nothing_else(n, d, F, dtype):
+    r = np.random.default_rng(n + d)
+    m = _layer(n, 1, d, dtype, F=F)
+    X, dY = _rand(r, (n, d), dtype), _rand(r, (n, d), dtype)
+    W_gu, W_dn = _rand(r, (2 * F, d), dtype, d ** -0.5), _rand(r, (d, F), dtype, F ** -0.5)
+    dX = torch.full((n, d), 512.0, dtype=_act(dtype), device=DEV)
+    m.shared_ffn_grad(X.to(DEV), dY.to(DEV), n, W_gu.to(DEV), W_dn.to(DEV), dX)
+    _ffn_check(_np(dX), *(_np(t) for t in (X, dY, W_gu, W_dn)), dtype)
+
+
 # ---- a layer with adapters, forward and back
 @pytest.mark.parametrize("dtype,score", [("fp32", "softmax"), ("bf16", "sigmoid")])
 def test_layer_with_adapters_forward_and_back(dtype, score):
