@@ -658,6 +658,12 @@ class SemMoE:
         c, s, need = self._adapter_call("adapters_grad", X, order, adapter_offsets, A, B, scale, dY, dX_base, dX)
         if (dA is not None and dA.shape != A.shape) or (dB is not None and dB.shape != B.shape):
             raise SemMoEError("adapters_grad: dA and dB have the shapes of A and B", -2)
+        taken = [A.data_ptr(), B.data_ptr()]  # dX is made from A after dA has been written
+        for t in (dA, dB):
+            if t is not None:
+                if t.data_ptr() in taken:
+                    raise SemMoEError("adapters_grad: dA and dB may not lie in the place of A, B or one another", -1)
+                taken.append(t.data_ptr())
         self._fit("adapters_grad", ((X, None, 0), (dY, None, 0), (order, torch.int32, 0),
                   (adapter_offsets, torch.int32, 1), (A, None, 0), (B, None, 0),
                   (scale, torch.float32, 0), (dX_base, None, 0), (dX, None, 0), (dA, None, 0),

@@ -337,3 +337,17 @@ def test_the_forward_call_asks_for_its_own_part():
     assert m._adapter_call("adapters", X, order, off, A, Bm, None, None, None, Y)[2] == forward < both
     assert m._adapter_call("adapters_grad", X, order, off, A, Bm, None, Y, None, X)[2] == both
     assert m.lib.semmoe_adapter_forward_workspace_bytes(None, None, None) == EINVAL
+
+
+def test_gradients_in_the_place_of_the_factors_are_refused():
+    """dX reads the factors after dA and dB have been written"""
+    m = S.SemMoE(S.Config(T=8, d=16, E=1, k=1, F=8, D=1, cap=8, dtype="fp32"), allocate_workspace=False)
+    X, dY = torch.zeros(8, 16), torch.zeros(8, 16)
+    A, Bm = torch.zeros(2, 8, 16), torch.zeros(2, 16, 8)
+    order, off = torch.zeros(8, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    same = torch.zeros(2, 8, 16)
+    for kw in (dict(dA=A), dict(dB=Bm), dict(dA=A, dB=Bm, dX=X), dict(dA=Bm.view(2, 8, 16)), dict(dA=same, dB=same.view(2, 16, 8))):
+        with pytest.raises(S.SemMoEError, match="place"):
+            m.adapters_grad(X, dY, order, off, A, Bm, **kw)
+    with pytest.raises(S.SemMoEError, match="device"):  # apart: the next thing that is wrong with them
+        m.adapters_grad(X, dY, order, off, A, Bm, dA=A.clone(), dB=Bm.clone())
