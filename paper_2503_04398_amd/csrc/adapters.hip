@@ -773,18 +773,28 @@ static int cut_columns(int N, int tt, long long tiles) {
   return cdiv(steps, int(cuts));
 }
 
-// Tokens of a tile.  A tile reads the whole of its adapter's factor, so many tokens want large tiles; few want many tiles: 16 / 32 / 64
-// tokens in both kernels, us: 1000 tokens of 8 adapters, 4096 x 4096, rank 64: 23 / 29 / 43; 16384 tokens of 4, 7168 x 7168, rank 16: 204 /
-// 191 / 179, with 32 in shrink and 64 in expand 177; 4096 of 64 adapters, 2880 x 2880, rank 128: 61 / 52 / 62.
+// Tokens of a tile.  A tile reads the whole of its adapter's factor, so many tokens want large tiles; few want many tiles.  us of the
+// forward (gradient) with the tokens in shrink / expand, bf16, 4096 x 4096 and 4 adapters where nothing else is said:
+//   * shrink 32: ranks up to 32 from 4000 tokens on (rank 16, 3000 tokens 16/32 20.7, 32/32 20.6; 4000 27.1, 24.6; 7168 x 7168: 36.4, 34.4
+//     and 55.1, 46.7), up to 64 from 5000 (rank 64, 4000 39.0 (84.6), 42.8 (90.4); 6000 56.9 (109), 51.7 (104)), wider ones from T *
+//     rank = 2^19 (rank 128, 3390 tokens, 688 x 800: 28.3 (60.0), 33.6 (68.2); 6000 82.4 (199), 77.7 (186))
+//   * shrink 64: ranks 33 to 64 from T * rank = 14000 * 64 (rank 64, 12000 tokens 32/64 91.3 (174), 64/64 95.4 (187); 16000 110 (219),
+//     106 (203); 16 adapters 118 (264), 114 (239))
+//   * expand 32 from 2048 tokens on (rank 16, 2000 15.6, 17.4, 3000 20.2, 20.7; rank 64, 2000 24.0, 25.8, 3000 30.3, 28.0)
+//   * expand 64 from 8192 tokens on (rank 16, 6000 32/32 39.9, 32/64 38.6, 12000 85.6, 73.1; rank 64, 8000 51.6, 59.2, 16 adapters 72.1, 74.1,
+//     12000 102, 91.3), not for bf16 ranks past 64, whose u in two parts takes the registers (rank 128, 16000 tokens 32/32 151
+//     (383), 32/64 187 (417), 16384 the same 226 (475) with both; rank 96, 15654 tokens of 24, 624 x 576: 31 (100), 60 (125))
 static bool shrink_has_64(int rank) { return rank > 32 && rank <= 64; }  // the ranks where 64-token tiles of shrink pay
+static constexpr bool expand_has_64(bool f32, int rank) { return f32 || rank <= 64; }
 
 static AdapterPlan plan_of(const semmoe_config* cfg, const semmoe_adapter_shape* s) {
   AdapterPlan p;
   const int T = cfg->T, es = int(act_bytes(cfg));
   const int mean = T / s->n_adapters, most = mean <= 24 ? 1 : (mean <= 48 ? 2 : 4);
   const long long work = (long long)T * s->rank;
-  const int shrink_tt = work >= 16384 * 64 && shrink_has_64(s->rank) ? 4 : (work >= 8192 * 64 || T >= 8192 ? 2 : 1);
-  const int expand_tt = T >= 8192 ? 4 : (T >= 2048 ? 2 : 1);
+  const bool shrink_32 = s->rank <= 32 ? T >= 4000 : (s->rank <= 64 ? T >= 5000 : work >= 1 << 19);
+  const int shrink_tt = work >= 14000 * 64 && shrink_has_64(s->rank) ? 4 : (shrink_32 ? 2 : 1);
+  const int expand_tt = T >= 8192 && expand_has_64(es == 4, s->rank) ? 4 : (T >= 2048 ? 2 : 1);
   p.shrink_tt = shrink_tt < most ? shrink_tt : most;
   p.expand_tt = expand_tt < most ? expand_tt : most;
   const long long tiles = p.tiles(p.shrink_tt, T, s->n_adapters), e_tiles = p.tiles(p.expand_tt, T, s->n_adapters + 1);
@@ -839,12 +849,6 @@ static int32_t with_rank_tiles(int rank, F f) {
   if (rt <= 4) return f(std::integral_constant<int, 4>{});
   static_assert(SEMMOE_MAX_RANK == 128, "the widths here");
   return f(std::integral_constant<int, 8>{});
-}
-template <typename F>
-static int32_t with_token_tiles(int tt, F f) {
-  if (tt <= 1) return f(std::integral_constant<int, 1>{});
-  if (tt <= 2) return f(std::integral_constant<int, 2>{});
-  return f(std::integral_constant<int, 4>{});
 }
 
 // One launch of 256 threads a workgroup.  `allowed`: the kernel's own flag word (allow_max_dynamic_lds).
@@ -902,20 +906,28 @@ static int32_t launch_shrink_both(const ShrinkArgs& v, const ShrinkArgs& u, bool
   });
 }
 
+template <bool F32, typename F>
+static int32_t with_expand_tiles(int rank, int tt, F f) {
+  return with_rank_tiles(rank, [&](auto rt) -> int32_t {
+    if (tt <= 1) return f(rt, std::integral_constant<int, 1>{});
+    if constexpr (expand_has_64(F32, 16 * decltype(rt)::value))
+      if (tt >= 4) return f(rt, std::integral_constant<int, 4>{});
+    return f(rt, std::integral_constant<int, 2>{});
+  });
+}
+
 template <bool F32, bool TR>
 static int32_t launch_expand(const ExpandArgs& a, int tt, hipStream_t s) {
-  return with_rank_tiles(a.ad.rank, [&](auto rt) -> int32_t {
-    return with_token_tiles(tt, [&](auto t4) -> int32_t {
-      constexpr int RT = decltype(rt)::value, TT = decltype(t4)::value;
-      const long long groups = AdapterPlan::tiles(TT, a.ad.T, a.ad.n_adapters + 1) * cdiv(a.N, a.chunks * kExpandCols);
-      if (groups <= 0) return SEMMOE_OK;
-      if (groups >= kMostGroups) return SEMMOE_EUNSUPPORTED;
-      using E = Elem<F32>;
-      constexpr size_t rows = (16 * RT + E::kStep - 1) / E::kStep * E::kStep;
-      constexpr size_t factor = TR ? rows * 32 * E::kSize : 32 * (16 * RT + E::kPer16) * E::kSize;
-      static std::atomic<uint64_t> allowed{0};
-      return launch_groups(expand_kernel<F32, RT, TT, TR>, &allowed, dim3(unsigned(groups)), 4 * (16 * 144 + factor), s, a);
-    });
+  return with_expand_tiles<F32>(a.ad.rank, tt, [&](auto rt, auto t4) -> int32_t {
+    constexpr int RT = decltype(rt)::value, TT = decltype(t4)::value;
+    const long long groups = AdapterPlan::tiles(TT, a.ad.T, a.ad.n_adapters + 1) * cdiv(a.N, a.chunks * kExpandCols);
+    if (groups <= 0) return SEMMOE_OK;
+    if (groups >= kMostGroups) return SEMMOE_EUNSUPPORTED;
+    using E = Elem<F32>;
+    constexpr size_t rows = (16 * RT + E::kStep - 1) / E::kStep * E::kStep;
+    constexpr size_t factor = TR ? rows * 32 * E::kSize : 32 * (16 * RT + E::kPer16) * E::kSize;
+    static std::atomic<uint64_t> allowed{0};
+    return launch_groups(expand_kernel<F32, RT, TT, TR>, &allowed, dim3(unsigned(groups)), 4 * (16 * 144 + factor), s, a);
   });
 }
 

@@ -673,3 +673,11 @@ def test_index_of_the_most_requests(n_req, n, longest):
     m.adapter_index(torch.from_numpy(off).to(DEV), torch.from_numpy(ads).to(DEV), n, order, starts)
     assert (order.cpu().numpy() == want).all()
     assert (starts.cpu().numpy() == np.searchsorted(np.sort(key), np.arange(n + 1))).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,rank", [
+    (2047, 16), (2048, 72), (3999, 24), (4000, 32), (4999, 40), (5000, 64), (4095, 128), (4096, 128), (8191, 96), (8192, 104), (13999, 64),
+    (14000, 64), (20000, 48), (18600, 48)])
+def test_both_sides_of_the_lines_of_the_token_tiles(T, rank, dtype):
+    _both(Batch([T // 2 + 5, 9, T - T // 2 - 21], [1, 0, 1], 2, rank, 40, 24, dtype, pad=7, seed=T))
