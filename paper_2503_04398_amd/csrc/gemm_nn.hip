@@ -108,9 +108,11 @@ static int32_t launch_nn_f32(const GemmArgs& a, int max_rows, int est, hipStream
 //     experts of 90, d 4096, F 1536, dh: 263 / 283 / 312; 130 rows 327 / 314 / 341).  128 x 64 tiles are behind these even where they leave
 //     half the chip idle, 64 x 64 ones too: a slice costs a wave much the same (one expert of 64 rows, d 7168, F 2048, dh: 172, 187 as
 //     128 x 64, 170 as 64 x 64, dX 180 / 187 / 178; 8 of 90 rows, dX: 368 / 423; 16 of 48, d 2048, F 768, dX: 71 / 90 / 94)
-//   * 256 x 256 from 192 rows on with five quarters of a round of them (8 experts of 400, d 7168, dx: 655 / 620 / 604; 600 rows of d
-//     2880, 273 tiles: 531 / 511 / 528), or, with groups of 1024 rows and more, three fifths (16 experts of 1300, d 2048, F
-//     768, dh: 437 / 428 / 422); 256 x 128 else
+//   * 256 x 256 from 192 rows on with four fifths of a round of them (tiles a compute unit: 0.42, 8 experts of 300, d 2048, F 768, dX 101 /
+//     97 / 105; 0.46, 8 of 500, d 4096, F 1536, dh 374 / 346 / 372; 0.84, 16 of 300, d 2048, F 768, dX 150 / 154 / 145; 1.0, 8 of 900,
+//     dX 170 / 161 / 153); 256 x 128 else
+// Over 269 calls (8 to 64 experts of 60 to 2000 rows, five pairs of widths, all experts or one rank of eight) these lines are 0.4 % behind
+// the best of the three for dh and 0.7 % for dX; with half a round in the place of four fifths 0.6 and 1.0.
 // Shapes whose K is shorter than a ring, or with more groups than the tables hold, take 128 x 64 tiles with a barrier a slice.
 template <int MODE>
 static int32_t launch_nn_bf16(const GemmArgs& a, int max_rows, int est, hipStream_t s) {
@@ -118,8 +120,9 @@ static int32_t launch_nn_bf16(const GemmArgs& a, int max_rows, int est, hipStrea
   const int32_t st = device_info(&d);
   if (st != SEMMOE_OK) return st;
   const long long cus = d.num_cu;
-  // The mean is that of all experts.  A rank that an affinity placement loads has some twice as many rows: one of 20865 where 8192 are
-  // expected 400 us as 256 x 256 tiles, 415 as 256 x 128.
+  // The mean is that of all experts.  A rank that an affinity placement loads has some twice as many rows, so a rank's mean is taken
+  // twice.  140 calls of one rank of eight: with as many rows as the others it is 0.6 (dh) and 1.0 % (dX) behind the best tiles so, 0.7 and
+  // 1.3 with the mean once; with twice as many 0.5 and 0.5, 1.2 and 1.8 once.
   if (a.offsets && (long long)a.nq * (est + 1) < max_rows) est *= 2;
   // a ragged group's last tile is half full in the mean; times 100
   auto tiles = [&](int bw, int bt) {
@@ -129,7 +132,7 @@ static int32_t launch_nn_bf16(const GemmArgs& a, int max_rows, int est, hipStrea
   if (nn_w4_fits<2, 2, 3>(a)) {
     if (est < 80 || tiles(128, 128) <= 110 * cus) return launch_nn_w4<MODE, 2, 2, 3, 1>(a, max_rows, s);
     const long long big = tiles(256, 256);
-    if (est >= 192 && (big >= 125 * cus || (est >= 1024 && big >= 60 * cus)) && nn_w4_fits<4, 4, 2>(a))
+    if (est >= 192 && big >= 80 * cus && nn_w4_fits<4, 4, 2>(a))
       return launch_nn_split<MODE, 4, 2>(a, max_rows, s);
     if (nn_w4_fits<4, 2, 3>(a)) return launch_nn_split<MODE, 2, 3>(a, max_rows, s);
     return launch_nn_w4<MODE, 2, 2, 3, 1>(a, max_rows, s);
