@@ -275,7 +275,7 @@ __global__ __launch_bounds__(256) void shrink_both_kernel(const ShrinkArgs v, in
 // Out is stored past the caches (8192 tokens x 4096, rank 16, with both products before it: 81 us, 85 otherwise); Base read past
 // them costs 94.  Measured, bf16: 16384 tokens x 7168, rank 64 (474 MB) 132 to 142 us, 3.4 to 3.6 TB/s: 64-token tiles wait for Base with
 // the few waves they leave room for, and 32-token ones read the factors twice as often (with shrink 228 us, 199 then).  8192 x 4096,
-// rank 16: 29 us, 4.6 TB/s.
+// rank 16: 30 to 31 us, 4.4 TB/s (29 with u as one bf16).
 struct ExpandArgs {
   AdapterArgs ad;
   const float* U;
@@ -491,7 +491,9 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
 //
 // Both operands run along the tokens, so a slice of 64 rows x 256 bytes and the numbers of its tokens go to LDS and are read
 // across; the next slice's rows are on their way meanwhile.  Every row is read once, the numbers once for each 256 bytes of it.
-// Measured, bf16, dA and dB of 8192 tokens x 4096 x 4096, rank 16, 8 adapters: 134 MB in 25 us, 5.3 TB/s, and 5 us to join.
+// Measured, bf16, dA and dB of 8192 tokens x 4096 x 4096, rank 16, 8 adapters: 134 MB in 26 us, 5.1 TB/s, and 5 us to join.  The numbers'
+// second parts cost 1 us of it; at rank 128, where their LDS reads count as much as the rows', they take the whole gradient of 16384
+// tokens of 4 adapters from 404 to 465 us.
 struct OuterArgs {
   AdapterArgs ad;
   const float* U;
@@ -673,7 +675,8 @@ __global__ __launch_bounds__(256) void outer_join_kernel(const OuterArgs da, int
 // A stable counting sort without counters: a request's place is the sum of the lengths of all requests that come before it
 // by (adapter, number), which a wave adds up 64 requests at a time.  One launch, no workspace, no atomics, the same bits
 // whatever runs first; n_req^2 / 64 steps over the chip, which beats a pass per digit for the batches of a serving step.
-// 4.0 us for 256 requests of a token each, 4.4 for 96 of 32768 tokens: a launch and three loads that wait for one another.
+// 4.0 us for 256 requests of a token each, 4.4 for 96 of 32768 tokens: a launch and three loads that wait for one another.  As a graph's
+// node 5.4 us for 256 requests of a token, 6.7 for 1024, 18 for 4096, 173 for 16384, 2.4 ms for 65536: past some 4000 requests the square tells.
 __device__ __forceinline__ int wave_sum(int v) {
 #pragma unroll
   for (int off = 32; off; off >>= 1) v += __shfl_xor(v, off);
