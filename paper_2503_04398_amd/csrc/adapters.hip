@@ -465,15 +465,17 @@ __global__ __launch_bounds__(256) void expand_kernel(const ExpandArgs a) {
         const float* d = reinterpret_cast<const float*>(delta + (q * (64 / LPR) + lane / LPR) * 144) + l_col;
         u32x4_t v = now[t][q];
         const f32x4_t lo = *reinterpret_cast<const f32x4_t*>(d);
-        if constexpr (F32) {
+        if (!none) {  // else Base as it is, bit for bit
+          if constexpr (F32) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + lo[e]);
-        } else {
-          const f32x4_t hi = *reinterpret_cast<const f32x4_t*>(d + 4);
+            for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + lo[e]);
+          } else {
+            const f32x4_t hi = *reinterpret_cast<const f32x4_t*>(d + 4);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const f32x4_t& two = e < 2 ? lo : hi;
-            v[e] = cvt_pk_bf16(__uint_as_float(v[e] << 16) + two[(e & 1) * 2], __uint_as_float(v[e] & 0xffff0000u) + two[(e & 1) * 2 + 1]);
+            for (int e = 0; e < 4; ++e) {
+              const f32x4_t& two = e < 2 ? lo : hi;
+              v[e] = cvt_pk_bf16(__uint_as_float(v[e] << 16) + two[(e & 1) * 2], __uint_as_float(v[e] & 0xffff0000u) + two[(e & 1) * 2 + 1]);
+            }
           }
         }
         if (there[t][q] && c0 + l_col < c_hi) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(out_row[t][q] + c0));

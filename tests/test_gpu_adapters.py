@@ -681,3 +681,16 @@ def test_index_of_the_most_requests(n_req, n, longest):
     (14000, 64), (20000, 48), (18600, 48)])
 def test_both_sides_of_the_lines_of_the_token_tiles(T, rank, dtype):
     _both(Batch([T // 2 + 5, 9, T - T // 2 - 21], [1, 0, 1], 2, rank, 40, 24, dtype, pad=7, seed=T))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_without_an_adapter_are_the_base_bit_for_bit(dtype):
+    """zeros of both signs, infinities and NaN of any bits among them, as in place"""
+    b = Batch([3, 40, 2], [-1, 5, 0], 2, 16, 72, 136, dtype, seed=41)
+    as_int, odd = (torch.int16, [-32768, 0, 0x7f80, 0x7f81, -1, 1]) if dtype == "bf16" else (torch.int32, [-2 ** 31, 0, 0x7f800000, 0x7f800001, -1, 1])
+    for t in (b.Yb, b.dXb):
+        bits = t.view(as_int)
+        bits[:43, ::2] = torch.tensor(odd, dtype=as_int).repeat(43 * bits.shape[1] // 2 // 6 + 1)[:43 * (bits.shape[1] // 2)].view(43, -1)
+    Y, dX = _forward(b), _gradient(b)[0]
+    assert torch.equal(Y[:43].view(as_int).cpu(), b.Yb[:43].view(as_int))
+    assert torch.equal(dX[:43].view(as_int).cpu(), b.dXb[:43].view(as_int))
