@@ -6,7 +6,7 @@
 //   dA_a = sum over a's tokens of v x^T        dB_a = sum of dY u^T
 // so everything is made of three kernels over the ordered tokens: `shrink` (rows times a factor, down to rank numbers),
 // `expand` (rank numbers times a factor, added to rows) and `outer` (sums over tokens).  u and v are fp32 sums in the
-// workspace.  As operands of the matrix instructions of bf16 rows they are taken in two parts, the nearest bf16 and what that leaves,
+// workspace.  As operands of the matrix instructions of bf16 rows they are taken in two parts, the upper half and what that leaves,
 // 16 bits between them: half a step of the result's type is then the whole error, where one rounding of u would add as much again
 // (8192 tokens x 4096, rank 16, against 64 bits: 1.66e-3, and 2.35e-3 with u and v in bf16).
 //
@@ -48,11 +48,16 @@ struct Elem<false> {
 template <bool F32>
 constexpr int kParts = F32 ? 1 : 2;
 
-// a and b as bf16 in hi, what these leave in lo; beside an infinity or NaN nothing is left
+// The upper halves of a and b in hi, and what these leave, as bf16, in lo.  Cut off and not rounded, so that what is left has the
+// number's sign: beside an infinity in the other operand both products are infinite the same way.  For that, too, nothing left
+// becomes 2^-60 of the number, and an infinity leaves an infinity; NaN leaves NaN.  2^-16 of a number is lost at most.
+__device__ __forceinline__ float left_of(float a) {
+  const float r = a - __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+  return fabsf(a) == __builtin_huge_valf() ? a : (r == 0.0f ? a * 0x1p-60f : r);
+}
 __device__ __forceinline__ void two_parts(float a, float b, uint32_t* hi, uint32_t* lo) {
-  *hi = cvt_pk_bf16(a, b);
-  const float ra = a - __uint_as_float(*hi << 16), rb = b - __uint_as_float(*hi & 0xffff0000u);
-  *lo = cvt_pk_bf16(fabsf(ra) <= fabsf(a) ? ra : 0.0f, fabsf(rb) <= fabsf(b) ? rb : 0.0f);
+  *hi = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+  *lo = cvt_pk_bf16(left_of(a), left_of(b));
 }
 
 __device__ __forceinline__ u32x4_t load_piece(const void* p) { return *reinterpret_cast<const u32x4_t*>(p); }

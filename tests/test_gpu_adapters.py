@@ -694,3 +694,33 @@ def test_rows_without_an_adapter_are_the_base_bit_for_bit(dtype):
     Y, dX = _forward(b), _gradient(b)[0]
     assert torch.equal(Y[:43].view(as_int).cpu(), b.Yb[:43].view(as_int))
     assert torch.equal(dX[:43].view(as_int).cpu(), b.dXb[:43].view(as_int))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("where", ["X", "dY", "A", "B", "large"])
+def test_infinities_keep_their_signs(where, dtype):
+    """one infinity in a row or a factor: what it meets is infinite with the sign of the product, all else is as exact as ever; u
+    and v near the end of the range stay finite"""
+    b = Batch([1, 40], [0, 1], 2, 16, 136, 72, dtype, seed=43)
+    if where == "large":
+        b.A[0], b.X[0] = 0.0, 0.0
+        b.A[0, :, 0], b.X[0, 0] = 1.0, 3.3895e38  # u = s times that, s below 1
+        b.scale[0], b.B[0] = 1.0 - 2.0 ** -20, b.B[0] * 2.0 ** -10
+    else:
+        t = getattr(b, where)
+        t[(0, 9) if t.dim() == 2 else (0, 2, 9) if where == "A" else (0, 9, 2)] = float("inf") if where in "XA" else -float("inf")
+    with np.errstate(invalid="ignore"):
+        of, s = b.of, _np(b.scale)
+        X, dY, A, B = _np(b.X), _np(b.dY), _np(b.A), _np(b.B)
+        wants = [G.adapters(X, of, A, B, s, _np(b.Yb)), *G.adapters_grad(X, dY, of, A, B, s, _np(b.dXb))]
+    for name, got, want in zip(("Y", "dX", "dA", "dB"), [_forward(b), *_gradient(b)], wants):
+        got = _np(got)
+        odd = ~np.isfinite(want)
+        if where == "large":
+            assert not odd.any()
+            odd = np.abs(want) > 3e38  # within a step of the end of the range
+        else:
+            inf = np.isinf(want)
+            assert (got[inf] == want[inf]).all() and not np.isfinite(got[np.isnan(want)]).any(), name  # NaN: infinities of both signs meet
+        assert np.isfinite(got[~odd]).all(), name
+        assert np.linalg.norm((got - want)[~odd] / 1e20) <= 2.0 ** -8 * np.linalg.norm(want[~odd] / 1e20), name
