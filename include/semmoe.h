@@ -58,6 +58,8 @@ extern "C" {
 #define SEMMOE_MAX_ADAPTERS 1024    /* low-rank adapters of one call */
 #define SEMMOE_MAX_RANK 128         /* their rank */
 #define SEMMOE_MAX_REQUESTS 65536   /* requests of one adapter_index */
+#define SEMMOE_MAX_NORM_D 16384     /* width of block_norm's rows */
+#define SEMMOE_MAX_I8_DEPTH 131056  /* numbers of an 8-bit row of a product: 2^31 / 2^14 and less, so that int32 sums are exact */
 
 typedef struct semmoe_config {
   int32_t T, d, E, k, F, D;
@@ -569,6 +571,112 @@ int32_t semmoe_adapters_grad(const semmoe_config* cfg, void* stream, const semmo
                              const void* dY, const int32_t* order, const int32_t* adapter_offsets, const void* A,
                              const void* B, const float* scale, const void* dX_base, void* dX, void* dA, void* dB,
                              void* ws, size_t ws_bytes);
+
+/*
+ * The layer in 8-bit integers, with a scale for each row of activations (token) and of weights (output channel):
+ *   quantize_rows, or block_norm's Xq  ->  linear_i8, shared_ffn_i8,  dispatch_rows_i8 -> expert_ffn_i8  (-> combine)
+ * A row x in 8 bits is q = rint(x * (127 / max|x|)), ties to even, and scale = max|x| / 127 (fp32; zero rows: 0 and 0); x is within
+ * max|x| / 254 of scale * q.  A row with an infinity or a NaN has scale NaN and q = 0, and so have the results made of it.  The
+ * products take any int8 values and scales; sums are int32 and exact.  Results are bf16: cfg->dtype is SEMMOE_BF16 in the calls
+ * that multiply (else SEMMOE_EUNSUPPORTED), either type in quantize_rows.
+ */
+
+/*
+ * quantize_rows - rows of activations, or of weights ([channels, inputs]), in 8 bits.  cfg: dtype is used.
+ * ldx: distance of X's rows in elements, 0 = packed, a multiple of 8; n_cols % 8 == 0.
+ * dev in : X[n_rows,n_cols] act.  dev out: Xq[n_rows,n_cols] i8, packed; x_scale[n_rows] f32.
+ */
+int32_t semmoe_quantize_rows(const semmoe_config* cfg, void* stream, const void* X, int32_t n_rows, int32_t n_cols,
+                             int64_t ldx, void* Xq, float* x_scale);
+
+/*
+ * dispatch_rows_i8 - semmoe_dispatch_rows for rows in 8 bits and their scales: Xq_perm[slot_of_pair[i*k+j],:] = Xq[i,:],
+ * x_scale_perm[slot_of_pair[i*k+j]] = x_scale[i].  d % 16 == 0; a slot outside [0,P) is left out.  cfg: T, k, d.
+ * dev in : Xq[T,d] i8; x_scale[T] f32; slot_of_pair[P].  dev out: Xq_perm[P,d] i8; x_scale_perm[P] f32.
+ */
+int32_t semmoe_dispatch_rows_i8(const semmoe_config* cfg, void* stream, const void* Xq, const float* x_scale,
+                                const int32_t* slot_of_pair, void* Xq_perm, float* x_scale_perm);
+
+/*
+ * linear_i8 - a projection: Y[t,n] = x_scale[t] w_scale[n] sum_c Xq[t,c] Wq[n,c], rounded once.  cfg: dtype is used.
+ * d_in % 16 == 0, at most SEMMOE_MAX_I8_DEPTH; d_out % 8 == 0.  ldx, ldy: distances of rows in elements, 0 = packed, multiples of 16
+ * and of 8; w_scale lies on 16 bytes.  No workspace.
+ * dev in : Xq[n_rows,d_in] i8; x_scale[n_rows] f32; Wq[d_out,d_in] i8; w_scale[d_out] f32.  dev out: Y[n_rows,d_out] bf16.
+ */
+typedef struct semmoe_linear_shape {
+  int32_t n_rows, d_in, d_out;
+  int64_t ldx, ldy;
+} semmoe_linear_shape;
+
+int32_t semmoe_linear_i8(const semmoe_config* cfg, void* stream, const semmoe_linear_shape* shape, const void* Xq,
+                         const float* x_scale, const void* Wq, const float* w_scale, void* Y);
+
+/*
+ * expert_ffn_i8 - semmoe_expert_ffn in 8 bits: with g, u = the two products with W_gate[e], W_up[e], scaled,
+ *   h = silu(g) u rounded to bf16, then in 8 bits with a scale for each row;  Y[s] = the product of that with W_down[e], scaled.
+ * rank, offsets and weights as in semmoe_expert_ffn; rows of other ranks in Y are not written.  d % 16 == 0 and F % 16 == 0.
+ * dev in : Xq_perm[P,d] i8, x_scale_perm[P] f32; expert_offsets[E+1]; expert_of_phys[E]; Wq_gu[E,2F,d] i8, w_scale_gu[E,2F] f32;
+ *          Wq_down[E,d,F] i8, w_scale_down[E,d] f32 (scales of weights on 16 bytes).  dev out: Y[P,d] bf16.
+ * ws: T*k rows of 3F bytes and a float, + 1024 bytes (not covered by semmoe_workspace_bytes).
+ */
+int32_t semmoe_expert_ffn_i8(const semmoe_config* cfg, void* stream, int32_t rank, const void* Xq_perm,
+                             const float* x_scale_perm, const int32_t* expert_offsets, const int32_t* expert_of_phys,
+                             const void* Wq_gu, const float* w_scale_gu, const void* Wq_down, const float* w_scale_down, void* Y,
+                             void* ws, size_t ws_bytes);
+
+/* shared_ffn_i8 - the same with one set of weights: Xq[n_tokens,d] -> Y_shared[n_tokens,d].  n_tokens <= T*k.
+ * ws: n_tokens rows of 3F bytes and a float, + 1024 bytes. */
+int32_t semmoe_shared_ffn_i8(const semmoe_config* cfg, void* stream, const void* Xq, const float* x_scale, int32_t n_tokens,
+                             const void* Wq_gu_sh, const float* w_scale_gu_sh, const void* Wq_down_sh,
+                             const float* w_scale_down_sh, void* Y_shared, void* ws, size_t ws_bytes);
+
+/*
+ * What stands between two blocks of a model whose residual is R (the layer here is one such block): the norm behind a block with
+ * its gate and the residual's scale, and the norm before the next one.
+ *   n = Y * rsqrt(mean(Y^2) + eps_post) * w_post   (w_post NULL: Y itself);
+ *   H = res_scale * R + gate * n                   (gate NULL: 1; R or Y NULL: without that term);
+ *   X = H * rsqrt(mean(H^2) + eps_pre) * w_pre.
+ * gate has one number for each channel (gate_rows = 0: gate[d]) or for each number of a row (gate_rows != 0: gate[T,d]).
+ * ld*: distances of rows in elements, 0 = packed, multiples of 8, at least d; pointers lie on 16 bytes.  d <= SEMMOE_MAX_NORM_D.
+ * cfg: T (rows), d and dtype are used.
+ */
+typedef struct semmoe_norm_shape {
+  float res_scale, eps_post, eps_pre;
+  int32_t gate_rows;
+  int64_t ld_r, ld_y, ld_h, ld_x, ld_gate;
+  int64_t ld_dh, ld_dx, ld_dr, ld_dy, ld_dgate; /* block_norm_grad */
+} semmoe_norm_shape;
+
+/*
+ * block_norm - H and X of one pass; statistics and everything between in fp32, H and X rounded once (X is made of H before its
+ * rounding).  Xq, x_scale: X in 8 bits (see above) in its place or beside it, made of X before its rounding, rows packed.
+ * dev in : R[T,d], Y[T,d], w_post[d], gate, w_pre[d] act, each may be NULL as far as the formulas say (w_pre where X and Xq are).
+ * dev out: H[T,d] act or NULL; X[T,d] act or NULL; Xq[T,d] i8 and x_scale[T] f32, or both NULL; one at least.  H and X may lie in the
+ *          place of R or Y (with the same ld), not in each other's.
+ */
+int32_t semmoe_block_norm(const semmoe_config* cfg, void* stream, const semmoe_norm_shape* shape, const void* R, const void* Y,
+                          const void* w_post, const void* gate, const void* w_pre, void* H, void* X, void* Xq, float* x_scale);
+
+/* Workspace of semmoe_block_norm_grad for this config: the columns' sums of its workgroups. */
+int32_t semmoe_block_norm_grad_workspace_bytes(const semmoe_config* cfg, size_t* bytes_out /*host*/);
+
+/*
+ * block_norm_grad - the gradient of semmoe_block_norm for dH (what reaches H on other ways; NULL: nothing) and dX (NULL: X has not
+ * been asked for, w_pre is NULL then), H as the forward call stored it:
+ *   dH' = dH + rh (dX w_pre - H rh mean(dX w_pre H rh)),  rh = rsqrt(mean(H^2) + eps_pre);
+ *   dR = res_scale dH';  dgate = dH' n (summed over the rows where gate has one row);
+ *   dY = ry (b - Y ry mean(b Y ry)),  b = dH' gate w_post,  ry = rsqrt(mean(Y^2) + eps_post)  (without w_post: dH' gate);
+ *   dw_pre = sum over rows of dX H rh;  dw_post = sum of dH' gate Y ry.
+ * fp32 throughout, sums over rows in a fixed order, the results rounded once.
+ * dev in : dH[T,d], dX[T,d], H[T,d] (with dX), Y[T,d], w_post, gate, w_pre act, as in the forward call.
+ * dev out: dR[T,d], dY[T,d], dgate (as gate), dw_post[d], dw_pre[d] act, each may be NULL, not all; dR, dY and dgate[T,d] may lie in
+ *          the place of one of dH, dX, H, Y (with the same ld), not in each other's.
+ * ws: semmoe_block_norm_grad_workspace_bytes; NULL where no sum over rows is asked for.
+ */
+int32_t semmoe_block_norm_grad(const semmoe_config* cfg, void* stream, const semmoe_norm_shape* shape, const void* dH,
+                               const void* dX, const void* H, const void* Y, const void* w_post, const void* gate,
+                               const void* w_pre, void* dR, void* dY, void* dgate, void* dw_post, void* dw_pre, void* ws,
+                               size_t ws_bytes);
 
 /*
  * Probes of what the chip sustains, for reading roofline fractions against (not part of the layer; no passage of

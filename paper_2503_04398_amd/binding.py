@@ -52,6 +52,17 @@ class _CAdapterShape(C.Structure):
                 ("ldx", C.c_int64), ("ldy", C.c_int64), ("ld_base", C.c_int64), ("ld_out", C.c_int64)]
 
 
+class _CLinearShape(C.Structure):
+    """semmoe_linear_shape of the C header, field for field"""
+    _fields_ = [("n_rows", C.c_int32), ("d_in", C.c_int32), ("d_out", C.c_int32), ("ldx", C.c_int64), ("ldy", C.c_int64)]
+
+
+class _CNormShape(C.Structure):
+    """semmoe_norm_shape of the C header, field for field"""
+    _fields_ = [("res_scale", C.c_float), ("eps_post", C.c_float), ("eps_pre", C.c_float), ("gate_rows", C.c_int32)] + [
+        (n, C.c_int64) for n in ("ld_r", "ld_y", "ld_h", "ld_x", "ld_gate", "ld_dh", "ld_dx", "ld_dr", "ld_dy", "ld_dgate")]
+
+
 @dataclass
 class Config:
     T: int
@@ -137,6 +148,14 @@ _SIGS = {
     "semmoe_adapter_forward_workspace_bytes": ([_P, _P, C.POINTER(C.c_size_t)], C.c_int32),
     "semmoe_adapters": ([_P] * 12 + [C.c_size_t], C.c_int32),
     "semmoe_adapters_grad": ([_P] * 15 + [C.c_size_t], C.c_int32),
+    "semmoe_quantize_rows": ([_P, _P, _P, C.c_int32, C.c_int32, C.c_int64, _P, _P], C.c_int32),
+    "semmoe_dispatch_rows_i8": ([_P] * 7, C.c_int32),
+    "semmoe_linear_i8": ([_P] * 8, C.c_int32),
+    "semmoe_expert_ffn_i8": ([_P, _P, C.c_int32] + [_P] * 10 + [C.c_size_t], C.c_int32),
+    "semmoe_shared_ffn_i8": ([_P] * 4 + [C.c_int32] + [_P] * 6 + [C.c_size_t], C.c_int32),
+    "semmoe_block_norm": ([_P] * 12, C.c_int32),
+    "semmoe_block_norm_grad_workspace_bytes": ([_P, C.POINTER(C.c_size_t)], C.c_int32),
+    "semmoe_block_norm_grad": ([_P] * 16 + [C.c_size_t], C.c_int32),
     "semmoe_probe_copy": ([_P, _P, _P, C.c_size_t], C.c_int32),
     "semmoe_probe_stream": ([_P, _P, C.c_size_t, C.c_int32, _P], C.c_int32),
     "semmoe_probe_mfma": ([_P, _P, C.c_int32, _P, C.POINTER(C.c_double)], C.c_int32),
@@ -206,7 +225,7 @@ class SemMoE:
     """One config + one workspace; methods mirror the C entry points one to one.
 
     Calls that use the workspace of the config (`ws`, `ws_shared`) take their turns on one stream.  Those that name a size of their own
-    (the FFN gradients and the adapters) may be made from several threads and on several streams at once."""
+    (the gradients of FFN and norms, the adapters, the FFN in 8 bits) may be made from several threads and on several streams at once."""
 
     def __init__(self, cfg: Config, device="cuda:0", allocate_workspace: bool = True):
         self.lib = load_library()
@@ -678,3 +697,149 @@ class SemMoE:
             C.byref(c), _stream(), C.byref(s), X.data_ptr(), dY.data_ptr(), _ptr(order), _ptr(adapter_offsets), _ptr(A), _ptr(B),
             _ptr(scale), None if dX_base is None else dX_base.data_ptr(), None if dX is None else dX.data_ptr(), _ptr(dA),
             _ptr(dB), ws, n))
+
+    # -- rows and weights in 8-bit integers
+    def quantize_rows(self, X, Xq, x_scale):
+        """X's rows may lie further apart than they are wide; Xq is packed.  Serves activations and weights alike."""
+        n, cols = X.shape
+        here, _, f32, acts = self._types
+        dev, act = X.get_device(), acts[self.cfg.dtype == BF16]
+        if dev < 0 or dev != here() or not (
+                act is X.dtype and self._torch.int8 is Xq.dtype and f32 is x_scale.dtype
+                and dev == Xq.get_device() == x_scale.get_device() and Xq.numel() >= n * cols and x_scale.numel() >= n):
+            self._fit("quantize_rows", ((X, None, 0), (Xq, self._torch.int8, n * cols), (x_scale, f32, n)))
+        if n == 0:
+            return
+        c = self._cfg()
+        self._check("semmoe_quantize_rows", self.lib.semmoe_quantize_rows(
+            C.byref(c), _stream(), X.data_ptr(), n, cols, _row_distance(X, cols, "X"), _ptr(Xq), _ptr(x_scale)))
+
+    def dispatch_rows_i8(self, Xq, x_scale, slot_of_pair, Xq_perm, x_scale_perm):
+        T, d, P = self.cfg.T, self.cfg.d, self.cfg.T * self.cfg.k
+        if T == 0:
+            return
+        here, i32, f32, _ = self._types
+        dev, i8 = Xq.get_device(), self._torch.int8
+        if dev < 0 or dev != here() or not (
+                i8 is Xq.dtype is Xq_perm.dtype and f32 is x_scale.dtype is x_scale_perm.dtype and i32 is slot_of_pair.dtype
+                and dev == x_scale.get_device() == slot_of_pair.get_device() == Xq_perm.get_device() == x_scale_perm.get_device()
+                and Xq.numel() >= T * d and x_scale.numel() >= T and slot_of_pair.numel() >= P and Xq_perm.numel() >= P * d
+                and x_scale_perm.numel() >= P):
+            self._fit("dispatch_rows_i8", ((Xq, i8, T * d), (x_scale, f32, T), (slot_of_pair, i32, P), (Xq_perm, i8, P * d),
+                                           (x_scale_perm, f32, P)))
+        c = self._cfg()
+        self._check("semmoe_dispatch_rows_i8", self.lib.semmoe_dispatch_rows_i8(
+            C.byref(c), _stream(), _ptr(Xq), _ptr(x_scale), _ptr(slot_of_pair), _ptr(Xq_perm), _ptr(x_scale_perm)))
+
+    def linear_i8(self, Xq, x_scale, Wq, w_scale, Y):
+        """Y[T,d_out] of Xq[T,d_in], Wq[d_out,d_in]; Xq and Y may be column ranges of wider tensors"""
+        (n, d_in), d_out = Xq.shape, Wq.shape[0]
+        if tuple(Wq.shape) != (d_out, d_in) or tuple(Y.shape) != (n, d_out):
+            raise SemMoEError("linear_i8: shapes must be Xq[T,d_in], Wq[d_out,d_in], Y[T,d_out]", -2)
+        here, _, f32, acts = self._types
+        dev, i8 = Xq.get_device(), self._torch.int8
+        if dev < 0 or dev != here() or not (
+                i8 is Xq.dtype is Wq.dtype and f32 is x_scale.dtype is w_scale.dtype and acts[1] is Y.dtype
+                and dev == x_scale.get_device() == Wq.get_device() == w_scale.get_device() == Y.get_device()
+                and x_scale.numel() >= n and w_scale.numel() >= d_out):
+            self._fit("linear_i8", ((Xq, i8, 0), (x_scale, f32, n), (Wq, i8, 0), (w_scale, f32, d_out), (Y, acts[1], 0)))
+        if n == 0:
+            return
+        c, s = self._cfg(), _CLinearShape(n, d_in, d_out, _row_distance(Xq, d_in, "Xq"), _row_distance(Y, d_out, "Y"))
+        self._check("semmoe_linear_i8", self.lib.semmoe_linear_i8(
+            C.byref(c), _stream(), C.byref(s), Xq.data_ptr(), _ptr(x_scale), _ptr(Wq), _ptr(w_scale), Y.data_ptr()))
+
+    def expert_ffn_i8(self, rank, Xq_perm, x_scale_perm, expert_offsets, expert_of_phys, Wq_gu, w_scale_gu, Wq_down, w_scale_down, Y):
+        """the weights and their scales hold every expert that expert_of_phys names for the rank"""
+        d, F, E, P = self.cfg.d, self.cfg.F, self.cfg.E, self.cfg.T * self.cfg.k
+        if P == 0:
+            return
+        here, i32, f32, acts = self._types
+        i8 = self._torch.int8
+        self._fit("expert_ffn_i8", ((Xq_perm, i8, P * d), (x_scale_perm, f32, P), (expert_offsets, i32, E + 1),
+                                    (expert_of_phys, i32, E), (Wq_gu, i8, 2 * F * d), (w_scale_gu, f32, 2 * F), (Wq_down, i8, F * d),
+                                    (w_scale_down, f32, d), (Y, acts[1], P * d)))
+        c = self._cfg()
+        ws, n, owner = self._workspace("expert_ffn_i8", P * (3 * F + 4) + 1024)
+        self._check("semmoe_expert_ffn_i8", self.lib.semmoe_expert_ffn_i8(
+            C.byref(c), _stream(), int(rank), _ptr(Xq_perm), _ptr(x_scale_perm), _ptr(expert_offsets), _ptr(expert_of_phys),
+            _ptr(Wq_gu), _ptr(w_scale_gu), _ptr(Wq_down), _ptr(w_scale_down), _ptr(Y), ws, n))
+
+    def shared_ffn_i8(self, Xq, x_scale, n_tokens, Wq_gu_sh, w_scale_gu_sh, Wq_down_sh, w_scale_down_sh, Y_shared):
+        d, F, n = self.cfg.d, self.cfg.F, int(n_tokens)
+        if n == 0:
+            return
+        here, _, f32, acts = self._types
+        i8 = self._torch.int8
+        self._fit("shared_ffn_i8", ((Xq, i8, n * d), (x_scale, f32, n), (Wq_gu_sh, i8, 2 * F * d), (w_scale_gu_sh, f32, 2 * F),
+                                    (Wq_down_sh, i8, F * d), (w_scale_down_sh, f32, d), (Y_shared, acts[1], n * d)))
+        c = self._cfg()
+        ws, size, owner = self._workspace("shared_ffn_i8", max(n, 0) * (3 * F + 4) + 1024)
+        self._check("semmoe_shared_ffn_i8", self.lib.semmoe_shared_ffn_i8(
+            C.byref(c), _stream(), _ptr(Xq), _ptr(x_scale), n, _ptr(Wq_gu_sh), _ptr(w_scale_gu_sh), _ptr(Wq_down_sh),
+            _ptr(w_scale_down_sh), _ptr(Y_shared), ws, size))
+
+    # -- the norms around a block
+    def _norm_call(self, call, T, d, res_scale, eps_post, eps_pre, gate, vectors, rows):
+        """(config, shape): vectors are w_post and w_pre with the gradients of such, rows the tensors [T,d] by the name of their
+        distance.  A gate of one dimension is all rows' (its gradient then is one row, too)."""
+        s = _CNormShape(res_scale, eps_post, eps_pre, int(gate is not None and gate.dim() == 2))
+        for t in vectors:
+            if t is not None and tuple(t.shape) != (d,):
+                raise SemMoEError("%s: a norm's weights and a gate of all rows have %d numbers" % (call, d), -2)
+        for name, t in rows:
+            if t is not None:
+                if tuple(t.shape) != (T, d):
+                    raise SemMoEError("%s: rows must be [%d, %d]" % (call, T, d), -2)
+                setattr(s, name, _row_distance(t, d, name))
+        return (self._cfg() if (self.cfg.T, self.cfg.d) == (T, d) else self._cfg(T=T, d=d)), s
+
+    def block_norm(self, R, H, Y=None, X=None, Xq=None, x_scale=None, w_post=None, w_pre=None, gate=None, res_scale=1.0,
+                   eps_post=1e-6, eps_pre=1e-6):
+        """H = res_scale R + gate norm(Y) w_post, X = norm(H) w_pre, and X in 8 bits as Xq and x_scale; what is None is left out.
+        gate: [d] or [T,d].  H and X may lie in the place of R or Y."""
+        T, d = (Y if R is None else R).shape
+        of_all = gate is not None and gate.dim() == 1
+        c, s = self._norm_call("block_norm", T, d, res_scale, eps_post, eps_pre, gate, (w_post, w_pre, gate if of_all else None), (
+            ("ld_r", R), ("ld_y", Y), ("ld_h", H), ("ld_x", X), ("ld_gate", None if of_all else gate)))
+        if H is not None and X is not None and T and H.data_ptr() == X.data_ptr():
+            raise SemMoEError("block_norm: H and X lie in the same place", -1)
+        torch = self._torch
+        self._fit("block_norm", ((R, None, 0), (Y, None, 0), (w_post, None, d), (gate, None, 0), (w_pre, None, d), (H, None, 0),
+                                 (X, None, 0), (Xq, torch.int8, T * d), (x_scale, torch.float32, T)))
+        if T == 0:
+            return
+        self._check("semmoe_block_norm", self.lib.semmoe_block_norm(
+            C.byref(c), _stream(), C.byref(s), *(None if t is None else t.data_ptr() for t in (R, Y, w_post, gate, w_pre, H, X)),
+            _ptr(Xq), _ptr(x_scale)))
+
+    def block_norm_grad(self, H, dR, Y=None, dH=None, dX=None, w_post=None, w_pre=None, gate=None, dY=None, dgate=None, dw_post=None,
+                        dw_pre=None, res_scale=1.0, eps_post=1e-6, eps_pre=1e-6):
+        """each of dR, dY, dgate, dw_post and dw_pre may be None; dH or dX may, and H without dX.  dR, dY and a dgate of rows may lie in
+        the place of one of dH, dX, H and Y, not in each other's."""
+        T, d = (dX if dH is None else dH).shape
+        of_all = gate is not None and gate.dim() == 1
+        if dgate is not None and (gate is None or dgate.shape != gate.shape):
+            raise SemMoEError("block_norm_grad: dgate has gate's shape", -2)
+        c, s = self._norm_call("block_norm_grad", T, d, res_scale, eps_post, eps_pre, gate,
+                               (w_post, w_pre, dw_post, dw_pre, gate if of_all else None), (
+            ("ld_dh", dH), ("ld_dx", dX), ("ld_h", H), ("ld_y", Y), ("ld_dr", dR), ("ld_dy", dY),
+            ("ld_gate", None if of_all else gate), ("ld_dgate", None if of_all else dgate)))
+        outs = [t.data_ptr() for t in (dR, dY, dgate, dw_post, dw_pre) if t is not None and t.numel()]
+        if len(set(outs)) != len(outs):
+            raise SemMoEError("block_norm_grad: two results lie in the same place", -1)
+        self._fit("block_norm_grad", tuple((t, None, 0) for t in (dH, dX, H, Y, w_post, gate, w_pre, dR, dY, dgate, dw_post, dw_pre)))
+        if T == 0:
+            for t in (dgate, dw_post, dw_pre):
+                if t is not None:
+                    t.zero_()
+            return
+        ws, n, owner = None, 0, None
+        if dw_post is not None or dw_pre is not None or (of_all and dgate is not None):
+            need = C.c_size_t(0)
+            self._check("semmoe_block_norm_grad_workspace_bytes",
+                        self.lib.semmoe_block_norm_grad_workspace_bytes(C.byref(c), C.byref(need)))
+            ws, n, owner = self._workspace("block_norm_grad", need.value)
+        self._check("semmoe_block_norm_grad", self.lib.semmoe_block_norm_grad(
+            C.byref(c), _stream(), C.byref(s),
+            *(None if t is None else t.data_ptr() for t in (dH, dX, H, Y, w_post, gate, w_pre, dR, dY, dgate, dw_post, dw_pre)), ws, n))

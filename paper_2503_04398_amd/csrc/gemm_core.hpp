@@ -14,9 +14,17 @@ namespace semmoe {
 
 // kModeSwigluGrad: the sums are gate and up as in kModeSwiglu; with dh, the gradient of silu(gate) * up, out[row] gets
 // [dgate | dup], 2N numbers.
-enum GemmMode { kModeLogits = 0, kModeSwiglu = 1, kModeStore = 2, kModeSwigluGrad = 3 };
+// kModeSwigluI8, kModeStoreI8: operands are 8-bit integers with a scale for each row of X and of W.  An MFMA takes 16 bytes of a
+// row a lane whatever they hold (16 integers of v_mfma_i32_32x32x32_i8 where it is 8 bf16 numbers, in the same number of cycles), so
+// these kernels are those of bf16 rows of half the length: K, ldx, ldw and w_group_stride count pairs of integers.  Sums are
+// int32, kept as bits in the float accumulators, and exact below 2^31, that is up to K = 2^17 integers.
+enum GemmMode { kModeLogits = 0, kModeSwiglu = 1, kModeStore = 2, kModeSwigluGrad = 3, kModeSwigluI8 = 4, kModeStoreI8 = 5 };
 template <int MODE>
-constexpr bool kPaired = MODE == kModeSwiglu || MODE == kModeSwigluGrad;  // weight rows are N gate and N up rows
+constexpr bool kI8 = MODE == kModeSwigluI8 || MODE == kModeStoreI8;
+template <int MODE>
+constexpr bool kHidden = MODE == kModeSwiglu || MODE == kModeSwigluI8;  // silu(gate) * up is stored
+template <int MODE>
+constexpr bool kPaired = kHidden<MODE> || MODE == kModeSwigluGrad;  // weight rows are N gate and N up rows
 
 struct GemmArgs {
   const void* X;          // [rows, K] act
@@ -54,11 +62,36 @@ struct GemmArgs {
   // workgroups run two kernels one after the other, one for the small groups and one for the large).
   int rows_min, rows_max;
   int sched_reverse;      // the tile list from its end (gemm_nn.hpp): the weights that the product before read last come first
+  // 8-bit operands: scales of X's rows, and of the weights' rows (N a group, 2N where gate and up are paired)
+  const float* x_scale;
+  const float* w_scale;
 };
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+
+typedef __attribute__((ext_vector_type(16))) int32_t i32x16_t;
+
+template <int MODE>
+__device__ __forceinline__ f32x16_t tile_mfma(bf16x8_t w, bf16x8_t x, f32x16_t c) {
+  if constexpr (kI8<MODE>)
+    return __builtin_bit_cast(f32x16_t, __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, w), __builtin_bit_cast(i32x4_t, x),
+                                                                              __builtin_bit_cast(i32x16_t, c), 0, 0, 0));
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, x, c, 0, 0, 0);
+}
+
+// a sum of products of 8-bit integers as what it stands for; the sum is rounded to fp32 (2^-24), as each product is
+__device__ __forceinline__ float scaled_sum(float bits, float x_scale, float w_scale) {
+  return float(__float_as_int(bits)) * x_scale * w_scale;
+}
+
+// rounded for the output rows; a NaN scale of 8-bit operands may have any bits
+template <int MODE>
+__device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
+  return kI8<MODE> ? cvt_pk_bf16(lo, hi) : pack_bf16x2(lo, hi);
+}
 
 __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
 
@@ -231,7 +264,7 @@ __device__ __forceinline__ bool walk_tile(const GemmArgs& a, const TileWalk& w, 
 // The caller guarantees that no wave still reads the LDS region and puts a barrier after the call.
 template <int MODE, int NWF, int NWT, int TF, int TT>
 __device__ __forceinline__ void store_tile_via_lds(f32x16_t (&acc)[TF][TT], unsigned char* lds, const GemmArgs& a,
-                                                   int row_lo, int n_tok, int f0, int wf, int wt) {
+                                                   int row_lo, int n_tok, int f0, int wf, int wt, int widx) {
   constexpr int BT = NWT * TT * 32;
   constexpr int FEAT = kPaired<MODE> ? NWF * TF * 16 : NWF * TF * 32;
   constexpr int CPR = FEAT / 8;                   // 16-byte chunks per output row
@@ -241,6 +274,25 @@ __device__ __forceinline__ void store_tile_via_lds(f32x16_t (&acc)[TF][TT], unsi
   const int lane = threadIdx.x & 63;
   const int tok_in = lane & 31, half = lane >> 5;
   bf16_t* out = static_cast<bf16_t*>(a.out);
+  if constexpr (kI8<MODE>) {
+    // a lane's four features of a token are 16 bytes of the weights' scales
+    const float* ws = a.w_scale + size_t(widx) * (kPaired<MODE> ? 2 * a.N : a.N);
+    float xs[TT];
+#pragma unroll
+    for (int j = 0; j < TT; ++j) xs[j] = a.x_scale[row_lo + min((wt * TT + j) * 32 + tok_in, n_tok - 1)];
+#pragma unroll
+    for (int i = 0; i < TF; ++i) {
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4) {
+        const int feat = f0 + (kPaired<MODE> ? wf * (TF / 2) + i / 2 : wf * TF + i) * 32 + g4 * 8 + half * 4;
+        const f32x4_t w = *reinterpret_cast<const f32x4_t*>(ws + (kPaired<MODE> && (i & 1) ? a.N : 0) + min(feat, a.N - 4));
+#pragma unroll
+        for (int j = 0; j < TT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][g4 * 4 + e] = scaled_sum(acc[i][j][g4 * 4 + e], xs[j], w[e]);
+      }
+    }
+  }
   if constexpr (MODE == kModeSwigluGrad) {
     // gate and up give way to their gradients; a lane's four features of a token are 16 bytes of dh
 #pragma unroll
@@ -273,7 +325,7 @@ __device__ __forceinline__ void store_tile_via_lds(f32x16_t (&acc)[TF][TT], unsi
     for (int j = 0; j < TT; ++j) {
       const int t = (wt * TT + j) * 32 + tok_in;
       unsigned char* rowp = lds + t * RB + half * 8;
-      if constexpr (MODE == kModeSwiglu) {
+      if constexpr (kHidden<MODE>) {
 #pragma unroll
         for (int i = 0; i < TF; i += 2) {
 #pragma unroll
@@ -284,7 +336,7 @@ __device__ __forceinline__ void store_tile_via_lds(f32x16_t (&acc)[TF][TT], unsi
             const float h2 = silu_mul(acc[i][j][g4 * 4 + 2], acc[i + 1][j][g4 * 4 + 2]);
             const float h3 = silu_mul(acc[i][j][g4 * 4 + 3], acc[i + 1][j][g4 * 4 + 3]);
             *reinterpret_cast<uint2*>(rowp + ((chunk ^ (t & MASK)) * 16)) =
-                make_uint2(pack_bf16x2(h0, h1), pack_bf16x2(h2, h3));
+                make_uint2(pack_out<MODE>(h0, h1), pack_out<MODE>(h2, h3));
           }
         }
       } else {
@@ -296,7 +348,7 @@ __device__ __forceinline__ void store_tile_via_lds(f32x16_t (&acc)[TF][TT], unsi
             const int chunk = (wf * (TF / STEP) + i / STEP) * 4 + g4;
             const f32x16_t& c = acc[i + part][j];
             *reinterpret_cast<uint2*>(rowp + ((chunk ^ (t & MASK)) * 16)) =
-                make_uint2(pack_bf16x2(c[g4 * 4 + 0], c[g4 * 4 + 1]), pack_bf16x2(c[g4 * 4 + 2], c[g4 * 4 + 3]));
+                make_uint2(pack_out<MODE>(c[g4 * 4 + 0], c[g4 * 4 + 1]), pack_out<MODE>(c[g4 * 4 + 2], c[g4 * 4 + 3]));
           }
         }
       }
@@ -464,7 +516,7 @@ __global__ __launch_bounds__(64 * NWF * NWT, MINW) void gemm_bf16_kernel(GemmArg
         for (int i = 0; i < TF; ++i)
 #pragma unroll
           for (int j = 0; j < TT; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[st & 1][i], bfr[st & 1][j], acc[i][j], 0, 0, 0);
+            acc[i][j] = tile_mfma<MODE>(af[st & 1][i], bfr[st & 1][j], acc[i][j]);
         __builtin_amdgcn_sched_barrier(0);
       }
       __syncthreads();
@@ -472,7 +524,7 @@ __global__ __launch_bounds__(64 * NWF * NWT, MINW) void gemm_bf16_kernel(GemmArg
 
     if constexpr (MODE != kModeLogits) {
       // the K loop ended with a barrier: the ring is free and takes the output tile
-      store_tile_via_lds<MODE, NWF, NWT, TF, TT>(acc, lds_raw, a, row_lo, n_tok, f0, wf, wt);
+      store_tile_via_lds<MODE, NWF, NWT, TF, TT>(acc, lds_raw, a, row_lo, n_tok, f0, wf, wt, widx);
       __syncthreads();
     } else {
       // logits: acc[i][j][r] is expert 8*(r/4) + 4*(lane/32) + r%4 of tile i, token lane%32 of tile j
@@ -680,13 +732,13 @@ __device__ __forceinline__ int gemm_bf16_dma_body(const GemmArgs& a, unsigned ch
         for (int i = 0; i < TF; ++i)
 #pragma unroll
           for (int j = 0; j < TT; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[st & 1][i], bfr[st & 1][j], acc[i][j], 0, 0, 0);
+            acc[i][j] = tile_mfma<MODE>(af[st & 1][i], bfr[st & 1][j], acc[i][j]);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
     __syncthreads();  // every wave has left the ring: it now takes the output tile
     static_assert(MODE != kModeLogits, "the router has its own kernel");
-    store_tile_via_lds<MODE, NWF, NWT, TF, TT>(acc, lds_raw, a, row_lo, n_tok, f0, wf, wt);
+    store_tile_via_lds<MODE, NWF, NWT, TF, TT>(acc, lds_raw, a, row_lo, n_tok, f0, wf, wt, widx);
     __syncthreads();  // the next tile's loads overwrite the staged tile
   }
   return walk.total;
@@ -700,6 +752,8 @@ __global__ __launch_bounds__(64 * NWF * NWT, MINW) void gemm_bf16_dma_kernel(Gem
 
 // host-side launcher: picks the kernel for the dtype, sizes a persistent grid.
 int32_t launch_gemm(int mode, int dtype, const GemmArgs& a, int max_rows, int est_rows_per_group, hipStream_t stream);
+// The same for 8-bit operands (kModeSwigluI8, kModeStoreI8), bf16 results.
+int32_t launch_gemm_i8(int mode, const GemmArgs& a, int max_rows, int est_rows_per_group, hipStream_t stream);
 // X[T, d] . W[N, d]^T with d cut into n_parts equal parts of whole 64-element slices: partial[p][t][n] = raw fp32 sums
 // of part p (four-wave 256 x 256 kernel).  SEMMOE_EUNSUPPORTED when the shape does not fit that kernel.
 int32_t launch_ksplit_gemm(const void* X, const void* W, int T, int N, int d, int n_parts, float* partial,

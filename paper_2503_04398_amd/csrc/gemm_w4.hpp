@@ -692,7 +692,7 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
     }
     wait_vmcnt<0>();   // the standing stream's last loads: nothing may write into the ring any more
     __syncthreads();   // every wave has left the ring: it now takes the output piece
-    store_tile_via_lds<MODE, 2, 2, 2, TT>(acc, lds_raw, a, at.row_lo, at.n_tok, at.f0, wf, wt);
+    store_tile_via_lds<MODE, 2, 2, 2, TT>(acc, lds_raw, a, at.row_lo, at.n_tok, at.f0, wf, wt, widx);
     __syncthreads();   // the next piece's loads overwrite the staged piece
   }
 }

@@ -1,0 +1,105 @@
+// Rows held in the registers of a team of waves: how they are read, written, summed and rounded to 8 bits.
+//
+// A team of `tr` threads (whole waves) owns a row; thread t holds the pieces t, t + tr, ... of eight numbers.  The teams of a workgroup
+// go through the same number of rows, so that their barriers match; a team without a row counts zeros and stores nothing.
+#pragma once
+#include "common.hpp"
+
+namespace semmoe {
+
+typedef __attribute__((ext_vector_type(4))) uint32_t row_u32x4_t;
+
+template <bool BF16>
+struct Eight {  // eight numbers of a row as they lie in memory
+  row_u32x4_t v[BF16 ? 1 : 2];
+  __device__ __forceinline__ void load(const void* base, size_t at) {
+    const row_u32x4_t* p = reinterpret_cast<const row_u32x4_t*>(static_cast<const char*>(base) + at * (BF16 ? 2 : 4));
+    v[0] = p[0];
+    if constexpr (!BF16) v[1] = p[1];
+  }
+  __device__ __forceinline__ void zero() {
+    v[0] = row_u32x4_t{0, 0, 0, 0};
+    if constexpr (!BF16) v[1] = v[0];
+  }
+  __device__ __forceinline__ float operator[](int x) const {
+    if constexpr (BF16) return __uint_as_float(x & 1 ? v[0][x >> 1] & 0xffff0000u : v[0][x >> 1] << 16);
+    else return __uint_as_float(v[x >> 2][x & 3]);
+  }
+  __device__ __forceinline__ void round(const float (&f)[8]) {
+    if constexpr (BF16) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) v[0][x] = cvt_pk_bf16(f[2 * x], f[2 * x + 1]);
+    } else {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) v[x >> 2][x & 3] = __float_as_uint(f[x]);
+    }
+  }
+  __device__ __forceinline__ void store(void* base, size_t at) const {
+    row_u32x4_t* p = reinterpret_cast<row_u32x4_t*>(static_cast<char*>(base) + at * (BF16 ? 2 : 4));
+    p[0] = v[0];
+    if constexpr (!BF16) p[1] = v[1];
+  }
+};
+
+// The sum (or, of bits, the maximum) over a team, the same in all of its threads, in an order that depends on the team's size alone.
+// `part` is LDS of N numbers a wave of the workgroup, of this use alone until another join's barrier has passed.
+template <int N, typename V, typename F>
+__device__ __forceinline__ void team_join(V (&v)[N], V* part, int team_waves, F f) {
+#pragma unroll
+  for (int off = 32; off; off >>= 1)
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = f(v[n], __shfl_xor(v[n], off));
+  if (team_waves == 1) return;  // uniform
+  const int wave = threadIdx.x >> 6, first = wave / team_waves * team_waves;
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int n = 0; n < N; ++n) part[wave * N + n] = v[n];
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < N; ++n) v[n] = part[first * N + n];
+  for (int w = 1; w < team_waves; ++w)
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = f(v[n], part[(first + w) * N + n]);
+}
+
+__device__ __forceinline__ uint32_t magnitude_bits(float f) { return __float_as_uint(f) & 0x7fffffffu; }
+
+// A row in 8 bits: scale = amax / 127, q = rint(x * (127 / amax)), ties to even; amax by its bits, so that NaN is more than any
+// number.  A row with an infinity or a NaN has scale NaN and q = 0: whatever is multiplied with it is NaN.  127 / amax leaves fp32
+// where amax is below 2^-121: such rows are taken times 2^64, which is exact.
+struct RowScale {
+  float scale, r;
+  bool small, bad;
+  __device__ __forceinline__ explicit RowScale(uint32_t amax_bits) {
+    const float amax = __uint_as_float(amax_bits);
+    bad = amax_bits >= 0x7f800000u;
+    small = amax < 0x1p-64f;
+    const float a = small ? amax * 0x1p64f : amax;
+    r = a > 0.0f ? 127.0f / a : 0.0f;
+    scale = bad ? __uint_as_float(0x7fc00000u) : amax / 127.0f;
+  }
+  __device__ __forceinline__ uint32_t q(float x) const {
+    const int v = bad ? 0 : __float2int_rn((small ? x * 0x1p64f : x) * r);
+    return uint32_t(v) & 255u;
+  }
+  __device__ __forceinline__ uint2 q8(const float (&f)[8]) const {
+    return make_uint2(q(f[0]) | q(f[1]) << 8 | q(f[2]) << 16 | q(f[3]) << 24, q(f[4]) | q(f[5]) << 8 | q(f[6]) << 16 | q(f[7]) << 24);
+  }
+};
+
+// Threads of a team for rows of `pieces` pieces, pieces a thread (1, 2 or 4; 0: too long for registers), teams of a workgroup.
+struct RowTeams {
+  int tr, np, teams;
+  explicit RowTeams(int pieces) {
+    np = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 0;
+    tr = np ? cdiv(cdiv(pieces, np), 64) * 64 : 512;
+    teams = tr >= 256 ? 1 : 256 / tr;
+  }
+};
+
+// Rows of `n_cols` activations in 8 bits, see semmoe_quantize_rows.  row_range (device, nullable): only the rows from row_range[0] up
+// to row_range[n_range] exist, n_rows is then the most there can be.
+int32_t launch_quantize_rows(bool bf16, const void* X, int64_t ldx, int n_rows, int n_cols, const int32_t* row_range, int n_range,
+                             void* Xq, float* x_scale, hipStream_t stream);
+
+}  // namespace semmoe
