@@ -377,8 +377,8 @@ static int32_t launch_w4_128(const GemmArgs& a, int max_rows, hipStream_t stream
 // tile shapes: id -> (waves along weight rows, waves along tokens, MFMA tiles per wave, K slice)
 template <int MODE>
 static int32_t launch_bf16_tile(int id, const GemmArgs& a, int max_rows, int bpc, hipStream_t s) {
-  switch (id) {
-    case 0: return launch_bf16<MODE, 2, 2, 2, 2, 64>(a, max_rows, bpc > 0 ? bpc : 2, s);  // 128 x 128, 4 waves
+  // shapes that the rule does not pick, for sweeps: not built for 8-bit operands
+  if constexpr (!kI8<MODE>) switch (id) {
     case 3: return launch_bf16<MODE, 2, 4, 4, 2, 64>(a, max_rows, bpc > 0 ? bpc : 1, s);  // 256 x 256, 8 waves
     case 4: return launch_bf16<MODE, 4, 2, 2, 4, 64>(a, max_rows, bpc > 0 ? bpc : 1, s);  // 256 x 256, 8 waves
     case 6: return launch_bf16<MODE, 2, 4, 2, 2, 64>(a, max_rows, bpc > 0 ? bpc : 1, s);  // 128 x 256, 8 waves
@@ -386,13 +386,17 @@ static int32_t launch_bf16_tile(int id, const GemmArgs& a, int max_rows, int bpc
     case 12: return launch_dma<MODE, 4, 2, 2, 4, 32, 4>(a, max_rows, bpc > 0 ? bpc : 1, s);     // 256 x 256, 8 waves
     case 14: return launch_dma<MODE, 2, 4, 2, 2, 32, 4>(a, max_rows, bpc > 0 ? bpc : 1, s);     // 128 x 256, 8 waves
     case 15: return launch_dma<MODE, 2, 4, 4, 2, 32, 3>(a, max_rows, bpc > 0 ? bpc : 1, s);     // 256 x 256, ring of 3
-    case 16: return launch_dma<MODE, 2, 4, 4, 2, 64, 2>(a, max_rows, bpc > 0 ? bpc : 1, s);     // 256 x 256, K 64 x 2
     case 17: return launch_bf16<MODE, 4, 1, 2, 1, 64>(a, max_rows, bpc > 0 ? bpc : 2, s);       // 256 x 32 (decode)
     case 18: return launch_bf16<MODE, 4, 1, 2, 2, 64>(a, max_rows, bpc > 0 ? bpc : 2, s);       // 256 x 64
     case 19: return launch_dma<MODE, 4, 1, 2, 1, 64, 4>(a, max_rows, bpc > 0 ? bpc : 1, s);     // 256 x 32, ring of 4 (decode)
     case 25: return launch_dma<MODE, 4, 1, 2, 2, 64, 3>(a, max_rows, bpc > 0 ? bpc : 1, s);     // 256 x 64, ring of 3
-    case 26: return launch_dma<MODE, 2, 2, 2, 1, 64, 3>(a, max_rows, bpc > 0 ? bpc : 2, s);     // 128 x 64, ring of 3, two per CU
     case 27: return launch_dma<MODE, 2, 2, 2, 1, 64, 4>(a, max_rows, bpc > 0 ? bpc : 1, s);     // 128 x 64, ring of 4
+    default: break;
+  }
+  switch (id) {
+    case 0: return launch_bf16<MODE, 2, 2, 2, 2, 64>(a, max_rows, bpc > 0 ? bpc : 2, s);  // 128 x 128, 4 waves
+    case 16: return launch_dma<MODE, 2, 4, 4, 2, 64, 2>(a, max_rows, bpc > 0 ? bpc : 1, s);     // 256 x 256, K 64 x 2
+    case 26: return launch_dma<MODE, 2, 2, 2, 1, 64, 3>(a, max_rows, bpc > 0 ? bpc : 2, s);     // 128 x 64, ring of 3, two per CU
     // weights streamed through registers: 16 x TW weight rows, 16 x TT tokens
     case 30: case 31: case 32: {
       const int32_t st = id == 30   ? launch_stream<MODE, false, 2, 2>(a, max_rows, bpc > 0 ? bpc : 2, s)
@@ -429,10 +433,10 @@ static int32_t launch_bf16_tile(int id, const GemmArgs& a, int max_rows, int bpc
     default: break;
   }
   if (id >= 20 && id <= 22) {  // four waves, 256 x 256, loads interleaved with the MFMAs
-    int32_t st;
-    switch (id) {
-      case 20: st = launch_w4<MODE, 32, 4, 4>(a, max_rows, s); break;  // K slices of 32, ring of 4, a load every 4th MFMA
-      case 21: st = launch_w4<MODE, 32, 4, 2>(a, max_rows, s); break;  // ... every 2nd MFMA
+    int32_t st = SEMMOE_EUNSUPPORTED;
+    switch (kI8<MODE> ? 22 : id) {
+      case 20: if constexpr (!kI8<MODE>) st = launch_w4<MODE, 32, 4, 4>(a, max_rows, s); break;  // K slices of 32, ring of 4, a load every 4th MFMA
+      case 21: if constexpr (!kI8<MODE>) st = launch_w4<MODE, 32, 4, 2>(a, max_rows, s); break;  // ... every 2nd MFMA
       default: st = launch_w4<MODE, 64, 2, 2>(a, max_rows, s); break;  // K slices of 64, ring of 2 (the fastest measured)
     }
     if (st != SEMMOE_EUNSUPPORTED) return st;
@@ -570,7 +574,9 @@ static bool split_launch(int id) {
 template <int MODE>
 static int32_t launch_by_rule(const GemmArgs& a, int max_rows, int est_rows_per_group, int bpc, hipStream_t stream) {
   const int knob = tuning_value(kPaired<MODE> ? SEMMOE_TUNE_GATEUP_TILE : SEMMOE_TUNE_DOWN_TILE);
-  const int id = knob >= 0 ? knob : default_tile(a, max_rows, est_rows_per_group, kPaired<MODE> ? 2 * a.N : a.N);
+  const bool known = !kI8<MODE> || knob == 0 || knob == 16 || knob == 22 || knob == 26 || knob == 28 || (knob >= 30 && knob <= 35) ||
+                     (knob >= 38 && knob <= 40);  // 8-bit operands: the shapes that are built for them
+  const int id = knob >= 0 && known ? knob : default_tile(a, max_rows, est_rows_per_group, kPaired<MODE> ? 2 * a.N : a.N);
   if (!split_launch(id)) return launch_bf16_tile<MODE>(id, a, max_rows, bpc, stream);
   GemmArgs h = a;
   h.sched_mode = 1;

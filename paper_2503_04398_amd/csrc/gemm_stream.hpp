@@ -51,9 +51,12 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t stream_rsrc(const unsigned cha
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(scalar_ptr(base)), 0, -1, 0x00027000);
 }
 
-template <bool F32>
+template <int MODE, bool F32>
 __device__ __forceinline__ f32x4_t stream_mfma(u32x4_t w, u32x4_t x, f32x4_t c) {
-  if constexpr (F32) {
+  if constexpr (kI8<MODE>) {
+    return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, w), __builtin_bit_cast(i32x4_t, x),
+                                                                             __builtin_bit_cast(i32x4_t, c), 0, 0, 0));
+  } else if constexpr (F32) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[j]), __uint_as_float(x[j]), c, 0, 0, 0);
@@ -212,7 +215,11 @@ __device__ __forceinline__ void gemm_stream_body(const GemmArgs& a, unsigned cha
     auto total_of = [&](int i, int j) __attribute__((always_inline)) {
       f32x4_t v = red[(i * TT + j) * 64 + lane];
 #pragma unroll
-      for (int w = 1; w < NW; ++w) v += red[((w * TW + i) * TT + j) * 64 + lane];
+      for (int w = 1; w < NW; ++w) {
+        const f32x4_t o = red[((w * TW + i) * TT + j) * 64 + lane];
+        if constexpr (kI8<MODE>) v = __builtin_bit_cast(f32x4_t, __builtin_bit_cast(i32x4_t, v) + __builtin_bit_cast(i32x4_t, o));
+        else v += o;
+      }
       return v;
     };
     constexpr int FT = kPaired<MODE> ? TW / 2 : TW;  // 16-feature tiles of the output
@@ -231,6 +238,20 @@ __device__ __forceinline__ void gemm_stream_body(const GemmArgs& a, unsigned cha
           swiglu_grad<F32>(dh[e], gt[e], up[e], &dg, &du);
           v[e] = dg;
           v2[e] = du;
+        }
+      } else if constexpr (kI8<MODE>) {
+        const float xs = a.x_scale[r.row_lo + min(tok, r.n_tok - 1)];
+        const float* const ws = a.w_scale + size_t(r.widx) * (kPaired<MODE> ? 2 * a.N : a.N) + min(feat, a.N - 4);
+        const f32x4_t s0 = *reinterpret_cast<const f32x4_t*>(ws);
+        if constexpr (kPaired<MODE>) {
+          const f32x4_t s1 = *reinterpret_cast<const f32x4_t*>(ws + a.N);
+          const f32x4_t gt = total_of(2 * p, j), up = total_of(2 * p + 1, j);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = silu_mul(scaled_sum(gt[e], xs, s0[e]), scaled_sum(up[e], xs, s1[e]));
+        } else {
+          const f32x4_t sum = total_of(p, j);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = scaled_sum(sum[e], xs, s0[e]);
         }
       } else if constexpr (MODE == kModeSwiglu) {
         const f32x4_t gt = total_of(2 * p, j), up = total_of(2 * p + 1, j);
@@ -259,7 +280,7 @@ __device__ __forceinline__ void gemm_stream_body(const GemmArgs& a, unsigned cha
           *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + row * a.ldo + a.N + feat) = v2;
       } else {
         *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + row * a.ldo + feat) =
-            make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+            make_uint2(pack_out<MODE>(v[0], v[1]), pack_out<MODE>(v[2], v[3]));
         if constexpr (MODE == kModeSwigluGrad)
           *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + row * a.ldo + a.N + feat) =
               make_uint2(pack_bf16x2(v2[0], v2[1]), pack_bf16x2(v2[2], v2[3]));
@@ -305,7 +326,7 @@ __device__ __forceinline__ void gemm_stream_body(const GemmArgs& a, unsigned cha
         if (j == 0 || j < ntt) {  // the first without a test: its MFMAs then wait for one fragment at a time
           const u32x4_t xf = *reinterpret_cast<const u32x4_t*>(from + (TW + j) * 2048);
 #pragma unroll
-          for (int i = 0; i < TW; ++i) acc[i][j] = stream_mfma<F32>(wf[i], xf, acc[i][j]);
+          for (int i = 0; i < TW; ++i) acc[i][j] = stream_mfma<MODE, F32>(wf[i], xf, acc[i][j]);
         }
     }
     __builtin_amdgcn_sched_barrier(0);

@@ -326,7 +326,7 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
         for (int j = 0; j < TJ; ++j) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[cur][i], bfr[cur][j], acc[i][j], 0, 0, 0);
+            acc[i][j] = tile_mfma<MODE>(af[cur][i], bfr[cur][j], acc[i][j]);
             {
               const int p = j * 4 + i;  // constant after unrolling
               if (p < 4)
@@ -412,9 +412,12 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
         dh[g4] = *reinterpret_cast<const f32x4_t*>(a.b_g + quad_at(a.N, row, min(col + g4 * 8, a.N - 4)));
     };
     if constexpr (MODE == kModeSwigluGrad) fetch_dh(0, 0);
+    const float* const w_scale = kI8<MODE> ? a.w_scale + size_t(t.widx) * (kPaired<MODE> ? 2 * a.N : a.N) : nullptr;
 #pragma unroll
     for (int j = 0; j < TJ; ++j) {
       if (j >= nj) break;
+      float x_scale = 0.0f;
+      if constexpr (kI8<MODE>) x_scale = a.x_scale[t.row_lo + min((j * 2 + wt) * 32 + tok_in, t.n_tok - 1)];
 #pragma unroll
       for (int h = 0; h < kPasses; ++h) {
         // One pass at a time.  The accumulators of the pass are pinned to the accumulation registers up to
@@ -460,6 +463,24 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
               uint2 v;
               if constexpr (MODE == kModeSwigluGrad) {
                 v = dgu[part][b][g4];
+              } else if constexpr (kI8<MODE>) {
+                // a lane's four features of a token are 16 bytes of the weights' scales
+                int col = t.f0 + (kPaired<MODE> ? wf * 64 : wf * 128) + (h * NB + b) * 32 + g4 * 8 + half * 4;
+                asm volatile("" : "+v"(col));  // addresses kept from pass to pass would be spilled
+                col = min(col, a.N - 4);
+                const f32x4_t s0 = *reinterpret_cast<const f32x4_t*>(w_scale + col);
+                float y[4];
+                if constexpr (kPaired<MODE>) {
+                  const f32x4_t s1 = *reinterpret_cast<const f32x4_t*>(w_scale + a.N + col);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e)
+                    y[e] = silu_mul_fast(scaled_sum(acc[2 * (NB * h + b)][j][g4 * 4 + e], x_scale, s0[e]),
+                                         scaled_sum(acc[2 * (NB * h + b) + 1][j][g4 * 4 + e], x_scale, s1[e]));
+                } else {
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) y[e] = scaled_sum(acc[NB * h + b][j][g4 * 4 + e], x_scale, s0[e]);
+                }
+                v = make_uint2(cvt_pk_bf16(y[0], y[1]), cvt_pk_bf16(y[2], y[3]));
               } else if constexpr (MODE == kModeSwiglu) {
                 const f32x16_t& g = acc[2 * (NB * h + b)][j];
                 const f32x16_t& u = acc[2 * (NB * h + b) + 1][j];
@@ -660,7 +681,7 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
         for (int j = 0; j < TT; ++j) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[cur][i], bfr[cur][j], acc[i][j], 0, 0, 0);
+            acc[i][j] = tile_mfma<MODE>(af[cur][i], bfr[cur][j], acc[i][j]);
             {
               // the 2 + TT fragment reads of the next k-step, spread over this k-step's 2 * TT MFMAs
               const int p = j * 2 + i;  // constant after unrolling
