@@ -236,6 +236,7 @@ class SemMoE:
         self.ws_shared = None
         self._mine = _OfThread()
         self._adapter_calls = {}  # config, shape and workspace bytes of the adapter calls seen, by their shapes
+        self._norm_calls = {}  # the same of the calls on the norms
         self._c_config = None  # (values, C struct of them)
         if allocate_workspace:
             import torch
@@ -780,10 +781,11 @@ class SemMoE:
             _ptr(w_scale_down_sh), _ptr(Y_shared), ws, size))
 
     # -- the norms around a block
-    def _norm_call(self, call, T, d, res_scale, eps_post, eps_pre, gate, vectors, rows):
-        """(config, shape): vectors are w_post and w_pre with the gradients of such, rows the tensors [T,d] by the name of their
-        distance.  A gate of one dimension is all rows' (its gradient then is one row, too)."""
-        s = _CNormShape(res_scale, eps_post, eps_pre, int(gate is not None and gate.dim() == 2))
+    def _norm_call(self, call, T, d, par, gate, vectors, rows):
+        """(config, shape) of a call on the norms: made and checked once for shapes, distances of rows and par (res_scale, eps_post,
+        eps_pre), which every layer of a step repeats.  vectors are w_post and w_pre with the gradients of such; rows the tensors [T,d]
+        by the name of their distance.  A gate of one dimension is all rows' (its gradient then is one row, too)."""
+        s = _CNormShape(*par, int(gate is not None and gate.dim() == 2))
         for t in vectors:
             if t is not None and tuple(t.shape) != (d,):
                 raise SemMoEError("%s: a norm's weights and a gate of all rows have %d numbers" % (call, d), -2)
@@ -794,52 +796,87 @@ class SemMoE:
                 setattr(s, name, _row_distance(t, d, name))
         return (self._cfg() if (self.cfg.T, self.cfg.d) == (T, d) else self._cfg(T=T, d=d)), s
 
+    def _kept_norm_call(self, key, make):
+        kept = self._norm_calls.get(key)
+        if kept is None:
+            if len(self._norm_calls) >= 256:
+                self._norm_calls.clear()
+            self._norm_calls[key] = kept = make()
+        return kept
+
     def block_norm(self, R, H, Y=None, X=None, Xq=None, x_scale=None, w_post=None, w_pre=None, gate=None, res_scale=1.0,
                    eps_post=1e-6, eps_pre=1e-6):
         """H = res_scale R + gate norm(Y) w_post, X = norm(H) w_pre, and X in 8 bits as Xq and x_scale; what is None is left out.
         gate: [d] or [T,d].  H and X may lie in the place of R or Y."""
         T, d = (Y if R is None else R).shape
-        of_all = gate is not None and gate.dim() == 1
-        c, s = self._norm_call("block_norm", T, d, res_scale, eps_post, eps_pre, gate, (w_post, w_pre, gate if of_all else None), (
-            ("ld_r", R), ("ld_y", Y), ("ld_h", H), ("ld_x", X), ("ld_gate", None if of_all else gate)))
-        if H is not None and X is not None and T and H.data_ptr() == X.data_ptr():
-            raise SemMoEError("block_norm: H and X lie in the same place", -1)
-        torch = self._torch
-        self._fit("block_norm", ((R, None, 0), (Y, None, 0), (w_post, None, d), (gate, None, 0), (w_pre, None, d), (H, None, 0),
-                                 (X, None, 0), (Xq, torch.int8, T * d), (x_scale, torch.float32, T)))
+        tensors = (R, Y, w_post, gate, w_pre, H, X)
+        par = (res_scale, eps_post, eps_pre)
+        key = (_config_values(self.cfg), par, *[None if t is None else (t.shape, t.stride()) for t in tensors])
+
+        def make():
+            of_all = gate is not None and gate.dim() == 1
+            return self._norm_call("block_norm", T, d, par, gate, (w_post, w_pre, gate if of_all else None), (
+                ("ld_r", R), ("ld_y", Y), ("ld_h", H), ("ld_x", X), ("ld_gate", None if of_all else gate)))
+
+        c, s = self._kept_norm_call(key, make)
+        here, _, f32, acts = self._types
+        dev, act, i8 = (Y if R is None else R).get_device(), acts[self.cfg.dtype == BF16], self._torch.int8
+        if dev < 0 or dev != here():
+            self._fit("block_norm", ((Y if R is None else R, None, 0),))
+        for t in tensors:
+            if t is not None and (t.dtype is not act or t.get_device() != dev):
+                self._fit("block_norm", ((t, None, 0),))
+        if not (Xq is None is x_scale) and not (
+                Xq is not None and x_scale is not None and i8 is Xq.dtype and f32 is x_scale.dtype
+                and dev == Xq.get_device() == x_scale.get_device() and Xq.numel() >= T * d and x_scale.numel() >= T):
+            self._fit("block_norm", ((Xq, i8, T * d), (x_scale, f32, T)))
         if T == 0:
             return
+        R, Y, w_post, gate, w_pre, H, X = [None if t is None else t.data_ptr() for t in tensors]
+        if H == X is not None:
+            raise SemMoEError("block_norm: H and X lie in the same place", -1)
         self._check("semmoe_block_norm", self.lib.semmoe_block_norm(
-            C.byref(c), _stream(), C.byref(s), *(None if t is None else t.data_ptr() for t in (R, Y, w_post, gate, w_pre, H, X)),
-            _ptr(Xq), _ptr(x_scale)))
+            C.byref(c), _stream(), C.byref(s), R, Y, w_post, gate, w_pre, H, X, _ptr(Xq), _ptr(x_scale)))
 
     def block_norm_grad(self, H, dR, Y=None, dH=None, dX=None, w_post=None, w_pre=None, gate=None, dY=None, dgate=None, dw_post=None,
                         dw_pre=None, res_scale=1.0, eps_post=1e-6, eps_pre=1e-6):
         """each of dR, dY, dgate, dw_post and dw_pre may be None; dH or dX may, and H without dX.  dR, dY and a dgate of rows may lie in
         the place of one of dH, dX, H and Y, not in each other's."""
         T, d = (dX if dH is None else dH).shape
+        tensors = (dH, dX, H, Y, w_post, gate, w_pre, dR, dY, dgate, dw_post, dw_pre)
+        par = (res_scale, eps_post, eps_pre)
+        key = (_config_values(self.cfg), par, *[None if t is None else (t.shape, t.stride()) for t in tensors])
         of_all = gate is not None and gate.dim() == 1
-        if dgate is not None and (gate is None or dgate.shape != gate.shape):
-            raise SemMoEError("block_norm_grad: dgate has gate's shape", -2)
-        c, s = self._norm_call("block_norm_grad", T, d, res_scale, eps_post, eps_pre, gate,
-                               (w_post, w_pre, dw_post, dw_pre, gate if of_all else None), (
-            ("ld_dh", dH), ("ld_dx", dX), ("ld_h", H), ("ld_y", Y), ("ld_dr", dR), ("ld_dy", dY),
-            ("ld_gate", None if of_all else gate), ("ld_dgate", None if of_all else dgate)))
-        outs = [t.data_ptr() for t in (dR, dY, dgate, dw_post, dw_pre) if t is not None and t.numel()]
-        if len(set(outs)) != len(outs):
-            raise SemMoEError("block_norm_grad: two results lie in the same place", -1)
-        self._fit("block_norm_grad", tuple((t, None, 0) for t in (dH, dX, H, Y, w_post, gate, w_pre, dR, dY, dgate, dw_post, dw_pre)))
+
+        def make():
+            if dgate is not None and (gate is None or dgate.shape != gate.shape):
+                raise SemMoEError("block_norm_grad: dgate has gate's shape", -2)
+            c, s = self._norm_call("block_norm_grad", T, d, par, gate, (w_post, w_pre, dw_post, dw_pre, gate if of_all else None), (
+                ("ld_dh", dH), ("ld_dx", dX), ("ld_h", H), ("ld_y", Y), ("ld_dr", dR), ("ld_dy", dY),
+                ("ld_gate", None if of_all else gate), ("ld_dgate", None if of_all else dgate)))
+            need = C.c_size_t(0)
+            self._check("semmoe_block_norm_grad_workspace_bytes",
+                        self.lib.semmoe_block_norm_grad_workspace_bytes(C.byref(c), C.byref(need)))
+            return c, s, int(need.value)
+
+        c, s, need = self._kept_norm_call(key, make)
+        dev, act = (dX if dH is None else dH).get_device(), self._types[3][self.cfg.dtype == BF16]
+        if dev < 0 or dev != self._types[0]():
+            self._fit("block_norm_grad", ((dX if dH is None else dH, None, 0),))
+        for t in tensors:
+            if t is not None and (t.dtype is not act or t.get_device() != dev):
+                self._fit("block_norm_grad", ((t, None, 0),))
         if T == 0:
             for t in (dgate, dw_post, dw_pre):
                 if t is not None:
                     t.zero_()
             return
+        at = [None if t is None else t.data_ptr() for t in tensors]
+        outs = [p for p in at[7:] if p is not None]
+        if len(set(outs)) != len(outs):
+            raise SemMoEError("block_norm_grad: two results lie in the same place", -1)
         ws, n, owner = None, 0, None
         if dw_post is not None or dw_pre is not None or (of_all and dgate is not None):
-            need = C.c_size_t(0)
-            self._check("semmoe_block_norm_grad_workspace_bytes",
-                        self.lib.semmoe_block_norm_grad_workspace_bytes(C.byref(c), C.byref(need)))
-            ws, n, owner = self._workspace("block_norm_grad", need.value)
+            ws, n, owner = self._workspace("block_norm_grad", need)
         self._check("semmoe_block_norm_grad", self.lib.semmoe_block_norm_grad(
-            C.byref(c), _stream(), C.byref(s),
-            *(None if t is None else t.data_ptr() for t in (dH, dX, H, Y, w_post, gate, w_pre, dR, dY, dgate, dw_post, dw_pre)), ws, n))
+            C.byref(c), _stream(), C.byref(s), *at, ws, n))

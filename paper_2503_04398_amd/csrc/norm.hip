@@ -28,20 +28,22 @@ struct NormArgs {
 __device__ __forceinline__ float add_f(float a, float b) { return a + b; }
 
 template <bool BF16, int NP>
-__global__ __launch_bounds__(512) void block_norm_kernel(const NormArgs a) {
-  __shared__ float part[2][8];
-  __shared__ uint32_t part_m[8];
-  const int teams = blockDim.x / a.tr, team = threadIdx.x / a.tr, t = threadIdx.x % a.tr, pieces = a.d / 8, tw = a.tr >> 6;
+__global__ __launch_bounds__(1024) void block_norm_kernel(const NormArgs a) {
+  using E = Piece<BF16>;
+  constexpr int N = E::N;
+  __shared__ float part[2][16];
+  __shared__ uint32_t part_m[16];
+  const int teams = blockDim.x / a.tr, team = threadIdx.x / a.tr, t = threadIdx.x % a.tr, pieces = a.d / N, tw = a.tr >> 6;
   const int row = blockIdx.x * teams + team;
   const bool have = row < a.n_rows;
   const size_t rw = have ? row : 0;
-  Eight<BF16> r[NP], y[NP], wp[NP], g[NP], wq[NP];
+  E r[NP], y[NP], wp[NP], g[NP], wq[NP];
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     const int c = t + p * a.tr;
     const bool in = c < pieces && have;
-    const size_t at = size_t(c) * 8;
-    auto get = [&](Eight<BF16>& e, const void* base, size_t off) __attribute__((always_inline)) {
+    const size_t at = size_t(c) * N;
+    auto get = [&](E& e, const void* base, size_t off) __attribute__((always_inline)) {
       if (in && base) e.load(base, off + at);
       else e.zero();
     };
@@ -58,15 +60,15 @@ __global__ __launch_bounds__(512) void block_norm_kernel(const NormArgs a) {
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int x = 0; x < 8; ++x) s[0] = fmaf(y[p][x], y[p][x], s[0]);
+      for (int x = 0; x < N; ++x) s[0] = fmaf(y[p][x], y[p][x], s[0]);
     team_join(s, part[0], tw, add_f);
     ry = 1.0f / sqrtf(s[0] * inv_d + a.eps_post);
   }
-  float h[NP][8];
+  float h[NP][N];
 #pragma unroll
   for (int p = 0; p < NP; ++p)
 #pragma unroll
-    for (int x = 0; x < 8; ++x) {
+    for (int x = 0; x < N; ++x) {
       float n = y[p][x];
       if (a.w_post) n = n * ry * wp[p][x];
       if (a.gate) n *= g[p][x];
@@ -76,9 +78,9 @@ __global__ __launch_bounds__(512) void block_norm_kernel(const NormArgs a) {
 #pragma unroll
     for (int p = 0; p < NP; ++p)
       if (have && t + p * a.tr < pieces) {
-        Eight<BF16> e;
+        E e;
         e.round(h[p]);
-        e.store(a.H, rw * a.ld_h + size_t(t + p * a.tr) * 8);
+        e.store(a.H, rw * a.ld_h + size_t(t + p * a.tr) * N);
       }
   }
   if (!a.w_pre) return;
@@ -86,20 +88,20 @@ __global__ __launch_bounds__(512) void block_norm_kernel(const NormArgs a) {
 #pragma unroll
   for (int p = 0; p < NP; ++p)
 #pragma unroll
-    for (int x = 0; x < 8; ++x) s[0] = fmaf(h[p][x], h[p][x], s[0]);
+    for (int x = 0; x < N; ++x) s[0] = fmaf(h[p][x], h[p][x], s[0]);
   team_join(s, part[1], tw, add_f);
   const float rh = 1.0f / sqrtf(s[0] * inv_d + a.eps_pre);
 #pragma unroll
   for (int p = 0; p < NP; ++p)
 #pragma unroll
-    for (int x = 0; x < 8; ++x) h[p][x] = h[p][x] * rh * wq[p][x];
+    for (int x = 0; x < N; ++x) h[p][x] = h[p][x] * rh * wq[p][x];
   if (a.X) {
 #pragma unroll
     for (int p = 0; p < NP; ++p)
       if (have && t + p * a.tr < pieces) {
-        Eight<BF16> e;
+        E e;
         e.round(h[p]);
-        e.store(a.X, rw * a.ld_x + size_t(t + p * a.tr) * 8);
+        e.store(a.X, rw * a.ld_x + size_t(t + p * a.tr) * N);
       }
   }
   if (!a.Xq) return;
@@ -108,27 +110,31 @@ __global__ __launch_bounds__(512) void block_norm_kernel(const NormArgs a) {
 #pragma unroll
   for (int p = 0; p < NP; ++p)
 #pragma unroll
-    for (int x = 0; x < 8; ++x) m[0] = max(m[0], magnitude_bits(h[p][x]));
+    for (int x = 0; x < N; ++x) m[0] = max(m[0], magnitude_bits(h[p][x]));
   team_join(m, part_m, tw, [](uint32_t u, uint32_t v) { return max(u, v); });
   const RowScale q(m[0]);
 #pragma unroll
   for (int p = 0; p < NP; ++p)
     if (have && t + p * a.tr < pieces)
-      *reinterpret_cast<uint2*>(a.Xq + rw * a.d + size_t(t + p * a.tr) * 8) = q.q8(h[p]);
+      q.put(a.Xq + rw * a.d + size_t(t + p * a.tr) * N, h[p]);
   if (have && t == 0) a.x_scale[row] = q.scale;
 }
 
 constexpr int kNormGradGroups = 512;  // workgroups of the backward pass at most: the rows of partial sums
 
-template <bool BF16, int NP>
-__global__ __launch_bounds__(512) void block_norm_grad_kernel(const NormArgs a) {
+// NP 1: the rows that come next are requested before this one's sums are joined; with NP 2 there are no registers for that.  GATES: a
+// gate for each row.
+template <bool BF16, int NP, bool GATES>
+__global__ __launch_bounds__(1024, 4) void block_norm_grad_kernel(const NormArgs a) {
+  using E = Piece<BF16>;
+  constexpr int N = E::N;
   extern __shared__ float lds[];
-  float* part = lds;  // [2][3][8 waves]
-  const int teams = blockDim.x / a.tr, team = threadIdx.x / a.tr, t = threadIdx.x % a.tr, pieces = a.d / 8, tw = a.tr >> 6;
+  float* part = lds;  // [3][16 waves], then [16 waves]
+  const int teams = blockDim.x / a.tr, team = threadIdx.x / a.tr, t = threadIdx.x % a.tr, pieces = a.d / N, tw = a.tr >> 6;
   const float inv_d = 1.0f / float(a.d);
-  const bool gate_of_all = a.gate && a.ld_gate == 0;
-  Eight<BF16> wp[NP], wq[NP], g[NP];
-  float sp[NP][8], sq[NP][8], sg[NP][8];  // dw_post, dw_pre, dgate of this thread's columns
+  constexpr bool AHEAD = NP == 1;
+  E wp[NP], wq[NP], g[NP];
+  float sp[NP][N], sq[NP][N], sg[GATES ? 1 : NP][N];  // dw_post, dw_pre, dgate of this thread's columns
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     const int c = t + p * a.tr;
@@ -136,91 +142,130 @@ __global__ __launch_bounds__(512) void block_norm_grad_kernel(const NormArgs a) 
     wq[p].zero();
     g[p].zero();
     if (c < pieces) {
-      if (a.w_post) wp[p].load(a.w_post, size_t(c) * 8);
-      if (a.w_pre) wq[p].load(a.w_pre, size_t(c) * 8);
-      if (gate_of_all) g[p].load(a.gate, size_t(c) * 8);
+      if (a.w_post) wp[p].load(a.w_post, size_t(c) * N);
+      if (a.w_pre) wq[p].load(a.w_pre, size_t(c) * N);
+      if (!GATES && a.gate) g[p].load(a.gate, size_t(c) * N);
     }
 #pragma unroll
-    for (int x = 0; x < 8; ++x) sp[p][x] = sq[p][x] = sg[p][x] = 0.0f;
+    for (int x = 0; x < N; ++x) {
+      sp[p][x] = sq[p][x] = 0.0f;
+      if constexpr (!GATES) sg[p][x] = 0.0f;
+    }
   }
+  struct Row {
+    E h[NP], x[NP], d[NP], y[NP], g[GATES ? NP : 1];
+  };
+  auto fetch = [&](Row& v, int row0) __attribute__((always_inline)) {
+    const int row = row0 + team;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int c = t + p * a.tr;
+      const bool in = row < a.n_rows && c < pieces;
+      const size_t at = size_t(c) * N, rw = row;
+      auto get = [&](E& e, const void* base, int64_t ld) __attribute__((always_inline)) {
+        if (in && base) e.load(base, rw * ld + at);
+        else e.zero();
+      };
+      get(v.x[p], a.dX, a.ld_dx);
+      get(v.h[p], a.dX ? a.H : nullptr, a.ld_h);
+      get(v.d[p], a.dH, a.ld_dh);
+      get(v.y[p], a.Y, a.ld_y);
+      if constexpr (GATES) get(v.g[p], a.gate, a.ld_gate);
+    }
+  };
+  Row next;
+  if constexpr (AHEAD) fetch(next, blockIdx.x * teams);
   for (int row0 = blockIdx.x * teams; row0 < a.n_rows; row0 += gridDim.x * teams) {
     const int row = row0 + team;
     const bool have = row < a.n_rows;
     const size_t rw = have ? row : row0;
-    Eight<BF16> vh[NP], vx[NP], vd[NP], vy[NP];
+    Row v;
+    if constexpr (AHEAD) {
+      v = next;
+      fetch(next, row0 + gridDim.x * teams);
+    } else {
+      fetch(v, row0);
+    }
+    if constexpr (GATES)
+#pragma unroll
+      for (int p = 0; p < NP; ++p) g[p] = v.g[p];
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      const int c = t + p * a.tr;
-      const bool in = have && c < pieces;
-      const size_t at = size_t(c) * 8;
-      auto get = [&](Eight<BF16>& e, const void* base, size_t off) __attribute__((always_inline)) {
-        if (in && base) e.load(base, off + at);
-        else e.zero();
-      };
-      get(vx[p], a.dX, rw * a.ld_dx);
-      get(vh[p], a.dX ? a.H : nullptr, rw * a.ld_h);
-      get(vd[p], a.dH, rw * a.ld_dh);
-      get(vy[p], a.Y, rw * a.ld_y);
-      if (a.gate && !gate_of_all) get(g[p], a.gate, rw * a.ld_gate);
+      wp[p].stay();
+      wq[p].stay();
+      g[p].stay();
     }
     // sums over the row: H^2, a H, Y^2
     float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        s[0] = fmaf(vh[p][x], vh[p][x], s[0]);
-        s[1] = fmaf(vx[p][x] * wq[p][x], vh[p][x], s[1]);
-        s[2] = fmaf(vy[p][x], vy[p][x], s[2]);
+      for (int x = 0; x < N; ++x) {
+        s[0] = fmaf(v.h[p][x], v.h[p][x], s[0]);
+        s[1] = fmaf(v.x[p][x] * wq[p][x], v.h[p][x], s[1]);
+        s[2] = fmaf(v.y[p][x], v.y[p][x], s[2]);
       }
     team_join(s, part, tw, add_f);
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      v.h[p].stay();
+      v.x[p].stay();
+      v.y[p].stay();
+      wq[p].stay();
+    }
     const float rh = 1.0f / sqrtf(s[0] * inv_d + a.eps_pre), ch = s[1] * rh * inv_d;
     const float ry = a.w_post ? 1.0f / sqrtf(s[2] * inv_d + a.eps_post) : 1.0f;
-    float dh[NP][8], e[1] = {0.0f};
+    float dh[NP][N], e[1] = {0.0f};
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        float v = vd[p][x];
+      for (int x = 0; x < N; ++x) {
+        float u = v.d[p][x];
         if (a.dX) {
-          const float xn = vh[p][x] * rh;
-          v += rh * (vx[p][x] * wq[p][x] - xn * ch);
-          sq[p][x] = fmaf(vx[p][x], xn, sq[p][x]);
+          const float xn = v.h[p][x] * rh;
+          u += rh * (v.x[p][x] * wq[p][x] - xn * ch);
+          sq[p][x] = fmaf(v.x[p][x], xn, sq[p][x]);
         }
-        dh[p][x] = v;
-        const float yn = vy[p][x] * ry, b = a.gate ? v * g[p][x] : v;
+        dh[p][x] = u;
+        const float yn = v.y[p][x] * ry, b = a.gate ? u * g[p][x] : u;
         if (a.w_post) {
           e[0] = fmaf(b * wp[p][x], yn, e[0]);
           sp[p][x] = fmaf(b, yn, sp[p][x]);
         }
-        if (gate_of_all) sg[p][x] = fmaf(v, a.w_post ? yn * wp[p][x] : yn, sg[p][x]);
+        if constexpr (!GATES) sg[p][x] = fmaf(u, a.w_post ? yn * wp[p][x] : yn, sg[p][x]);
       }
-    if (a.w_post) team_join(e, part + 24, tw, add_f);
+    if (a.w_post) team_join(e, part + 48, tw, add_f);
     else if (tw > 1) __syncthreads();  // `part` has been read
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      v.y[p].stay();
+      wp[p].stay();
+      g[p].stay();
+    }
     const float cy = e[0] * inv_d;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      const size_t at = size_t(t + p * a.tr) * 8;
+      const size_t at = size_t(t + p * a.tr) * N;
       if (!have || t + p * a.tr >= pieces) continue;
-      float f[8];
-      Eight<BF16> o;
+      float f[N];
+      E o;
       if (a.dR) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x) f[x] = a.res_scale * dh[p][x];
+        for (int x = 0; x < N; ++x) f[x] = a.res_scale * dh[p][x];
         o.round(f);
         o.store(a.dR, rw * a.ld_dr + at);
       }
-      if (a.dgate && !gate_of_all) {
+      if (GATES && a.dgate) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x) f[x] = dh[p][x] * (a.w_post ? vy[p][x] * ry * wp[p][x] : vy[p][x]);
+        for (int x = 0; x < N; ++x) f[x] = dh[p][x] * (a.w_post ? v.y[p][x] * ry * wp[p][x] : v.y[p][x]);
         o.round(f);
         o.store(a.dgate, rw * a.ld_dgate + at);
       }
       if (a.dY) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
+        for (int x = 0; x < N; ++x) {
           const float b = a.gate ? dh[p][x] * g[p][x] : dh[p][x];
-          f[x] = a.w_post ? ry * (b * wp[p][x] - vy[p][x] * ry * cy) : b;
+          f[x] = a.w_post ? ry * (b * wp[p][x] - v.y[p][x] * ry * cy) : b;
         }
         o.round(f);
         o.store(a.dY, rw * a.ld_dy + at);
@@ -231,50 +276,63 @@ __global__ __launch_bounds__(512) void block_norm_grad_kernel(const NormArgs a) 
   // the teams' sums meet in LDS, in the order of the teams
   float* meet = lds + 64;
 #pragma unroll
-  for (int which = 0; which < 3; ++which) {
+  for (int which = 0; which < (GATES ? 2 : 3); ++which) {
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const int c = t + p * a.tr;
-      float v[8];
+      float v[N];
 #pragma unroll
-      for (int x = 0; x < 8; ++x) v[x] = which == 0 ? sp[p][x] : which == 1 ? sq[p][x] : sg[p][x];
+      for (int x = 0; x < N; ++x) v[x] = which == 0 ? sp[p][x] : which == 1 ? sq[p][x] : sg[GATES ? 0 : p][x];
       if (teams > 1) {
         __syncthreads();
 #pragma unroll
-        for (int x = 0; x < 8; ++x) meet[(team * a.tr + t) * 8 + x] = v[x];
+        for (int x = 0; x < N; ++x) meet[(team * a.tr + t) * N + x] = v[x];
         __syncthreads();
         if (team == 0)
           for (int w = 1; w < teams; ++w)
 #pragma unroll
-            for (int x = 0; x < 8; ++x) v[x] += meet[(w * a.tr + t) * 8 + x];
+            for (int x = 0; x < N; ++x) v[x] += meet[(w * a.tr + t) * N + x];
       }
       if (team == 0 && c < pieces) {
-        Eight<false> o;
-        o.round(v);
-        o.store(a.sums, (size_t(which) * gridDim.x + blockIdx.x) * a.d + size_t(c) * 8);
+        float* const to = a.sums + (size_t(which) * gridDim.x + blockIdx.x) * a.d + size_t(c) * N;
+#pragma unroll
+        for (int x = 0; x < N; x += 4)
+          *reinterpret_cast<row_u32x4_t*>(to + x) = row_u32x4_t{__float_as_uint(v[x]), __float_as_uint(v[x + 1]),
+                                                                __float_as_uint(v[x + 2]), __float_as_uint(v[x + 3])};
       }
     }
   }
 }
 
-// Columns of the workgroups' sums: 64 columns and four runs of the rows a workgroup, the runs joined in order.
+// Columns of the workgroups' sums: 64 columns, four a thread, and 16 runs of the rows a workgroup, the runs joined in order.
 template <bool BF16>
 __global__ __launch_bounds__(256) void norm_sums_kernel(const float* __restrict__ sums, int groups, int d, void* dw_post, void* dw_pre,
                                                         void* dgate) {
-  __shared__ float part[4][64];
-  const int which = blockIdx.y, lane = threadIdx.x & 63, run = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+  typedef __attribute__((ext_vector_type(4))) float f4;
+  __shared__ f4 part[16][16];
+  const int which = blockIdx.y, quad = threadIdx.x & 15, run = threadIdx.x >> 4, col = blockIdx.x * 64 + quad * 4;
   void* const out = which == 0 ? dw_post : which == 1 ? dw_pre : dgate;
   if (!out) return;  // the whole workgroup
-  const int per = (groups + 3) / 4, lo = run * per, hi = min(lo + per, groups);
-  const float* from = sums + size_t(which) * groups * d + min(col, d - 1);
-  float s = 0.0f;
-  for (int r = lo; r < hi; ++r) s += from[size_t(r) * d];
-  part[run][lane] = s;
+  const f4* from = reinterpret_cast<const f4*>(sums + size_t(which) * groups * d + min(col, d - 4));
+  const int per = (groups + 15) / 16, lo = run * per, hi = min(lo + per, groups);
+  f4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int r = lo; r < hi; r += 8) {
+    f4 v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = r + u < hi ? from[size_t(r + u) * d / 4] : f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += v[u];
+  }
+  part[run][quad] = s;
   __syncthreads();
   if (run || col >= d) return;
-  s = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
-  if constexpr (BF16) static_cast<bf16_t*>(out)[col] = bf16_t(cvt_pk_bf16(s, 0.0f));
-  else static_cast<float*>(out)[col] = s;
+#pragma unroll
+  for (int w = 1; w < 16; ++w) s += part[w][quad];
+  if constexpr (BF16) {
+    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(out) + col) = make_uint2(cvt_pk_bf16(s[0], s[1]), cvt_pk_bf16(s[2], s[3]));
+  } else {
+    *reinterpret_cast<f4*>(static_cast<float*>(out) + col) = s;
+  }
 }
 
 static int32_t check_norm(const semmoe_config* cfg, const semmoe_norm_shape* n, std::initializer_list<int64_t> lds) {
@@ -291,8 +349,10 @@ static int32_t check_norm(const semmoe_config* cfg, const semmoe_norm_shape* n, 
   return SEMMOE_OK;
 }
 
+static RowTeams norm_grad_teams(const semmoe_config* cfg) { return RowTeams(cfg->dtype == SEMMOE_BF16, cfg->d, 1024); }
+
 static size_t norm_groups(const semmoe_config* cfg) {
-  const int rows = cdiv(cfg->T, RowTeams(cfg->d / 8).teams);
+  const int rows = cdiv(cfg->T, norm_grad_teams(cfg).teams);
   return rows < kNormGradGroups ? rows : kNormGradGroups;
 }
 
@@ -310,7 +370,8 @@ extern "C" int32_t semmoe_block_norm(const semmoe_config* cfg, void* stream, con
   for (const void* p : {R, Y, w_post, gate, w_pre, static_cast<const void*>(H), static_cast<const void*>(X), static_cast<const void*>(Xq)})
     if (!aligned16(p)) return SEMMOE_EINVAL;
   if (cfg->T == 0) return SEMMOE_OK;
-  const RowTeams g(cfg->d / 8);
+  const bool bf = cfg->dtype == SEMMOE_BF16;
+  const RowTeams g(bf, cfg->d, bf ? 512 : 1024);
   NormArgs a{};
   a.n_rows = cfg->T; a.d = cfg->d; a.tr = g.tr;
   a.res_scale = n->res_scale; a.eps_post = n->eps_post; a.eps_pre = n->eps_pre;
@@ -321,7 +382,7 @@ extern "C" int32_t semmoe_block_norm(const semmoe_config* cfg, void* stream, con
   a.ld_gate = n->gate_rows ? (n->ld_gate ? n->ld_gate : d) : 0;
   const dim3 grid(cdiv(cfg->T, g.teams)), block(g.tr * g.teams);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (cfg->dtype == SEMMOE_BF16) {
+  if (bf) {
     if (g.np == 1) hipLaunchKernelGGL((block_norm_kernel<true, 1>), grid, block, 0, s, a);
     else if (g.np == 2) hipLaunchKernelGGL((block_norm_kernel<true, 2>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((block_norm_kernel<true, 4>), grid, block, 0, s, a);
@@ -364,7 +425,7 @@ extern "C" int32_t semmoe_block_norm_grad(const semmoe_config* cfg, void* stream
     if (!c.ok) return SEMMOE_EWORKSPACE;
   }
   if (cfg->T == 0 && !columns) return SEMMOE_OK;
-  const RowTeams g(cfg->d / 8);
+  const RowTeams g = norm_grad_teams(cfg);
   NormArgs a{};
   a.n_rows = cfg->T; a.d = cfg->d; a.tr = g.tr;
   a.res_scale = n->res_scale; a.eps_post = n->eps_post; a.eps_pre = n->eps_pre;
@@ -379,16 +440,21 @@ extern "C" int32_t semmoe_block_norm_grad(const semmoe_config* cfg, void* stream
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (cfg->T > 0) {
     const dim3 grid(groups), block(g.tr * g.teams);
-    const size_t lds = 256 + (columns && g.teams > 1 ? size_t(g.tr) * g.teams * 32 : 0);
+    const size_t lds = 256 + (columns && g.teams > 1 ? size_t(g.tr) * g.teams * (bf ? 32 : 16) : 0);
+#define SEMMOE_NORM_GRAD(BF_, NP_)                                                                             \
+  do {                                                                                                         \
+    if (a.gate && n->gate_rows) hipLaunchKernelGGL((block_norm_grad_kernel<BF_, NP_, true>), grid, block, lds, s, a); \
+    else hipLaunchKernelGGL((block_norm_grad_kernel<BF_, NP_, false>), grid, block, lds, s, a);                \
+  } while (0)
     if (bf) {
-      if (g.np == 1) hipLaunchKernelGGL((block_norm_grad_kernel<true, 1>), grid, block, lds, s, a);
-      else if (g.np == 2) hipLaunchKernelGGL((block_norm_grad_kernel<true, 2>), grid, block, lds, s, a);
-      else hipLaunchKernelGGL((block_norm_grad_kernel<true, 4>), grid, block, lds, s, a);
+      if (g.np == 1) SEMMOE_NORM_GRAD(true, 1);
+      else SEMMOE_NORM_GRAD(true, 2);
     } else {
-      if (g.np == 1) hipLaunchKernelGGL((block_norm_grad_kernel<false, 1>), grid, block, lds, s, a);
-      else if (g.np == 2) hipLaunchKernelGGL((block_norm_grad_kernel<false, 2>), grid, block, lds, s, a);
-      else hipLaunchKernelGGL((block_norm_grad_kernel<false, 4>), grid, block, lds, s, a);
+      if (g.np == 1) SEMMOE_NORM_GRAD(false, 1);
+      else if (g.np == 2) SEMMOE_NORM_GRAD(false, 2);
+      else SEMMOE_NORM_GRAD(false, 4);
     }
+#undef SEMMOE_NORM_GRAD
     SEMMOE_LAUNCH_CHECK();
   }
   if (columns) {

@@ -1,6 +1,6 @@
 // Rows held in the registers of a team of waves: how they are read, written, summed and rounded to 8 bits.
 //
-// A team of `tr` threads (whole waves) owns a row; thread t holds the pieces t, t + tr, ... of eight numbers.  The teams of a workgroup
+// A team of `tr` threads (whole waves) owns a row; thread t holds the pieces t, t + tr, ... of 16 bytes.  The teams of a workgroup
 // go through the same number of rows, so that their barriers match; a team without a row counts zeros and stores nothing.
 #pragma once
 #include "common.hpp"
@@ -10,35 +10,26 @@ namespace semmoe {
 typedef __attribute__((ext_vector_type(4))) uint32_t row_u32x4_t;
 
 template <bool BF16>
-struct Eight {  // eight numbers of a row as they lie in memory
-  row_u32x4_t v[BF16 ? 1 : 2];
+struct Piece {  // 16 bytes of a row as they lie in memory
+  static constexpr int N = BF16 ? 8 : 4;
+  row_u32x4_t v;
   __device__ __forceinline__ void load(const void* base, size_t at) {
-    const row_u32x4_t* p = reinterpret_cast<const row_u32x4_t*>(static_cast<const char*>(base) + at * (BF16 ? 2 : 4));
-    v[0] = p[0];
-    if constexpr (!BF16) v[1] = p[1];
+    v = *reinterpret_cast<const row_u32x4_t*>(static_cast<const char*>(base) + at * (BF16 ? 2 : 4));
   }
-  __device__ __forceinline__ void zero() {
-    v[0] = row_u32x4_t{0, 0, 0, 0};
-    if constexpr (!BF16) v[1] = v[0];
-  }
+  __device__ __forceinline__ void zero() { v = row_u32x4_t{0, 0, 0, 0}; }
   __device__ __forceinline__ float operator[](int x) const {
-    if constexpr (BF16) return __uint_as_float(x & 1 ? v[0][x >> 1] & 0xffff0000u : v[0][x >> 1] << 16);
-    else return __uint_as_float(v[x >> 2][x & 3]);
+    if constexpr (BF16) return __uint_as_float(x & 1 ? v[x >> 1] & 0xffff0000u : v[x >> 1] << 16);
+    else return __uint_as_float(v[x]);
   }
-  __device__ __forceinline__ void round(const float (&f)[8]) {
-    if constexpr (BF16) {
+  __device__ __forceinline__ void round(const float (&f)[N]) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) v[0][x] = cvt_pk_bf16(f[2 * x], f[2 * x + 1]);
-    } else {
-#pragma unroll
-      for (int x = 0; x < 8; ++x) v[x >> 2][x & 3] = __float_as_uint(f[x]);
-    }
+    for (int x = 0; x < 4; ++x) v[x] = BF16 ? cvt_pk_bf16(f[(2 * x) % N], f[(2 * x + 1) % N]) : __float_as_uint(f[x]);
   }
   __device__ __forceinline__ void store(void* base, size_t at) const {
-    row_u32x4_t* p = reinterpret_cast<row_u32x4_t*>(static_cast<char*>(base) + at * (BF16 ? 2 : 4));
-    p[0] = v[0];
-    if constexpr (!BF16) p[1] = v[1];
+    *reinterpret_cast<row_u32x4_t*>(static_cast<char*>(base) + at * (BF16 ? 2 : 4)) = v;
   }
+  // keeps the numbers packed from here on: unpacked ahead of time they take twice the registers
+  __device__ __forceinline__ void stay() { asm volatile("" : "+v"(v)); }
 };
 
 // The sum (or, of bits, the maximum) over a team, the same in all of its threads, in an order that depends on the team's size alone.
@@ -82,17 +73,22 @@ struct RowScale {
     const int v = bad ? 0 : __float2int_rn((small ? x * 0x1p64f : x) * r);
     return uint32_t(v) & 255u;
   }
-  __device__ __forceinline__ uint2 q8(const float (&f)[8]) const {
-    return make_uint2(q(f[0]) | q(f[1]) << 8 | q(f[2]) << 16 | q(f[3]) << 24, q(f[4]) | q(f[5]) << 8 | q(f[6]) << 16 | q(f[7]) << 24);
+  // N numbers at `to`, which lies on N bytes
+  template <int N>
+  __device__ __forceinline__ void put(uint8_t* to, const float (&f)[N]) const {
+    const uint32_t lo = q(f[0]) | q(f[1]) << 8 | q(f[2]) << 16 | q(f[3]) << 24;
+    if constexpr (N == 4) *reinterpret_cast<uint32_t*>(to) = lo;
+    else *reinterpret_cast<uint2*>(to) = make_uint2(lo, q(f[4]) | q(f[5]) << 8 | q(f[6]) << 16 | q(f[7]) << 24);
   }
 };
 
-// Threads of a team for rows of `pieces` pieces, pieces a thread (1, 2 or 4; 0: too long for registers), teams of a workgroup.
+// Threads of a team for rows of n_cols numbers, pieces a thread (1, 2 or 4; 0: too long for registers), teams of a workgroup.
 struct RowTeams {
   int tr, np, teams;
-  explicit RowTeams(int pieces) {
-    np = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 0;
-    tr = np ? cdiv(cdiv(pieces, np), 64) * 64 : 512;
+  RowTeams(bool bf16, int n_cols, int most) {  // most: threads of a team
+    const int pieces = n_cols / (bf16 ? 8 : 4);
+    np = pieces <= most ? 1 : pieces <= 2 * most ? 2 : pieces <= 4 * most ? 4 : 0;
+    tr = np ? cdiv(cdiv(pieces, np), 64) * 64 : most;
     teams = tr >= 256 ? 1 : 256 / tr;
   }
 };

@@ -7,45 +7,47 @@
 
 namespace semmoe {
 
-// NP pieces of eight a thread; 0: a row too long for that is read twice, the second time from the caches.
+// NP pieces a thread; 0: a row too long for that is read twice, the second time from the caches.
 template <bool BF16, int NP>
-__global__ __launch_bounds__(512) void quantize_rows_kernel(const void* __restrict__ X, int64_t ldx, int n_rows, int n_cols,
+__global__ __launch_bounds__(1024) void quantize_rows_kernel(const void* __restrict__ X, int64_t ldx, int n_rows, int n_cols,
                                                             const int32_t* __restrict__ row_range, int n_range, int tr,
                                                             uint8_t* __restrict__ Xq, float* __restrict__ x_scale) {
-  __shared__ uint32_t part[8];
-  const int teams = blockDim.x / tr, team = threadIdx.x / tr, t = threadIdx.x % tr, pieces = n_cols / 8;
+  using E = Piece<BF16>;
+  constexpr int N = E::N;
+  __shared__ uint32_t part[16];
+  const int teams = blockDim.x / tr, team = threadIdx.x / tr, t = threadIdx.x % tr, pieces = n_cols / N;
   const int lo = row_range ? row_range[0] : 0, hi = row_range ? min(row_range[n_range], n_rows) : n_rows;
   for (int row0 = lo + int(blockIdx.x) * teams; row0 < hi; row0 += int(gridDim.x) * teams) {
     const int row = row0 + team;
     const bool have = row < hi;
     const size_t at = size_t(have ? row : row0) * ldx;
-    Eight<BF16> v[NP ? NP : 1];
+    E v[NP ? NP : 1];
     uint32_t m[1] = {0};
     if constexpr (NP > 0) {
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
         const int c = t + p * tr;
-        if (c < pieces) v[p].load(X, at + size_t(c) * 8);
+        if (c < pieces) v[p].load(X, at + size_t(c) * N);
         else v[p].zero();
       }
 #pragma unroll
       for (int p = 0; p < NP; ++p)
 #pragma unroll
-        for (int x = 0; x < 8; ++x) m[0] = max(m[0], magnitude_bits(v[p][x]));
+        for (int x = 0; x < N; ++x) m[0] = max(m[0], magnitude_bits(v[p][x]));
     } else {
       for (int c = t; c < pieces; c += tr) {
-        v[0].load(X, at + size_t(c) * 8);
+        v[0].load(X, at + size_t(c) * N);
 #pragma unroll
-        for (int x = 0; x < 8; ++x) m[0] = max(m[0], magnitude_bits(v[0][x]));
+        for (int x = 0; x < N; ++x) m[0] = max(m[0], magnitude_bits(v[0][x]));
       }
     }
     team_join(m, part, tr >> 6, [](uint32_t a, uint32_t b) { return max(a, b); });
     const RowScale s(m[0]);
-    auto put = [&](const Eight<BF16>& e, int c) __attribute__((always_inline)) {
-      float f[8];
+    auto put = [&](const E& e, int c) __attribute__((always_inline)) {
+      float f[N];
 #pragma unroll
-      for (int x = 0; x < 8; ++x) f[x] = e[x];
-      if (have) *reinterpret_cast<uint2*>(Xq + size_t(row) * n_cols + size_t(c) * 8) = s.q8(f);
+      for (int x = 0; x < N; ++x) f[x] = e[x];
+      if (have) s.put(Xq + size_t(row) * n_cols + size_t(c) * N, f);
     };
     if constexpr (NP > 0) {
 #pragma unroll
@@ -53,7 +55,7 @@ __global__ __launch_bounds__(512) void quantize_rows_kernel(const void* __restri
         if (t + p * tr < pieces) put(v[p], t + p * tr);
     } else {
       for (int c = t; c < pieces; c += tr) {
-        v[0].load(X, at + size_t(c) * 8);
+        v[0].load(X, at + size_t(c) * N);
         put(v[0], c);
       }
     }
@@ -67,7 +69,7 @@ int32_t launch_quantize_rows(bool bf16, const void* X, int64_t ldx, int n_rows, 
   DeviceInfo dev;
   const int32_t st = device_info(&dev);
   if (st != SEMMOE_OK) return st;
-  const RowTeams g(n_cols / 8);
+  const RowTeams g(bf16, n_cols, bf16 ? 512 : 1024);
   const long long groups = cdiv(n_rows, g.teams), most = (long long)dev.num_cu * 16;
   const int grid = int(groups < most ? groups : most);
 #define SEMMOE_QUANTIZE(BF_, NP_)                                                                                             \
