@@ -65,11 +65,13 @@ static int32_t launch_dma(const GemmArgs& a, int max_rows, int blocks_per_cu, hi
 }
 
 // Four-wave 256 x 256 kernel; shapes it does not take are reported with SEMMOE_EUNSUPPORTED before any launch.
-template <int MODE, int BK, int NSTAGE, int DMA_EVERY, int TJ = 4>
+template <int MODE, int BK, int NSTAGE, int DMA_EVERY, int TJ = 4, bool KT = false>
 static int32_t launch_w4(const GemmArgs& a, int max_rows, hipStream_t stream) {
+  if constexpr (kI8<MODE> && !KT)
+    if (a.K % BK != 0) return launch_w4<MODE, BK, NSTAGE, DMA_EVERY, TJ, true>(a, max_rows, stream);
   using C = W4Cfg<MODE, BK, NSTAGE, DMA_EVERY, TJ>;
   const int w_rows = kPaired<MODE> ? 2 * a.N : a.N;
-  if (a.K % BK != 0 || a.K / BK < NSTAGE) return SEMMOE_EUNSUPPORTED;
+  if ((!KT && a.K % BK != 0) || cdiv(a.K, BK) < NSTAGE) return SEMMOE_EUNSUPPORTED;
   if ((unsigned long long)w_rows * a.ldw * 2 >= (1ull << 32) || (unsigned long long)C::BT * a.ldx * 2 >= (1ull << 32))
     return SEMMOE_EUNSUPPORTED;  // per-lane row offsets are 32-bit
   const size_t lds = TJ == 4 ? C::kLdsBytes : C::lds_bytes(a.nq);
@@ -78,7 +80,7 @@ static int32_t launch_w4(const GemmArgs& a, int max_rows, hipStream_t stream) {
   const long long bound = (long long)(max_rows / C::BT + a.nq) * n_ftiles;
   if (bound <= 0) return SEMMOE_OK;
   const int grid = grid_for(bound, num_cu());
-  auto kern = gemm_bf16_w4_kernel<MODE, BK, NSTAGE, DMA_EVERY, TJ>;
+  auto kern = gemm_bf16_w4_kernel<MODE, BK, NSTAGE, DMA_EVERY, TJ, KT>;
   static std::atomic<uint64_t> lds_allowed{0};  // one flag word per instantiation, a bit per device
   {
     const int32_t as = allow_max_dynamic_lds(&lds_allowed, reinterpret_cast<const void*>(kern));
@@ -121,11 +123,13 @@ static int32_t launch_tail_as(GemmArgs a, int max_rows, int head_grid, hipStream
 
 // Tail launch with 128 x 128 pieces (four per parent tile), one workgroup per compute unit: the K loop of the
 // four-wave kernel in small.  K must be a multiple of 64 with at least a ring of slices.
-template <int MODE, int NSTAGE>
+template <int MODE, int NSTAGE, bool KT = false>
 static int32_t launch_tail_pieces(GemmArgs a, int max_rows, int head_grid, hipStream_t stream) {
+  if constexpr (kI8<MODE> && !KT)
+    if (a.K % 64 != 0) return launch_tail_pieces<MODE, NSTAGE, true>(a, max_rows, head_grid, stream);
   using C = DmaCfg<MODE, 2, 2, 2, 2, 64, NSTAGE>;
   const int w_rows = kPaired<MODE> ? 2 * a.N : a.N;
-  if (a.K % 64 != 0 || a.K / 64 < NSTAGE) return SEMMOE_EUNSUPPORTED;
+  if ((!KT && a.K % 64 != 0) || cdiv(a.K, 64) < NSTAGE) return SEMMOE_EUNSUPPORTED;
   if ((unsigned long long)w_rows * a.ldw * 2 >= (1ull << 32) || (unsigned long long)C::BT * a.ldx * 2 >= (1ull << 32))
     return SEMMOE_EUNSUPPORTED;  // per-lane row offsets are 32-bit
   if (C::kLdsBytes > size_t(max_lds())) return SEMMOE_EUNSUPPORTED;
@@ -139,7 +143,7 @@ static int32_t launch_tail_pieces(GemmArgs a, int max_rows, int head_grid, hipSt
   a.sched_sub_t = kSubT;
   a.sched_sub_f = kSubF;
   const int grid = grid_for(left_p * kSubT * kSubF, num_cu());
-  auto kern = gemm_bf16_piece_kernel<MODE, NSTAGE>;
+  auto kern = gemm_bf16_piece_kernel<MODE, NSTAGE, KT>;
   static std::atomic<uint64_t> lds_allowed{0};  // one flag word per instantiation, a bit per device
   {
     const int32_t as = allow_max_dynamic_lds(&lds_allowed, reinterpret_cast<const void*>(kern));
@@ -153,11 +157,13 @@ static int32_t launch_tail_pieces(GemmArgs a, int max_rows, int head_grid, hipSt
 // Every tile as 128 x 128 pieces with the loads placed between the MFMAs (the tail's piece kernel with nothing left
 // to a head launch): for problems whose 256 x 256 tiles would leave most compute units idle, such as the shared
 // expert on one rank's shard of tokens.
-template <int MODE>
+template <int MODE, bool KT = false>
 static int32_t launch_all_pieces(GemmArgs a, int max_rows, hipStream_t stream) {
+  if constexpr (kI8<MODE> && !KT)
+    if (a.K % 64 != 0) return launch_all_pieces<MODE, true>(a, max_rows, stream);
   using C = DmaCfg<MODE, 2, 2, 2, 2, 64, 3>;
   const int w_rows = kPaired<MODE> ? 2 * a.N : a.N;
-  if (a.K % 64 != 0 || a.K / 64 < 3) return SEMMOE_EUNSUPPORTED;
+  if ((!KT && a.K % 64 != 0) || cdiv(a.K, 64) < 3) return SEMMOE_EUNSUPPORTED;
   if ((unsigned long long)w_rows * a.ldw * 2 >= (1ull << 32) || (unsigned long long)C::BT * a.ldx * 2 >= (1ull << 32))
     return SEMMOE_EUNSUPPORTED;  // per-lane row offsets are 32-bit
   if (C::kLdsBytes > size_t(max_lds())) return SEMMOE_EUNSUPPORTED;
@@ -170,7 +176,7 @@ static int32_t launch_all_pieces(GemmArgs a, int max_rows, hipStream_t stream) {
   a.sched_sub_f = 2;
   a.sched_fine = 1;  // 128 x 64 pieces when the 128 x 128 ones would leave half the compute units idle
   const int grid = grid_for(bound_p * 8, num_cu());
-  auto kern = gemm_bf16_piece_kernel<MODE, 3>;
+  auto kern = gemm_bf16_piece_kernel<MODE, 3, KT>;
   static std::atomic<uint64_t> lds_allowed{0};  // one flag word per instantiation, a bit per device
   {
     const int32_t as = allow_max_dynamic_lds(&lds_allowed, reinterpret_cast<const void*>(kern));
@@ -183,12 +189,14 @@ static int32_t launch_all_pieces(GemmArgs a, int max_rows, hipStream_t stream) {
 
 // Head (four-wave 256 x 256 tiles, K slices of 64, ring of 2) and tail (128 x 128 pieces, ring of 3) in one launch.
 // SEMMOE_EUNSUPPORTED when either half does not take the shape: the caller then launches them one after the other.
-template <int MODE, int NSTAGE = 2, int TJ = 4>
+template <int MODE, int NSTAGE = 2, int TJ = 4, bool KT = false>
 static int32_t launch_w4_split(const GemmArgs& h, int max_rows, hipStream_t stream) {
+  if constexpr (kI8<MODE> && !KT)
+    if (h.K % 64 != 0) return launch_w4_split<MODE, NSTAGE, TJ, true>(h, max_rows, stream);
   using CH = W4Cfg<MODE, 64, NSTAGE, 2, TJ>;
   using CP = DmaCfg<MODE, 2, 2, 2, 2, 64, 3>;
   const int w_rows = kPaired<MODE> ? 2 * h.N : h.N;
-  if (h.K % 64 != 0 || h.K / 64 < 3) return SEMMOE_EUNSUPPORTED;
+  if ((!KT && h.K % 64 != 0) || cdiv(h.K, 64) < 3) return SEMMOE_EUNSUPPORTED;
   if ((unsigned long long)w_rows * h.ldw * 2 >= (1ull << 32) || (unsigned long long)CH::BT * h.ldx * 2 >= (1ull << 32))
     return SEMMOE_EUNSUPPORTED;  // per-lane row offsets are 32-bit
   const size_t head_lds = TJ == 4 ? CH::kLdsBytes : CH::lds_bytes(h.nq);
@@ -204,7 +212,7 @@ static int32_t launch_w4_split(const GemmArgs& h, int max_rows, hipStream_t stre
   t.sched_sub_t = CH::BT / CP::BT;
   t.sched_sub_f = CH::BW / CP::BW;
   t.sched_fine = tuning_value(SEMMOE_TUNE_TAIL_RING) == 2 ? 0 : 1;
-  auto kern = gemm_bf16_w4_split_kernel<MODE, 64, NSTAGE, 2, 3, TJ>;
+  auto kern = gemm_bf16_w4_split_kernel<MODE, 64, NSTAGE, 2, 3, TJ, KT>;
   static std::atomic<uint64_t> lds_allowed{0};  // one flag word per instantiation, a bit per device
   {
     const int32_t as = allow_max_dynamic_lds(&lds_allowed, reinterpret_cast<const void*>(kern));
@@ -516,10 +524,11 @@ static int32_t launch_bf16_tile(int id, const GemmArgs& a, int max_rows, int bpc
 // it: 45 83 179 as 256 x 128 tiles, 66 112 236 as 256 x 256, 37 105 234 as pieces.  256 x 256 tiles are ahead of 256 x 128
 // from three fifths of the compute units on (170 to 190 of them: 2 to 4 %; 130 to 150: 2 % behind); 2514 rows of d 6968,
 // F 1312, gate/up without whole slices: 248 us for the FFN with pieces, 331 with 256 x 256 tiles on less than half of the chip.
-static int default_tile(const GemmArgs& a, int max_rows, int est_rows_per_group, int w_rows) {
+// tails: the tiles with a running load stream take any K (8-bit operands)
+static int default_tile(const GemmArgs& a, int max_rows, int est_rows_per_group, int w_rows, bool tails = false) {
   const int est = est_rows_per_group, t256 = cdiv(w_rows, 256);
   const long long cus = num_cu();
-  const bool whole_slices = a.K % 64 == 0 && a.K / 64 >= 3;  // what the tiles with a running load stream need
+  const bool whole_slices = (tails || a.K % 64 == 0) && cdiv(a.K, 64) >= 3;  // what the tiles with a running load stream need
   const int big_tile = (long long)(max_rows / 256 + a.nq) * t256 * 2 >= cus ? 22 : 28;
   if (!a.offsets) {
     auto tiles = [&](int w, int t) { return (long long)cdiv(w_rows, w) * cdiv(est, t); };
@@ -576,7 +585,7 @@ static int32_t launch_by_rule(const GemmArgs& a, int max_rows, int est_rows_per_
   const int knob = tuning_value(kPaired<MODE> ? SEMMOE_TUNE_GATEUP_TILE : SEMMOE_TUNE_DOWN_TILE);
   const bool known = !kI8<MODE> || knob == 0 || knob == 16 || knob == 22 || knob == 26 || knob == 28 || (knob >= 30 && knob <= 35) ||
                      (knob >= 38 && knob <= 40);  // 8-bit operands: the shapes that are built for them
-  const int id = knob >= 0 && known ? knob : default_tile(a, max_rows, est_rows_per_group, kPaired<MODE> ? 2 * a.N : a.N);
+  const int id = knob >= 0 && known ? knob : default_tile(a, max_rows, est_rows_per_group, kPaired<MODE> ? 2 * a.N : a.N, kI8<MODE>);
   if (!split_launch(id)) return launch_bf16_tile<MODE>(id, a, max_rows, bpc, stream);
   GemmArgs h = a;
   h.sched_mode = 1;

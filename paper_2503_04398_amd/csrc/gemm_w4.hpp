@@ -18,7 +18,7 @@
 //   * the stream of slices does not stop at a tile boundary: the loads run NSTAGE slices ahead of the
 //     MFMAs, into the next tile of this workgroup, so the epilogue of a tile (accumulators -> a small
 //     per-wave LDS staging area -> 16-byte coalesced stores, no barrier) overlaps the loads of the next.
-// Needs K % BK == 0 and K / BK >= NSTAGE; other shapes take the kernels of gemm_core.hpp.
+// Needs K % BK == 0 (but for 8-bit operands) and K / BK >= NSTAGE; other shapes take the kernels of gemm_core.hpp.
 #pragma once
 #include <type_traits>
 
@@ -58,6 +58,18 @@ __device__ __forceinline__ void lds_dma16_imm(const void* sbase, uint32_t voff, 
 __device__ __forceinline__ float silu_mul_fast(float g, float u) {
   // silu(g) * u with one exp2 and one reciprocal
   return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * g)) * u;
+}
+
+// fragments of k that lie behind the end of the rows
+template <int N>
+__device__ __forceinline__ void clear_behind(bf16x8_t (&f)[N], bool behind) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    i32x4_t v = __builtin_bit_cast(i32x4_t, f[j]);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) v[x] = behind ? 0 : v[x];
+    f[j] = __builtin_bit_cast(bf16x8_t, v);
+  }
 }
 
 // TJ: MFMA columns (32 tokens) of a wave; the tile is 256 weight rows x 64*TJ tokens
@@ -113,7 +125,9 @@ __device__ __forceinline__ TileRef locate_tile(const GemmArgs& a, const int* pre
   return t;
 }
 
-template <int MODE, int BK, int NSTAGE, int DMA_EVERY, int TJ = 4>
+// KT (8-bit operands): K is no multiple of a slice.  The last slice's loads of what lies behind K fetch the slice's first chunk instead
+// (they stay inside the row), and those k of the token fragments are cleared before they are multiplied: integers times zero are zero.
+template <int MODE, int BK, int NSTAGE, int DMA_EVERY, int TJ = 4, bool KT = false>
 __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned char* lds_raw) {
   using C = W4Cfg<MODE, BK, NSTAGE, DMA_EVERY, TJ>;
   // kModeLogits here: raw fp32 sums, no bias terms (the K-split router adds the parts and the biases afterwards)
@@ -143,7 +157,9 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
   }
   const int listed = __builtin_amdgcn_readfirstlane(build_tile_prefix(a, n_ftiles, pre, C::BT));  // ends with a barrier
   const int total = a.sched_mode == 1 ? head_tiles(listed, G, a.sched_thr) : listed;  // head launch of a split
-  const int nk = a.K / BK;
+  static_assert(!KT || (kI8<MODE> && BK == 64), "integers times zero; two places of a chunk");
+  const int nk = (a.K + BK - 1) / BK;
+  const int k_tail = (a.K - (nk - 1) * BK) * 2;  // bytes of a row in the last slice
   const ItemWalk my = xcd_share(total);
   if (my.count == 0) return;  // whole workgroup: no barrier is pending
 
@@ -178,6 +194,19 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
   const unsigned char* i_base2 = nullptr;  // ... of the loads from kSplit on (128 token rows only)
   uint32_t i_off[C::IPW];                 // per lane: byte offset of the row + chunk it fetches
 
+  // KT: how far back those loads of the last slice go whose chunk lies behind K.  A lane's chunk is the same for every second load.
+  const int k_chunk = d_pos ^ (d_row >> 1);
+  const uint32_t back0 = KT && k_chunk * 16 >= k_tail ? k_chunk * 16 : 0, back1 = KT && (k_chunk ^ 4) * 16 >= k_tail ? (k_chunk ^ 4) * 16 : 0;
+  bool at_tail = false;  // i_off are those of the last slice
+  auto i_tail = [&](bool on) __attribute__((always_inline)) {
+    if constexpr (KT) {
+      if (on == at_tail) return;
+      at_tail = on;
+#pragma unroll
+      for (int i = 0; i < C::IPW; ++i) i_off[i] += on ? 0u - (i & 1 ? back1 : back0) : (i & 1 ? back1 : back0);
+    }
+  };
+
   // (the lambdas are forced inline: one left as a call makes the argument block a stack object, and every access
   // to it a scratch load that waits for all the tile loads in flight)
   TileRef s_tile;  // the tile the stream stands in: the MFMAs reach it NSTAGE slices later and take it from here
@@ -207,6 +236,7 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
       return uint32_t(min(sr, t.n_tok - 1)) * uint32_t(a.ldx) * 2u + uint32_t(c) * 16u;
     };
     i_k = first_step(a, t.widx, 2, nk);
+    at_tail = false;
     i_base = (first_w ? w_panel : x_panel) + i_k * C::RB;
     if constexpr (TJ != 4) i_base2 = (loads_w ? w_panel : x_panel) + i_k * C::RB;
     if (first_w) {
@@ -242,6 +272,7 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
       ++i_tile;
       i_setup(my.item(i_tile));
     }
+    i_tail(i_k + 1 == nk);
   };
   // load number i of the current slice of the stream; after the last one the stream moves to the next slice
   auto i_issue = [&](auto idx) __attribute__((always_inline)) {
@@ -267,8 +298,8 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
   for (int s = 0; s < NSTAGE; ++s) {  // nk >= NSTAGE: these slices belong to the first tile
 #pragma unroll
     for (int i = 0; i < C::IPW; ++i)
-      lds_dma16_s((i < kSplit ? i_base : i_base2) + (i_k + s < nk ? s : s - nk) * C::RB, i_off[i],
-                  lds_base + s * C::kStageBytes + (wave * C::IPW + i) * 1024);
+      lds_dma16_s((i < kSplit ? i_base : i_base2) + (i_k + s < nk ? s : s - nk) * C::RB,
+                  KT && i_k + s + 1 == nk ? i_off[i] - (i & 1 ? back1 : back0) : i_off[i], lds_base + s * C::kStageBytes + (wave * C::IPW + i) * 1024);
   }
   // The stream stands at slice NSTAGE-1, already fetched.  Where the last load of a window falls behind the
   // window's first k-step, the k-steps before the first barrier carry that tail: they fetch the rest of the
@@ -278,6 +309,7 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
   i_base += ahead * C::RB;
   if constexpr (TJ != 4) i_base2 += ahead * C::RB;
   i_k += ahead;
+  i_tail(i_k + 1 == nk);
   i_slice = NSTAGE - 1;
   i_stage = NSTAGE - 1;
   i_dst = lds_base + i_stage * C::kStageBytes + wave * C::IPW * 1024;
@@ -301,6 +333,7 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
+    int c_left = KT ? nk - first_step(a, t.widx, 2, nk) : 0;  // slices to the row's end, the one being multiplied among them
     for (int it = 0; it < nk; ++it) {
       const int n_stage = (c_stage + 1 == NSTAGE) ? 0 : c_stage + 1;
       // one k-step; the k-step index is a compile-time constant (a pragma-unrolled loop over it was left partly
@@ -321,6 +354,8 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
         // one behind the first eight MFMAs: as a burst in front of the MFMAs they cost about 2 %
         const unsigned char* S_next = lds_raw + ((ks == kLast) ? n_stage : c_stage) * C::kStageBytes;
         const int off_next = ((((ks == kLast) ? 0 : ks + 1) * 2 + (lane >> 5)) ^ frag_swz) * 16;
+        if constexpr (KT)
+          if (c_left == 1) clear_behind(bfr[cur], (ks * 2 + (lane >> 5)) * 16 >= k_tail);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
@@ -358,6 +393,7 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
         k_step(std::integral_constant<int, 3>{});
       }
       c_stage = n_stage;
+      if (KT && --c_left == 0) c_left = nk;
     }
 
     // ---- epilogue: no barrier; the ring already holds the next tile's first slices
@@ -529,7 +565,8 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
 // TT = 2: 128 x 128 pieces (four per parent tile).  TT = 1: 128 weight rows x 64 tokens (eight per parent tile), for
 // when so few parent tiles are left over that the bigger pieces would leave most compute units idle; sub_t is then
 // the number of pieces along the tokens of a parent tile (4) in place of the launch's value.
-template <int MODE, int NSTAGE, int TT>
+// KT as above.
+template <int MODE, int NSTAGE, int TT, bool KT = false>
 __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned char* lds_raw, int sub_t = 0, bool spread = true) {
   using C = DmaCfg<MODE, 2, 2, 2, TT, 64, NSTAGE>;
   static_assert(C::KS == 4 && C::RB == 128 && C::BW == 128 && (TT == 1 || TT == 2), "geometry the loop below is written for");
@@ -545,7 +582,9 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
   const int wf = wave & 1;
   const int wt = wave >> 1;
   const TileWalk walk = make_walk(a, pre, C::BT, C::FEAT, sub_t);
-  const int nk = a.K / 64;
+  static_assert(!KT || kI8<MODE>, "integers times zero");
+  const int nk = (a.K + 63) / 64;
+  const int k_tail = (a.K - (nk - 1) * 64) * 2;
 
   const int frag_swz = ((lane & 31) / C::RPB) % C::CPR;
   const unsigned frag_w = (wf * 64 + (lane & 31)) * C::RB;
@@ -592,6 +631,17 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
         i_off[i] = uint32_t(min(xr, at.n_tok - 1)) * uint32_t(a.ldx) * 2u + uint32_t(c) * 16u;
       }
     }
+    const int k_chunk = d_pos ^ (d_row >> 1);
+    const uint32_t back0 = KT && k_chunk * 16 >= k_tail ? k_chunk * 16 : 0, back1 = KT && (k_chunk ^ 4) * 16 >= k_tail ? (k_chunk ^ 4) * 16 : 0;
+    bool at_tail = false;
+    auto i_tail = [&](bool on) __attribute__((always_inline)) {
+      if constexpr (KT) {
+        if (on == at_tail) return;
+        at_tail = on;
+#pragma unroll
+        for (int i = 0; i < kIpwW; ++i) i_off[i] += on ? 0u - (i & 1 ? back1 : back0) : (i & 1 ? back1 : back0);
+      }
+    };
     int i_slice = 0, i_stage = 0;
     int i_k = first_step(a, widx, 2, nk);  // place of the slice in K
     i_base += i_k * C::RB;
@@ -608,6 +658,7 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
       i_base += step * C::RB;
       i_stage = (i_stage + 1 == NSTAGE) ? 0 : i_stage + 1;
       i_dst = lds_base + i_stage * C::kStageBytes + my_rows_lds;
+      i_tail(i_k + 1 == nk);
     };
     auto i_issue = [&](auto idx) __attribute__((always_inline)) {
       constexpr int i = decltype(idx)::value;
@@ -639,12 +690,13 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
 #pragma unroll
       for (int i = 0; i < kIpwW; ++i)
         if (i < n_my)
-          lds_dma16_s(i_base + (i_k + s0 < nk ? s0 : s0 - nk) * C::RB, i_off[i],
-                      lds_base + s0 * C::kStageBytes + my_rows_lds + i * 1024);
+          lds_dma16_s(i_base + (i_k + s0 < nk ? s0 : s0 - nk) * C::RB,
+                      KT && i_k + s0 + 1 == nk ? i_off[i] - (i & 1 ? back1 : back0) : i_off[i], lds_base + s0 * C::kStageBytes + my_rows_lds + i * 1024);
     }
     const int ahead = i_k + NSTAGE - 1 < nk ? NSTAGE - 1 : NSTAGE - 1 - nk;
     i_base += ahead * C::RB;
     i_k += ahead;
+    i_tail(i_k + 1 == nk);
     i_slice = NSTAGE - 1;
     i_stage = NSTAGE - 1;
     i_dst = lds_base + i_stage * C::kStageBytes + my_rows_lds;
@@ -661,6 +713,7 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
+    int c_left = KT ? nk - first_step(a, widx, 2, nk) : 0;
     for (int it = 0; it < nk; ++it) {
       const int n_stage = (c_stage + 1 == NSTAGE) ? 0 : c_stage + 1;
       auto k_step = [&](auto ks_tag) __attribute__((always_inline)) {
@@ -676,6 +729,8 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
         // the four fragment reads of the next k-step go out one by one behind the MFMAs
         const unsigned char* S_next = lds_raw + ((ks == 3) ? n_stage : c_stage) * C::kStageBytes;
         const int off_next = ((((ks == 3) ? 0 : ks + 1) * 2 + (lane >> 5)) ^ frag_swz) * 16;
+        if constexpr (KT)
+          if (c_left == 1) clear_behind(bfr[cur], (ks * 2 + (lane >> 5)) * 16 >= k_tail);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < TT; ++j) {
@@ -710,6 +765,7 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
       k_step(std::integral_constant<int, 2>{});
       k_step(std::integral_constant<int, 3>{});
       c_stage = n_stage;
+      if (KT && --c_left == 0) c_left = nk;
     }
     wait_vmcnt<0>();   // the standing stream's last loads: nothing may write into the ring any more
     __syncthreads();   // every wave has left the ring: it now takes the output piece
@@ -718,45 +774,45 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
   }
 }
 
-template <int MODE, int BK, int NSTAGE, int DMA_EVERY, int TJ = 4>
+template <int MODE, int BK, int NSTAGE, int DMA_EVERY, int TJ = 4, bool KT = false>
 __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(GemmArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-  gemm_bf16_w4_body<MODE, BK, NSTAGE, DMA_EVERY, TJ>(a, lds_raw);
+  gemm_bf16_w4_body<MODE, BK, NSTAGE, DMA_EVERY, TJ, KT>(a, lds_raw);
 }
 
 // Pieces as a launch of their own.  With sched_fine set the kernel halves the pieces along the tokens (128 x 64)
 // when twice the number of 128 x 128 pieces still fits the grid, as the split kernel below does for its tail.
-template <int MODE, int NSTAGE>
+template <int MODE, int NSTAGE, bool KT = false>
 __global__ __launch_bounds__(256, 1) void gemm_bf16_piece_kernel(GemmArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
   if (a.sched_fine) {
     const TileWalk probe = make_walk(a, reinterpret_cast<int*>(lds_raw), 128, kPaired<MODE> ? 64 : 128);
     __syncthreads();
     if (probe.total > 0 && probe.total * 2 <= int(gridDim.x)) {
-      gemm_bf16_piece_body<MODE, NSTAGE, 1>(a, lds_raw, 4, false);
+      gemm_bf16_piece_body<MODE, NSTAGE, 1, KT>(a, lds_raw, 4, false);
       return;
     }
   }
-  gemm_bf16_piece_body<MODE, NSTAGE, 2>(a, lds_raw, 0, false);
+  gemm_bf16_piece_body<MODE, NSTAGE, 2, KT>(a, lds_raw, 0, false);
 }
 
 // Head and tail of a split in one launch: every workgroup first works through its 256 x 256 tiles of the full rounds,
 // then takes pieces of the left-over tiles.  Pieces and head tiles write disjoint outputs, so nothing has to be waited
 // for in between except this workgroup's own LDS.  Saves the second launch (also when nothing is left over, which
 // only the device knows) and lets a workgroup that is done early start on the pieces.
-template <int MODE, int BK, int NSTAGE, int DMA_EVERY, int PIECE_RING, int TJ = 4>
+template <int MODE, int BK, int NSTAGE, int DMA_EVERY, int PIECE_RING, int TJ = 4, bool KT = false>
 __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_split_kernel(GemmArgs head, GemmArgs tail) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-  gemm_bf16_w4_body<MODE, BK, NSTAGE, DMA_EVERY, TJ>(head, lds_raw);
+  gemm_bf16_w4_body<MODE, BK, NSTAGE, DMA_EVERY, TJ, KT>(head, lds_raw);
   __syncthreads();  // the head's last output staging has been read
   // few parent tiles left over: 128 x 64 pieces, eight per parent tile, so that twice as many compute units take part
   // (a piece walks all of K however few there are: its time does not shrink with their number)
   const TileWalk probe = make_walk(tail, reinterpret_cast<int*>(lds_raw), 128, kPaired<MODE> ? 64 : 128);
   __syncthreads();
   if (tail.sched_fine && probe.total > 0 && probe.total * 2 <= int(gridDim.x)) {
-    gemm_bf16_piece_body<MODE, PIECE_RING, 1>(tail, lds_raw, TJ);  // 64 tokens a piece
+    gemm_bf16_piece_body<MODE, PIECE_RING, 1, KT>(tail, lds_raw, TJ);  // 64 tokens a piece
   } else {
-    gemm_bf16_piece_body<MODE, PIECE_RING, 2>(tail, lds_raw);
+    gemm_bf16_piece_body<MODE, PIECE_RING, 2, KT>(tail, lds_raw);
   }
 }
 

@@ -137,6 +137,26 @@ def test_linear_i8(T, d_in, d_out):
     assert (Y[T] == 7.0).all()
 
 
+@pytest.mark.parametrize("d_in", [400, 416, 464, 496, 528, 1168, 2880])
+@pytest.mark.parametrize("T,d_out", [(150, 1024), (700, 2056), (1024, 2880), (2600, 5768)])
+def test_linear_i8_of_partial_slices(T, d_out, d_in):
+    """rows that end inside a slice of 128 bytes, through 128 x 128 pieces, 256 x 128 and 256 x 256 tiles; the rows behind the last
+    one hold the largest numbers"""
+    r = np.random.default_rng(T + d_in)
+    (q, s), (w, ws) = _quantized(r, T + 1, d_in), _quantized(r, d_out + 1, d_in, d_in ** -0.5)
+    q[T], w[d_out] = -128, -128
+    Y = torch.empty(T, d_out, dtype=torch.bfloat16, device=DEV)
+    _m().linear_i8(q[:T], s[:T], w[:d_out], ws[:d_out], Y)
+    want = Q.linear(*(t.cpu().numpy() for t in (q[:T], s[:T], w[:d_out], ws[:d_out])))
+    _within(Y, want, (R["bf16"] + 3 * E32) * np.abs(want) + TINY, "Y")
+
+
+@pytest.mark.parametrize("d,F", [(400, 272), (528, 464), (720, 400)])
+@pytest.mark.parametrize("rows", [[45] * 8, [130, 0, 257, 64, 1, 300], [700, 300, 900]])
+def test_expert_ffn_i8_of_partial_slices(rows, d, F):
+    _experts(rows, d, F, seed=5)
+
+
 def test_linear_i8_sums_are_exact():
     """the largest sums there are: rows of -128, as deep as a product may be, and sums that cancel but for one"""
     K = 131056
