@@ -44,6 +44,14 @@ __device__ __forceinline__ void lds_dma16_s(const void* sbase, uint32_t voff, un
                : "memory", "m0");
 }
 
+// 4 bytes per lane: lane L writes LDS[m0 + 4 L]
+__device__ __forceinline__ void lds_dma4_s(const void* sbase, uint32_t voff, unsigned lds_addr_uniform) {
+  sbase = scalar_ptr(static_cast<const unsigned char*>(sbase));
+  lds_addr_uniform = unsigned(__builtin_amdgcn_readfirstlane(int(lds_addr_uniform)));
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_addr_uniform), "v"(voff), "s"(sbase)
+               : "memory", "m0");
+}
+
 // The same with the LDS address given as a uniform base plus a compile-time offset: one scalar add into m0 and the
 // load, nothing else, so that the pair fits in the shadow of the MFMA issued before it.
 template <int IMM>
@@ -90,9 +98,11 @@ struct W4Cfg {
   static constexpr int NB = TJ == 4 ? 2 : 1;           // blocks of 32 features that an epilogue pass stages
   static constexpr int kStgRow = NB * 64 + 16;         // staging row: 32*NB bf16 + pad against bank conflicts
   static constexpr int kStgWave = 32 * kStgRow;        // 32 tokens per pass
-  static constexpr size_t kLdsBytes = kRingBytes + 4 * kStgWave + 4 * 520 * 4;  // + tile prefix + group table
+  // 8-bit operands: the tile's scales, 256 weight rows' and then the tokens'
+  static constexpr int kScales = kI8<MODE> ? BW + BT : 0, kScaleBytes = kScales * 4;
+  static constexpr size_t kLdsBytes = kRingBytes + 4 * kStgWave + kScaleBytes + 4 * 520 * 4;  // + tile prefix + group table
   static_assert(BK == 32 || BK == 64, "row of 64 or 128 bytes");
-  static constexpr size_t lds_bytes(int nq) { return kRingBytes + 4 * kStgWave + (4 * size_t(nq) + 8) * 4; }
+  static constexpr size_t lds_bytes(int nq) { return kRingBytes + 4 * kStgWave + kScaleBytes + (4 * size_t(nq) + 8) * 4; }
   static_assert(KS * 4 * TJ / DMA_EVERY >= IPW, "the loads of a slice fit between two barriers");
   static_assert(TJ == 4 || TJ == 2, "how the rows of a slice are dealt out to the waves");
   static_assert(NSTAGE >= 2 && (NSTAGE - 1) * IPW < 64, "vmcnt range");
@@ -139,7 +149,8 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
   const int wf = wave & 1;   // quadrant along weight rows
   const int wt = wave >> 1;  // quadrant along tokens
   unsigned char* stg = lds_raw + C::kRingBytes + wave * C::kStgWave;
-  int* pre = reinterpret_cast<int*>(lds_raw + C::kRingBytes + 4 * C::kStgWave);
+  float* const scales = reinterpret_cast<float*>(lds_raw + C::kRingBytes + 4 * C::kStgWave);
+  int* pre = reinterpret_cast<int*>(lds_raw + C::kRingBytes + 4 * C::kStgWave + C::kScaleBytes);
 
   int* gtab = pre + (TJ == 4 ? 520 : a.nq + 1);
   const int n_ftiles = (a.N + C::FEAT - 1) / C::FEAT;
@@ -282,6 +293,20 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
     if constexpr (i == C::IPW - 1) i_next_slice();
   };
 
+  // The scales of a tile of 8-bit operands, straight to LDS: 16 bytes a lane of the weights' rows, 4 of the tokens'.  Requested behind
+  // the first barrier of the tile, when no wave reads those of the tile before any more, and there by the next one (an older load than
+  // those which the wait there leaves in flight).  From memory in the epilogue each read waits for the stores of the pass before.
+  auto fetch_scales = [&](const TileRef& t) __attribute__((always_inline)) {
+    const unsigned to = lds_base + C::kRingBytes + 4 * C::kStgWave;
+    if (wave == 0) {
+      const float* ws = a.w_scale + size_t(t.widx) * (kPaired<MODE> ? 2 * a.N : a.N);
+      const int col = kPaired<MODE> ? (lane >> 5) * a.N + min(t.f0 + (lane & 31) * 4, a.N - 4) : min(t.f0 + lane * 4, a.N - 4);
+      lds_dma16_s(ws, uint32_t(col) * 4u, to);
+    }
+    if (wave * 64 < C::BT)
+      lds_dma4_s(a.x_scale + t.row_lo, uint32_t(min(wave * 64 + lane, t.n_tok - 1)) * 4u, to + (C::BW + wave * 64) * 4);
+  };
+
   // ---- fragments
   bf16x8_t af[2][4], bfr[2][TJ];
   auto frag = [&](int stage, int ks, bf16x8_t(&fa)[4], bf16x8_t(&fb)[TJ]) __attribute__((always_inline)) {
@@ -349,6 +374,8 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
           // issued, unless the stream has ended)
           if (!i_done) wait_vmcnt<(NSTAGE - 2) * C::IPW>(); else wait_vmcnt<0>();
           __syncthreads();
+          if constexpr (kI8<MODE>)
+            if (it == 0) fetch_scales(t);
         }
         // the eight fragment reads of the next k-step (the next slice's first one after the barrier) go out one by
         // one behind the first eight MFMAs: as a burst in front of the MFMAs they cost about 2 %
@@ -448,12 +475,11 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
         dh[g4] = *reinterpret_cast<const f32x4_t*>(a.b_g + quad_at(a.N, row, min(col + g4 * 8, a.N - 4)));
     };
     if constexpr (MODE == kModeSwigluGrad) fetch_dh(0, 0);
-    const float* const w_scale = kI8<MODE> ? a.w_scale + size_t(t.widx) * (kPaired<MODE> ? 2 * a.N : a.N) : nullptr;
 #pragma unroll
     for (int j = 0; j < TJ; ++j) {
       if (j >= nj) break;
       float x_scale = 0.0f;
-      if constexpr (kI8<MODE>) x_scale = a.x_scale[t.row_lo + min((j * 2 + wt) * 32 + tok_in, t.n_tok - 1)];
+      if constexpr (kI8<MODE>) x_scale = scales[C::BW + (j * 2 + wt) * 32 + tok_in];
 #pragma unroll
       for (int h = 0; h < kPasses; ++h) {
         // One pass at a time.  The accumulators of the pass are pinned to the accumulation registers up to
@@ -501,13 +527,11 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
                 v = dgu[part][b][g4];
               } else if constexpr (kI8<MODE>) {
                 // a lane's four features of a token are 16 bytes of the weights' scales
-                int col = t.f0 + (kPaired<MODE> ? wf * 64 : wf * 128) + (h * NB + b) * 32 + g4 * 8 + half * 4;
-                asm volatile("" : "+v"(col));  // addresses kept from pass to pass would be spilled
-                col = min(col, a.N - 4);
-                const f32x4_t s0 = *reinterpret_cast<const f32x4_t*>(w_scale + col);
+                const float* const ws = scales + (kPaired<MODE> ? wf * 64 : wf * 128) + (h * NB + b) * 32 + g4 * 8 + half * 4;
+                const f32x4_t s0 = *reinterpret_cast<const f32x4_t*>(ws);
                 float y[4];
                 if constexpr (kPaired<MODE>) {
-                  const f32x4_t s1 = *reinterpret_cast<const f32x4_t*>(w_scale + a.N + col);
+                  const f32x4_t s1 = *reinterpret_cast<const f32x4_t*>(ws + C::BW / 2);
 #pragma unroll
                   for (int e = 0; e < 4; ++e)
                     y[e] = silu_mul_fast(scaled_sum(acc[2 * (NB * h + b)][j][g4 * 4 + e], x_scale, s0[e]),
