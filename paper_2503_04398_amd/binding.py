@@ -237,6 +237,7 @@ class SemMoE:
         self._mine = _OfThread()
         self._adapter_calls = {}  # config, shape and workspace bytes of the adapter calls seen, by their shapes
         self._norm_calls = {}  # the same of the calls on the norms
+        self._linear_shapes = {}  # semmoe_linear_shape by its fields
         self._c_config = None  # (values, C struct of them)
         if allocate_workspace:
             import torch
@@ -713,7 +714,8 @@ class SemMoE:
             return
         c = self._cfg()
         self._check("semmoe_quantize_rows", self.lib.semmoe_quantize_rows(
-            C.byref(c), _stream(), X.data_ptr(), n, cols, _row_distance(X, cols, "X"), _ptr(Xq), _ptr(x_scale)))
+            C.byref(c), _stream(), X.data_ptr(), n, cols, cols if X.is_contiguous() else _row_distance(X, cols, "X"), _ptr(Xq),
+            _ptr(x_scale)))
 
     def dispatch_rows_i8(self, Xq, x_scale, slot_of_pair, Xq_perm, x_scale_perm):
         T, d, P = self.cfg.T, self.cfg.d, self.cfg.T * self.cfg.k
@@ -735,7 +737,7 @@ class SemMoE:
     def linear_i8(self, Xq, x_scale, Wq, w_scale, Y):
         """Y[T,d_out] of Xq[T,d_in], Wq[d_out,d_in]; Xq and Y may be column ranges of wider tensors"""
         (n, d_in), d_out = Xq.shape, Wq.shape[0]
-        if tuple(Wq.shape) != (d_out, d_in) or tuple(Y.shape) != (n, d_out):
+        if Wq.shape != (d_out, d_in) or Y.shape != (n, d_out):
             raise SemMoEError("linear_i8: shapes must be Xq[T,d_in], Wq[d_out,d_in], Y[T,d_out]", -2)
         here, _, f32, acts = self._types
         dev, i8 = Xq.get_device(), self._torch.int8
@@ -746,7 +748,14 @@ class SemMoE:
             self._fit("linear_i8", ((Xq, i8, 0), (x_scale, f32, n), (Wq, i8, 0), (w_scale, f32, d_out), (Y, acts[1], 0)))
         if n == 0:
             return
-        c, s = self._cfg(), _CLinearShape(n, d_in, d_out, _row_distance(Xq, d_in, "Xq"), _row_distance(Y, d_out, "Y"))
+        key = (n, d_in, d_out, d_in if Xq.is_contiguous() else _row_distance(Xq, d_in, "Xq"),
+               d_out if Y.is_contiguous() else _row_distance(Y, d_out, "Y"))
+        s = self._linear_shapes.get(key)
+        if s is None:
+            if len(self._linear_shapes) >= 256:
+                self._linear_shapes.clear()
+            self._linear_shapes[key] = s = _CLinearShape(*key)
+        c = self._cfg()
         self._check("semmoe_linear_i8", self.lib.semmoe_linear_i8(
             C.byref(c), _stream(), C.byref(s), Xq.data_ptr(), _ptr(x_scale), _ptr(Wq), _ptr(w_scale), Y.data_ptr()))
 
@@ -756,10 +765,18 @@ class SemMoE:
         if P == 0:
             return
         here, i32, f32, acts = self._types
-        i8 = self._torch.int8
-        self._fit("expert_ffn_i8", ((Xq_perm, i8, P * d), (x_scale_perm, f32, P), (expert_offsets, i32, E + 1),
-                                    (expert_of_phys, i32, E), (Wq_gu, i8, 2 * F * d), (w_scale_gu, f32, 2 * F), (Wq_down, i8, F * d),
-                                    (w_scale_down, f32, d), (Y, acts[1], P * d)))
+        dev, i8 = Y.get_device(), self._torch.int8
+        if dev < 0 or dev != here() or not (
+                i8 is Xq_perm.dtype is Wq_gu.dtype is Wq_down.dtype and acts[1] is Y.dtype and i32 is expert_offsets.dtype is expert_of_phys.dtype
+                and f32 is x_scale_perm.dtype is w_scale_gu.dtype is w_scale_down.dtype
+                and dev == Xq_perm.get_device() == x_scale_perm.get_device() == expert_offsets.get_device() == expert_of_phys.get_device()
+                and dev == Wq_gu.get_device() == w_scale_gu.get_device() == Wq_down.get_device() == w_scale_down.get_device()
+                and Xq_perm.numel() >= P * d and x_scale_perm.numel() >= P and expert_offsets.numel() > E and expert_of_phys.numel() >= E
+                and Wq_gu.numel() >= 2 * F * d and w_scale_gu.numel() >= 2 * F and Wq_down.numel() >= F * d and w_scale_down.numel() >= d
+                and Y.numel() >= P * d):
+            self._fit("expert_ffn_i8", ((Xq_perm, i8, P * d), (x_scale_perm, f32, P), (expert_offsets, i32, E + 1),
+                                        (expert_of_phys, i32, E), (Wq_gu, i8, 2 * F * d), (w_scale_gu, f32, 2 * F), (Wq_down, i8, F * d),
+                                        (w_scale_down, f32, d), (Y, acts[1], P * d)))
         c = self._cfg()
         ws, n, owner = self._workspace("expert_ffn_i8", P * (3 * F + 4) + 1024)
         self._check("semmoe_expert_ffn_i8", self.lib.semmoe_expert_ffn_i8(
@@ -771,9 +788,16 @@ class SemMoE:
         if n == 0:
             return
         here, _, f32, acts = self._types
-        i8 = self._torch.int8
-        self._fit("shared_ffn_i8", ((Xq, i8, n * d), (x_scale, f32, n), (Wq_gu_sh, i8, 2 * F * d), (w_scale_gu_sh, f32, 2 * F),
-                                    (Wq_down_sh, i8, F * d), (w_scale_down_sh, f32, d), (Y_shared, acts[1], n * d)))
+        dev, i8 = Y_shared.get_device(), self._torch.int8
+        if dev < 0 or dev != here() or not (
+                i8 is Xq.dtype is Wq_gu_sh.dtype is Wq_down_sh.dtype and acts[1] is Y_shared.dtype
+                and f32 is x_scale.dtype is w_scale_gu_sh.dtype is w_scale_down_sh.dtype
+                and dev == Xq.get_device() == x_scale.get_device() == Wq_gu_sh.get_device() == w_scale_gu_sh.get_device()
+                and dev == Wq_down_sh.get_device() == w_scale_down_sh.get_device() and Xq.numel() >= n * d and x_scale.numel() >= n
+                and Wq_gu_sh.numel() >= 2 * F * d and w_scale_gu_sh.numel() >= 2 * F and Wq_down_sh.numel() >= F * d
+                and w_scale_down_sh.numel() >= d and Y_shared.numel() >= n * d):
+            self._fit("shared_ffn_i8", ((Xq, i8, n * d), (x_scale, f32, n), (Wq_gu_sh, i8, 2 * F * d), (w_scale_gu_sh, f32, 2 * F),
+                                        (Wq_down_sh, i8, F * d), (w_scale_down_sh, f32, d), (Y_shared, acts[1], n * d)))
         c = self._cfg()
         ws, size, owner = self._workspace("shared_ffn_i8", max(n, 0) * (3 * F + 4) + 1024)
         self._check("semmoe_shared_ffn_i8", self.lib.semmoe_shared_ffn_i8(
