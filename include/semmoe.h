@@ -600,7 +600,7 @@ int32_t semmoe_dispatch_rows_i8(const semmoe_config* cfg, void* stream, const vo
 /*
  * linear_i8 - a projection: Y[t,n] = x_scale[t] w_scale[n] sum_c Xq[t,c] Wq[n,c], rounded once.  cfg: dtype is used.
  * d_in % 16 == 0, at most SEMMOE_MAX_I8_DEPTH; d_out % 8 == 0.  ldx, ldy: distances of rows in elements, 0 = packed, multiples of 16
- * and of 8; w_scale lies on 16 bytes.  No workspace.
+ * and of 8, ldy (and d_out) below 2^26; w_scale lies on 16 bytes.  No workspace.
  * dev in : Xq[n_rows,d_in] i8; x_scale[n_rows] f32; Wq[d_out,d_in] i8; w_scale[d_out] f32.  dev out: Y[n_rows,d_out] bf16.
  */
 typedef struct semmoe_linear_shape {

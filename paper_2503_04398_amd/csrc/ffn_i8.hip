@@ -85,7 +85,7 @@ extern "C" int32_t semmoe_linear_i8(const semmoe_config* cfg, void* stream, cons
   if (st != SEMMOE_OK) return st;
   if (n.d_out % 8 != 0 || n.ldx % 16 != 0 || n.ldy % 8 != 0 || (n.ldx > 0 && n.ldx < n.d_in) || (n.ldy > 0 && n.ldy < n.d_out))
     return SEMMOE_ESHAPE;
-  if (n.n_rows > 0x3fffffff || n.ldx > 0x7fffffff || n.ldy > 0x7fffffff) return SEMMOE_EUNSUPPORTED;
+  if (n.n_rows > 0x3fffffff || n.ldx > 0x7fffffff || n.ldy >= 1 << 26 || n.d_out >= 1 << 26) return SEMMOE_EUNSUPPORTED;
   if (!Xq || !x_scale || !Wq || !w_scale || !Y) return SEMMOE_EINVAL;
   if (!aligned16(Xq) || !aligned16(Wq) || !aligned16(w_scale) || !aligned16(Y)) return SEMMOE_EINVAL;
   if (n.n_rows == 0) return SEMMOE_OK;

@@ -140,8 +140,14 @@ __device__ __forceinline__ int first_step(const GemmArgs& a, int widx, int elem_
 // feature tile runs fastest.  Returns total tile count.  `pre` is LDS of nq+1 ints.
 template <bool SIZED = false>
 __device__ __forceinline__ int build_tile_prefix(const GemmArgs& a, int n_ftiles, int* pre, int BT) {
-  // wave 0 scans: lane l owns groups [l*per, (l+1)*per)
   const int tid = threadIdx.x;
+  if (a.nq == 1) {
+    const int n = ((listed_rows<SIZED>(a, 0) + BT - 1) / BT) * n_ftiles;
+    if (tid < 2) pre[tid] = tid * n;
+    __syncthreads();
+    return n;
+  }
+  // wave 0 scans: lane l owns groups [l*per, (l+1)*per)
   if (tid < 64) {
     const int per = (a.nq + 63) / 64;
     const int lo = min(tid * per, a.nq), hi = min(lo + per, a.nq);

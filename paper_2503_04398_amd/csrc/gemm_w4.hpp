@@ -68,6 +68,12 @@ __device__ __forceinline__ float silu_mul_fast(float g, float u) {
   return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * g)) * u;
 }
 
+// 16 bytes of global memory at a uniform base: named so, for behind scalar_ptr the compiler would not know and use flat stores
+typedef __attribute__((address_space(1))) i32x4_t* global_i32x4_ptr;
+__device__ __forceinline__ global_i32x4_ptr global_i32x4(const unsigned char* base, uint32_t off) {
+  return (global_i32x4_ptr)((__attribute__((address_space(1))) unsigned char*)base + off);
+}
+
 // fragments of k that lie behind the end of the rows
 template <int N>
 __device__ __forceinline__ void clear_behind(bf16x8_t (&f)[N], bool behind) {
@@ -137,8 +143,9 @@ __device__ __forceinline__ TileRef locate_tile(const GemmArgs& a, const int* pre
 
 // KT (8-bit operands): K is no multiple of a slice.  The last slice's loads of what lies behind K fetch the slice's first chunk instead
 // (they stay inside the row), and those k of the token fragments are cleared before they are multiplied: integers times zero are zero.
+// Returns the number of tiles in the list.
 template <int MODE, int BK, int NSTAGE, int DMA_EVERY, int TJ = 4, bool KT = false>
-__device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned char* lds_raw) {
+__device__ __forceinline__ int gemm_bf16_w4_body(const GemmArgs& a, unsigned char* lds_raw) {
   using C = W4Cfg<MODE, BK, NSTAGE, DMA_EVERY, TJ>;
   // kModeLogits here: raw fp32 sums, no bias terms (the K-split router adds the parts and the biases afterwards)
   const unsigned lds_base = static_cast<unsigned>(reinterpret_cast<size_t>(lds_raw));
@@ -172,7 +179,7 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
   const int nk = (a.K + BK - 1) / BK;
   const int k_tail = (a.K - (nk - 1) * BK) * 2;  // bytes of a row in the last slice
   const ItemWalk my = xcd_share(total);
-  if (my.count == 0) return;  // whole workgroup: no barrier is pending
+  if (my.count == 0) return listed;  // whole workgroup: no barrier is pending
 
   // fragment-read geometry: lane reads row (lane & 31) of a 32-row MFMA tile, chunk 2*ks + lane/32
   const int frag_swz = ((lane & 31) / C::RPB) % C::CPR;
@@ -246,7 +253,7 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
       const int c = d_pos ^ (((sr + C::BW) / C::RPB) % C::CPR);
       return uint32_t(min(sr, t.n_tok - 1)) * uint32_t(a.ldx) * 2u + uint32_t(c) * 16u;
     };
-    i_k = first_step(a, t.widx, 2, nk);
+    i_k = KT ? 0 : first_step(a, t.widx, 2, nk);  // such rows are no multiple of 4 KB
     at_tail = false;
     i_base = (first_w ? w_panel : x_panel) + i_k * C::RB;
     if constexpr (TJ != 4) i_base2 = (loads_w ? w_panel : x_panel) + i_k * C::RB;
@@ -358,8 +365,8 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-    int c_left = KT ? nk - first_step(a, t.widx, 2, nk) : 0;  // slices to the row's end, the one being multiplied among them
-    for (int it = 0; it < nk; ++it) {
+    auto slice = [&](int it, auto tail_tag) __attribute__((always_inline)) {
+      constexpr bool kTail = decltype(tail_tag)::value;  // KT: the last slice
       const int n_stage = (c_stage + 1 == NSTAGE) ? 0 : c_stage + 1;
       // one k-step; the k-step index is a compile-time constant (a pragma-unrolled loop over it was left partly
       // rolled by the compiler, which turns the fragment buffers into scratch memory)
@@ -381,8 +388,7 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
         // one behind the first eight MFMAs: as a burst in front of the MFMAs they cost about 2 %
         const unsigned char* S_next = lds_raw + ((ks == kLast) ? n_stage : c_stage) * C::kStageBytes;
         const int off_next = ((((ks == kLast) ? 0 : ks + 1) * 2 + (lane >> 5)) ^ frag_swz) * 16;
-        if constexpr (KT)
-          if (c_left == 1) clear_behind(bfr[cur], (ks * 2 + (lane >> 5)) * 16 >= k_tail);
+        if constexpr (kTail) clear_behind(bfr[cur], (ks * 2 + (lane >> 5)) * 16 >= k_tail);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
@@ -420,8 +426,9 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
         k_step(std::integral_constant<int, 3>{});
       }
       c_stage = n_stage;
-      if (KT && --c_left == 0) c_left = nk;
-    }
+    };
+    for (int it = 0; it < nk - KT; ++it) slice(it, std::false_type{});
+    if constexpr (KT) slice(nk - 1, std::true_type{});
 
     // ---- epilogue: no barrier; the ring already holds the next tile's first slices
     bf16_t* out = static_cast<bf16_t*>(a.out);
@@ -462,6 +469,87 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
       }
       continue;
     }
+    if constexpr (kI8<MODE>) {
+      // Pass by pass as below, but the rows staged by a pass are stored in the middle of the next one: its arithmetic (a conversion and two
+      // products a sum) covers the way through LDS.  A wave's LDS operations complete in order, so that it reads the staged
+      // rows before it writes the next ones in their place.  The tokens are the inner loop: scales are read once for all of them.
+      constexpr int NB = kPaired<MODE> ? 1 : C::NB;  // with two there its scales spill
+      constexpr int kPasses = (kPaired<MODE> ? 2 : 4) / NB, kLpr = 4 * NB, kRpr = 64 / kLpr, kReads = 32 / kRpr;
+      constexpr int M = kPaired<MODE> ? 2 : 1;  // MFMA tiles behind a block of features
+      const int b_row = lane / kLpr, b_chunk = lane % kLpr;
+      const uint32_t lane_off = (uint32_t(b_row) * uint32_t(a.ldo) + b_chunk * 8) * 2u;  // 64 ldo < 2^32 (checked by the launcher)
+      unsigned char* const put = stg + tok_in * C::kStgRow + half * 8;
+      const unsigned char* const get = stg + b_row * C::kStgRow + b_chunk * 16;
+      float x_scale[TJ];
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) x_scale[j] = scales[C::BW + (j * 2 + wt) * 32 + tok_in];
+      const unsigned char* was = nullptr;  // where the staged rows go, how many of them there are
+      int was_left = 0;
+      bool was_in = false;
+#pragma unroll
+      for (int h = 0; h < kPasses; ++h) {
+        // a lane's four features of a token are 16 bytes of the weights' scales
+        const int f_wave = (kPaired<MODE> ? wf * 64 : wf * 128) + h * NB * 32;
+        f32x4_t ws[NB][4], us[kPaired<MODE> ? NB : 1][4];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int g4 = 0; g4 < 4; ++g4) {
+            const float* const from = scales + f_wave + b * 32 + g4 * 8 + half * 4;
+            ws[b][g4] = *reinterpret_cast<const f32x4_t*>(from);
+            if constexpr (kPaired<MODE>) us[b][g4] = *reinterpret_cast<const f32x4_t*>(from + C::BW / 2);
+          }
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) {
+          if (j >= nj) break;
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < M * NB; ++i) asm volatile("" : "+a"(acc[M * NB * h + i][j]));
+          i32x4_t staged[kReads];
+          if (h || j) {
+#pragma unroll
+            for (int p = 0; p < kReads; ++p) staged[p] = *reinterpret_cast<const i32x4_t*>(get + p * kRpr * C::kStgRow);
+          }
+          asm volatile("" ::: "memory");
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
+              float y[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                y[e] = scaled_sum(acc[M * (NB * h + b)][j][g4 * 4 + e], x_scale[j], ws[b][g4][e]);
+                if constexpr (kPaired<MODE>)
+                  y[e] = silu_mul_fast(y[e], scaled_sum(acc[M * (NB * h + b) + 1][j][g4 * 4 + e], x_scale[j], us[b][g4][e]));
+              }
+              *reinterpret_cast<uint2*>(put + (b * 4 + g4) * 16) = make_uint2(cvt_pk_bf16(y[0], y[1]), cvt_pk_bf16(y[2], y[3]));
+            }
+          asm volatile("" ::: "memory");
+          __builtin_amdgcn_wave_barrier();
+          if (h || j) {
+#pragma unroll
+            for (int p = 0; p < kReads; ++p)
+              if (was_in && p * kRpr + b_row < was_left)
+                *global_i32x4(scalar_ptr(was + size_t(p * kRpr) * a.ldo * 2), lane_off) = staged[p];
+          }
+          was = reinterpret_cast<const unsigned char*>(out + (size_t(t.row_lo) + (j * 2 + wt) * 32) * a.ldo + t.f0 + f_wave);
+          was_left = t.n_tok - (j * 2 + wt) * 32;
+          was_in = t.f0 + f_wave + b_chunk * 8 < a.N;
+        }
+      }
+      if (nj) {
+#pragma unroll
+        for (int p = 0; p < kReads; ++p) {
+          const i32x4_t v = *reinterpret_cast<const i32x4_t*>(get + p * kRpr * C::kStgRow);
+          if (was_in && p * kRpr + b_row < was_left)
+            *global_i32x4(scalar_ptr(was + size_t(p * kRpr) * a.ldo * 2), lane_off) = v;
+        }
+      }
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+      continue;
+    }
     constexpr int NB = MODE == kModeSwigluGrad ? 1 : C::NB;  // its two results and dh take the registers of a second block
     constexpr int kPasses = (kPaired<MODE> ? 2 : 4) / NB;  // 32*NB output features per pass
     // kModeSwigluGrad: a lane's part of dh for the pass to come, four features of a token 16 bytes
@@ -478,8 +566,6 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
 #pragma unroll
     for (int j = 0; j < TJ; ++j) {
       if (j >= nj) break;
-      float x_scale = 0.0f;
-      if constexpr (kI8<MODE>) x_scale = scales[C::BW + (j * 2 + wt) * 32 + tok_in];
 #pragma unroll
       for (int h = 0; h < kPasses; ++h) {
         // One pass at a time.  The accumulators of the pass are pinned to the accumulation registers up to
@@ -525,22 +611,6 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
               uint2 v;
               if constexpr (MODE == kModeSwigluGrad) {
                 v = dgu[part][b][g4];
-              } else if constexpr (kI8<MODE>) {
-                // a lane's four features of a token are 16 bytes of the weights' scales
-                const float* const ws = scales + (kPaired<MODE> ? wf * 64 : wf * 128) + (h * NB + b) * 32 + g4 * 8 + half * 4;
-                const f32x4_t s0 = *reinterpret_cast<const f32x4_t*>(ws);
-                float y[4];
-                if constexpr (kPaired<MODE>) {
-                  const f32x4_t s1 = *reinterpret_cast<const f32x4_t*>(ws + C::BW / 2);
-#pragma unroll
-                  for (int e = 0; e < 4; ++e)
-                    y[e] = silu_mul_fast(scaled_sum(acc[2 * (NB * h + b)][j][g4 * 4 + e], x_scale, s0[e]),
-                                         scaled_sum(acc[2 * (NB * h + b) + 1][j][g4 * 4 + e], x_scale, s1[e]));
-                } else {
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) y[e] = scaled_sum(acc[NB * h + b][j][g4 * 4 + e], x_scale, s0[e]);
-                }
-                v = make_uint2(cvt_pk_bf16(y[0], y[1]), cvt_pk_bf16(y[2], y[3]));
               } else if constexpr (MODE == kModeSwiglu) {
                 const f32x16_t& g = acc[2 * (NB * h + b)][j];
                 const f32x16_t& u = acc[2 * (NB * h + b) + 1][j];
@@ -574,6 +644,7 @@ __device__ __forceinline__ void gemm_bf16_w4_body(const GemmArgs& a, unsigned ch
     }
   }
   wait_vmcnt<0>();  // nothing may still be writing into this workgroup's LDS when it ends
+  return listed;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -667,7 +738,7 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
       }
     };
     int i_slice = 0, i_stage = 0;
-    int i_k = first_step(a, widx, 2, nk);  // place of the slice in K
+    int i_k = KT ? 0 : first_step(a, widx, 2, nk);  // place of the slice in K
     i_base += i_k * C::RB;
     bool i_done = false;
     unsigned i_dst = 0;
@@ -737,8 +808,8 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-    int c_left = KT ? nk - first_step(a, widx, 2, nk) : 0;
-    for (int it = 0; it < nk; ++it) {
+    auto slice = [&](auto tail_tag) __attribute__((always_inline)) {
+      constexpr bool kTail = decltype(tail_tag)::value;
       const int n_stage = (c_stage + 1 == NSTAGE) ? 0 : c_stage + 1;
       auto k_step = [&](auto ks_tag) __attribute__((always_inline)) {
         constexpr int ks = decltype(ks_tag)::value;
@@ -753,8 +824,7 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
         // the four fragment reads of the next k-step go out one by one behind the MFMAs
         const unsigned char* S_next = lds_raw + ((ks == 3) ? n_stage : c_stage) * C::kStageBytes;
         const int off_next = ((((ks == 3) ? 0 : ks + 1) * 2 + (lane >> 5)) ^ frag_swz) * 16;
-        if constexpr (KT)
-          if (c_left == 1) clear_behind(bfr[cur], (ks * 2 + (lane >> 5)) * 16 >= k_tail);
+        if constexpr (kTail) clear_behind(bfr[cur], (ks * 2 + (lane >> 5)) * 16 >= k_tail);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < TT; ++j) {
@@ -789,8 +859,9 @@ __device__ __forceinline__ void gemm_bf16_piece_body(const GemmArgs& a, unsigned
       k_step(std::integral_constant<int, 2>{});
       k_step(std::integral_constant<int, 3>{});
       c_stage = n_stage;
-      if (KT && --c_left == 0) c_left = nk;
-    }
+    };
+    for (int it = 0; it < nk - KT; ++it) slice(std::false_type{});
+    if constexpr (KT) slice(std::true_type{});
     wait_vmcnt<0>();   // the standing stream's last loads: nothing may write into the ring any more
     __syncthreads();   // every wave has left the ring: it now takes the output piece
     store_tile_via_lds<MODE, 2, 2, 2, TT>(acc, lds_raw, a, at.row_lo, at.n_tok, at.f0, wf, wt, widx);
@@ -827,7 +898,8 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_piece_kernel(GemmArgs a) {
 template <int MODE, int BK, int NSTAGE, int DMA_EVERY, int PIECE_RING, int TJ = 4, bool KT = false>
 __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_split_kernel(GemmArgs head, GemmArgs tail) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-  gemm_bf16_w4_body<MODE, BK, NSTAGE, DMA_EVERY, TJ, KT>(head, lds_raw);
+  const int listed = gemm_bf16_w4_body<MODE, BK, NSTAGE, DMA_EVERY, TJ, KT>(head, lds_raw);
+  if (listed == head_tiles(listed, int(gridDim.x), head.sched_thr)) return;  // no tile is left over (2 us of a launch)
   __syncthreads();  // the head's last output staging has been read
   // few parent tiles left over: 128 x 64 pieces, eight per parent tile, so that twice as many compute units take part
   // (a piece walks all of K however few there are: its time does not shrink with their number)

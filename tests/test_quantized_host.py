@@ -52,7 +52,8 @@ def test_dispatch_rows_i8_refuses():
 @pytest.mark.parametrize("kw,status", [
     (dict(n_rows=-1), EINVAL), (dict(d_in=0), EINVAL), (dict(d_out=-8), EINVAL), (dict(ldx=-16), EINVAL), (dict(ldy=-8), EINVAL),
     (dict(d_in=72), ESHAPE), (dict(d_out=36), ESHAPE), (dict(ldx=72), ESHAPE), (dict(ldx=48), ESHAPE), (dict(ldy=36), ESHAPE),
-    (dict(ldy=24), ESHAPE), (dict(d_in=131072), EUNSUPPORTED), (dict(n_rows=0x40000000), EUNSUPPORTED), (dict(n_rows=0), 0),
+    (dict(ldy=24), ESHAPE), (dict(d_in=131072), EUNSUPPORTED), (dict(n_rows=0x40000000), EUNSUPPORTED),
+    (dict(ldy=1 << 26), EUNSUPPORTED), (dict(d_out=1 << 26), EUNSUPPORTED), (dict(ldx=1 << 31), EUNSUPPORTED), (dict(n_rows=0), 0),
 ])
 def test_linear_i8_refuses_shapes(kw, status):
     lib, c, p, _keep = _lib()
