@@ -575,8 +575,8 @@ int32_t semmoe_adapters_grad(const semmoe_config* cfg, void* stream, const semmo
 /*
  * The layer in 8-bit integers, with a scale for each row of activations (token) and of weights (output channel):
  *   quantize_rows, or block_norm's Xq  ->  linear_i8, shared_ffn_i8,  dispatch_rows_i8 -> expert_ffn_i8  (-> combine)
- * A row x in 8 bits is q = rint(x * (127 / max|x|)), ties to even, and scale = max|x| / 127 (fp32; zero rows: 0 and 0); x is within
- * max|x| / 254 of scale * q.  A row with an infinity or a NaN has scale NaN and q = 0, and so have the results made of it.  The
+ * A row x in 8 bits is q = rint(x * ((1 / max|x|) * 127)), ties to even, and scale = max|x| * (1 / 127) in fp32 operations (zero
+ * rows: 0 and 0); x is within max|x| / 254 of scale * q, but for these operations' roundings.  A row with an infinity or a NaN has scale NaN and q = 0, and so have the results made of it.  The
  * products take any int8 values and scales; sums are int32 and exact.  Results are bf16: cfg->dtype is SEMMOE_BF16 in the calls
  * that multiply (else SEMMOE_EUNSUPPORTED), either type in quantize_rows.
  */

@@ -9,17 +9,18 @@ import numpy as np
 
 
 def quantize_rows(x):
-    """(q int8, scale float32) in the sequence of fp32 operations that the definition names: 127 / amax, the product, rint; rows
-    whose amax lies below 2^-64 times 2^64"""
+    """(q int8, scale float32) in the sequence of fp32 operations that the definition names: 1 / amax, times 127, the product, rint;
+    rows whose amax lies below 2^-64 times 2^64, above 2^64 times 2^-64"""
     x = np.asarray(x, dtype=np.float32)
-    amax = np.abs(x).max(1) if x.shape[1] else np.zeros(x.shape[0], np.float32)
+    f = np.float32
+    amax = np.abs(x).max(1) if x.shape[1] else np.zeros(x.shape[0], f)
     bad = ~np.isfinite(x).all(1)
-    amax = np.where(bad, np.float32(1), amax).astype(np.float32)
-    pre = np.where(amax < np.float32(2.0 ** -64), np.float32(2.0 ** 64), np.float32(1))
+    amax = np.where(bad, f(1), amax).astype(f)
+    pre = np.where(amax < f(2.0 ** -64), f(2.0 ** 64), np.where(amax > f(2.0 ** 64), f(2.0 ** -64), f(1))).astype(f)
     with np.errstate(divide="ignore", invalid="ignore"):
-        r = np.where(amax > 0, np.float32(127) / (amax * pre), np.float32(0)).astype(np.float32)
-        q = np.rint((x * pre[:, None]).astype(np.float32) * r[:, None])
-        scale = (amax / np.float32(127)).astype(np.float32)
+        r = np.where(amax > 0, (f(1) / (amax * pre)).astype(f) * f(127), f(0)).astype(f)
+        q = np.rint((x * pre[:, None]).astype(f) * r[:, None])
+        scale = (amax * (f(1) / f(127))).astype(f)
     q[bad], scale[bad] = 0, np.nan
     return q.astype(np.int8), scale
 

@@ -55,22 +55,21 @@ __device__ __forceinline__ void team_join(V (&v)[N], V* part, int team_waves, F 
 
 __device__ __forceinline__ uint32_t magnitude_bits(float f) { return __float_as_uint(f) & 0x7fffffffu; }
 
-// A row in 8 bits: scale = amax / 127, q = rint(x * (127 / amax)), ties to even; amax by its bits, so that NaN is more than any
-// number.  A row with an infinity or a NaN has scale NaN and q = 0: whatever is multiplied with it is NaN.  127 / amax leaves fp32
-// where amax is below 2^-121: such rows are taken times 2^64, which is exact.
+// A row in 8 bits: scale = amax * (1 / 127), q = rint(x * ((1 / amax) * 127)), ties to even; amax by its bits, so that NaN is more than
+// any number.  A row with an infinity or a NaN has scale NaN and q = 0: whatever is multiplied with it is NaN.  The reciprocal keeps
+// its bits where amax lies between 2^-64 and 2^64; rows beyond are taken times 2^64 or 2^-64, which loses nothing that q holds.
 struct RowScale {
-  float scale, r;
-  bool small, bad;
+  float scale, r, pre;
+  bool bad;
   __device__ __forceinline__ explicit RowScale(uint32_t amax_bits) {
     const float amax = __uint_as_float(amax_bits);
     bad = amax_bits >= 0x7f800000u;
-    small = amax < 0x1p-64f;
-    const float a = small ? amax * 0x1p64f : amax;
-    r = a > 0.0f ? 127.0f / a : 0.0f;
-    scale = bad ? __uint_as_float(0x7fc00000u) : amax / 127.0f;
+    pre = amax < 0x1p-64f ? 0x1p64f : amax > 0x1p64f ? 0x1p-64f : 1.0f;
+    r = amax > 0.0f ? 1.0f / (amax * pre) * 127.0f : 0.0f;
+    scale = bad ? __uint_as_float(0x7fc00000u) : amax * (1.0f / 127.0f);
   }
   __device__ __forceinline__ uint32_t q(float x) const {
-    const int v = bad ? 0 : __float2int_rn((small ? x * 0x1p64f : x) * r);
+    const int v = bad ? 0 : __float2int_rn(x * pre * r);
     return uint32_t(v) & 255u;
   }
   // N numbers at `to`, which lies on N bytes

@@ -1,8 +1,9 @@
 // Rows in 8-bit integers with a scale each: quantize_rows and the row moves of dispatch on such rows.
 //
-//   scale = max |x| / 127,   q = rint(x * (127 / max |x|))
+//   scale = max |x| * (1 / 127),   q = rint(x * ((1 / max |x|) * 127))
 // Both stream: a row is read once into registers, its largest magnitude found, and written as a byte a number.  A number's error is
-// at most half a step, max |x| / 254, beside which the two roundings of the factor and the product (2^-23 of the value) are nothing.
+// at most half a step, max |x| / 254, beside which the roundings of the factor and the product (2^-24 each) are nothing but for a
+// number on the border of two steps, such as half of the largest one, which may go either way.
 #include "rows.hpp"
 
 namespace semmoe {

@@ -354,8 +354,8 @@ def test_block_norm(T, d, dtype):
     _within(X[:T], *b["X"], "X")
     want, dX = b["X32"]
     step = _np(s[:T])[:, None]
-    _within(_np(Xq[:T]) * step, want, step * 0.5 + dX + 4 * E32 * np.abs(want), "Xq")
-    assert np.abs(_np(s[:T]) * 127 - np.abs(want).max(1)).max() <= (dX.max(1) + 2 * E32 * np.abs(want).max(1)).max()
+    _within(_np(Xq[:T]) * step, want, step * 0.5 + dX + 6 * E32 * np.abs(want), "Xq")
+    assert np.abs(_np(s[:T]) * 127 - np.abs(want).max(1)).max() <= (dX.max(1) + 3 * E32 * np.abs(want).max(1)).max()
     assert (np.abs(_np(Xq[:T])).max(1) == 127).all()
     assert (H[T] == 7.0).all() and (X[T] == 7.0).all() and (Xq[T] == 77).all() and s[T] == 7.0
     # the parts alone give the same bits

@@ -11,16 +11,17 @@ def test_rows_in_8_bits_lie_within_half_a_step():
     x[3] = 0
     q, scale = Q.quantize_rows(x)
     assert (np.abs(q).max(1)[np.arange(50) != 3] == 127).all() and (q[3] == 0).all() and scale[3] == 0
-    # the factor and the product are rounded (2^-24 each, of at most 127), the scale as well
-    assert (np.abs(q * scale[:, None].astype(np.float64) - x) <= scale[:, None] * (0.5 + 3 * 127 * 2.0 ** -24)).all()
+    # the reciprocal, the factor, the product and the scale's factor and product are rounded (2^-24 each, of at most 127)
+    assert (np.abs(q * scale[:, None].astype(np.float64) - x) <= scale[:, None] * (0.5 + 5 * 127 * 2.0 ** -24)).all()
 
 
 def test_ties_are_even_and_tiny_rows_keep_their_numbers():
-    x = np.array([[254.0, 1.0, 3.0, 5.0, -1.0, -3.0, 2.0, 0.0]], np.float32)  # a step of 2
+    x = np.array([[128.0, 64.0, -64.0, 32.0, 1.0, -1.0, 0.5, 0.0]], np.float32)  # steps of 128 / 127: 64 is 63.5 of them
     q, scale = Q.quantize_rows(x)
-    assert q.tolist() == [[127, 0, 2, 2, 0, -2, 1, 0]] and scale[0] == 2.0
-    q2, scale2 = Q.quantize_rows(x * np.float32(2.0 ** -140))
-    assert (q2 == q).all() and scale2[0] == np.float32(2.0 ** -139)
+    assert q.tolist() == [[127, 64, -64, 32, 1, -1, 0, 0]] and abs(scale[0] - 128 / 127) < 2.0 ** -23
+    for e in (-140, -133, -100, 100, 120):
+        q2, scale2 = Q.quantize_rows(x * np.float32(2.0) ** e)
+        assert (q2 == q).all() and abs(scale2[0] / 2.0 ** e - 128 / 127) < (2.0 ** -23 if e > -120 else 2.0 ** -9)
 
 
 @pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
