@@ -524,11 +524,13 @@ static int32_t launch_bf16_tile(int id, const GemmArgs& a, int max_rows, int bpc
 // it: 45 83 179 as 256 x 128 tiles, 66 112 236 as 256 x 256, 37 105 234 as pieces.  256 x 256 tiles are ahead of 256 x 128
 // from three fifths of the compute units on (170 to 190 of them: 2 to 4 %; 130 to 150: 2 % behind); 2514 rows of d 6968,
 // F 1312, gate/up without whole slices: 248 us for the FFN with pieces, 331 with 256 x 256 tiles on less than half of the chip.
-// tails: the tiles with a running load stream take any K (8-bit operands)
+// tails: the tiles with a running load stream take any K (8-bit operands; rows that are no whole 128 bytes go to the staged tiles all the
+// same: 128 experts of 16 rows, d = F = 2880 in 8 bits, 662 us with 64 x 64 streamed, 630 so)
 static int default_tile(const GemmArgs& a, int max_rows, int est_rows_per_group, int w_rows, bool tails = false) {
   const int est = est_rows_per_group, t256 = cdiv(w_rows, 256);
   const long long cus = num_cu();
-  const bool whole_slices = (tails || a.K % 64 == 0) && cdiv(a.K, 64) >= 3;  // what the tiles with a running load stream need
+  const bool aligned = a.K % 64 == 0;
+  const bool whole_slices = (tails || aligned) && cdiv(a.K, 64) >= 3;  // what the tiles with a running load stream need
   const int big_tile = (long long)(max_rows / 256 + a.nq) * t256 * 2 >= cus ? 22 : 28;
   if (!a.offsets) {
     auto tiles = [&](int w, int t) { return (long long)cdiv(w_rows, w) * cdiv(est, t); };
@@ -556,7 +558,7 @@ static int default_tile(const GemmArgs& a, int max_rows, int est_rows_per_group,
     if (whole_slices && w4_room && (all_rows ? est >= 34 && a.K >= 1024 && mid >= full * cus
                                              : est >= 20 && mid * 8 >= 5 * cus && mid <= cus && a.K >= 2560))
       return 33;
-    if (!whole_slices || (est >= 20 && !all_rows)) return 26;
+    if (!aligned || !whole_slices || (est >= 20 && !all_rows)) return 26;
     if (pow2 && (est < 34 || a.K >= 4096 || mid >= cus)) return 35;
     const bool one_each = ring * 2 > cus && ring <= cus;
     if (est < 20) return a.K >= (ring * 2 <= cus ? 640 : (one_each ? 2560 : 960)) ? 35 : 26;
