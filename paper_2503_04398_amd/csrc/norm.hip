@@ -341,7 +341,7 @@ static int32_t check_norm(const semmoe_config* cfg, const semmoe_norm_shape* n, 
   if (cfg->T < 0 || cfg->d <= 0) return SEMMOE_EINVAL;
   if (!(n->eps_post >= 0.0f) || !(n->eps_pre >= 0.0f)) return SEMMOE_EINVAL;
   if (cfg->d % 8 != 0) return SEMMOE_ESHAPE;
-  if (cfg->d > SEMMOE_MAX_NORM_D) return SEMMOE_EUNSUPPORTED;
+  if (cfg->d > SEMMOE_MAX_NORM_D || cfg->T > 0x3fffffff) return SEMMOE_EUNSUPPORTED;
   for (int64_t ld : lds) {
     if (ld < 0) return SEMMOE_EINVAL;
     if (ld % 8 != 0 || (ld > 0 && ld < cfg->d)) return SEMMOE_ESHAPE;

@@ -132,6 +132,7 @@ extern "C" int32_t semmoe_quantize_rows(const semmoe_config* cfg, void* stream, 
   if (cfg->dtype != SEMMOE_FP32 && cfg->dtype != SEMMOE_BF16) return SEMMOE_EUNSUPPORTED;
   if (!X || !Xq || !x_scale || n_rows < 0 || n_cols <= 0 || ldx < 0) return SEMMOE_EINVAL;
   if (n_cols % 8 != 0 || ldx % 8 != 0 || (ldx > 0 && ldx < n_cols)) return SEMMOE_ESHAPE;
+  if (n_rows > 0x3fffffff) return SEMMOE_EUNSUPPORTED;
   if (!aligned16(X) || !aligned16(Xq)) return SEMMOE_EINVAL;
   if (n_rows == 0) return SEMMOE_OK;
   return launch_quantize_rows(cfg->dtype == SEMMOE_BF16, X, ldx ? ldx : n_cols, n_rows, n_cols, nullptr, 0, Xq, x_scale,

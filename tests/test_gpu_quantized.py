@@ -123,7 +123,7 @@ def test_dispatch_rows_i8(T, k, d):
 # ---- products
 LINEAR = [(1, 16, 8), (1, 4096, 64), (5, 272, 200), (16, 512, 1032), (31, 2880, 304), (33, 1040, 128), (64, 4096, 512), (65, 192, 2056),
           (130, 1024, 264), (200, 7168, 136), (257, 48, 520), (300, 2064, 1040), (777, 640, 328), (1025, 384, 512), (2000, 2048, 264),
-          (3001, 256, 1536), (4096, 512, 4096)]
+          (3001, 256, 1536), (4096, 512, 4096), (3000, 16, 3000), (3000, 48, 2048), (5000, 144, 4104), (2600, 256, 2600)]
 
 
 @pytest.mark.parametrize("T,d_in,d_out", LINEAR)
@@ -155,6 +155,51 @@ def test_linear_i8_of_partial_slices(T, d_out, d_in):
 @pytest.mark.parametrize("rows", [[45] * 8, [130, 0, 257, 64, 1, 300], [700, 300, 900]])
 def test_expert_ffn_i8_of_partial_slices(rows, d, F):
     _experts(rows, d, F, seed=5)
+
+
+SHAPES = [0, 16, 22, 26, 28, 30, 31, 32, 33, 34, 35, 38, 39, 40, 7]  # the last one is none of theirs
+
+
+@pytest.mark.parametrize("d,F", [(512, 384), (400, 272), (48, 32)])
+@pytest.mark.parametrize("tile", SHAPES)
+def test_every_tile_shape(tile, d, F):
+    m = _m()
+    try:
+        m.set_tuning(0, tile)
+        m.set_tuning(1, tile)
+        _experts(RAGGED + [520, 129], d, F, seed=tile)
+    finally:
+        m.set_tuning(0, -1)
+        m.set_tuning(1, -1)
+
+
+@pytest.mark.parametrize("ring,grid,cut", [(-1, 16, -1), (1, 16, 16), (2, 24, 16), (3, 16, 16), (6, 16, 16), (-1, 8, 0), (-1, 40, 16)])
+@pytest.mark.parametrize("tile", [22, 33, 16])
+@pytest.mark.parametrize("d,F", [(512, 640), (720, 464)])
+def test_tiles_and_pieces_in_every_form_of_launch(tile, ring, grid, cut, d, F):
+    m = _m()
+    knobs = {0: tile, 1: tile, 4: grid, 5: cut, 6: ring}
+    try:
+        for key, v in knobs.items():
+            m.set_tuning(key, v)
+        _experts([300, 0, 700, 33, 257, 1], d, F, seed=ring + 7)
+    finally:
+        for key in knobs:
+            m.set_tuning(key, -1)
+
+
+@pytest.mark.parametrize("T,d_out", [(40, 512), (300, 2048), (700, 4096)])
+def test_linear_i8_of_rows_far_apart(T, d_out):
+    """rows of a tile that 32-bit offsets do not reach"""
+    r = np.random.default_rng(T)
+    (q, s), (w, ws) = _quantized(r, T, 512), _quantized(r, d_out, 512)
+    wide = torch.zeros(T, 1 << 24, dtype=torch.int8, device=DEV)
+    wide[:, 64:576] = q
+    Y, Z = (torch.empty(T, d_out, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    m = _m()
+    m.linear_i8(wide[:, 64:576], s, w, ws, Y)
+    m.linear_i8(q, s, w, ws, Z)
+    assert torch.equal(Y, Z)
 
 
 def test_linear_i8_sums_are_exact():

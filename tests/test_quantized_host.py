@@ -30,6 +30,7 @@ def test_quantize_rows_refuses():
     assert call(cols=60) == call(ldx=68) == call(ldx=56) == ESHAPE
     assert lib.semmoe_quantize_rows(None, None, p, 4, 64, 0, p, p) == EINVAL
     assert call(n=0) == 0
+    assert call(n=0x40000000) == EUNSUPPORTED
     c.dtype = 7
     assert call() == EUNSUPPORTED
 
@@ -157,7 +158,7 @@ def test_norms_refuse_sizes():
         assert lib.semmoe_block_norm(C.byref(c), None, C.byref(_norm(**kw)), *forward) == status
     for kw, status in ((dict(ld_dh=-8), EINVAL), (dict(ld_dgate=68), ESHAPE), (dict(ld_dy=56), ESHAPE)):
         assert lib.semmoe_block_norm_grad(C.byref(c), None, C.byref(_norm(**kw)), *backward, p, 1 << 30) == status
-    for field, value, status in (("d", 60, ESHAPE), ("d", 16392, EUNSUPPORTED), ("d", 0, EINVAL), ("T", -1, EINVAL), ("dtype", 3, EUNSUPPORTED)):
+    for field, value, status in (("d", 60, ESHAPE), ("d", 16392, EUNSUPPORTED), ("d", 0, EINVAL), ("T", -1, EINVAL), ("T", 0x40000000, EUNSUPPORTED), ("dtype", 3, EUNSUPPORTED)):
         lib, c, p, _keep = _lib()
         setattr(c, field, value)
         assert lib.semmoe_block_norm(C.byref(c), None, C.byref(s), *forward) == status
