@@ -349,11 +349,20 @@ static int32_t check_norm(const semmoe_config* cfg, const semmoe_norm_shape* n, 
   return SEMMOE_OK;
 }
 
-static RowTeams norm_grad_teams(const semmoe_config* cfg) { return RowTeams(cfg->dtype == SEMMOE_BF16, cfg->d, 1024); }
+// The backward pass' kernel holds 128 registers a thread: 16 waves a compute unit.  Workgroups of 8 waves, two a compute unit, as many
+// teams in each as fit: their sums meet in LDS, and the rows of partial sums are fewer (16384 rows of 2048: 93 us, one team a workgroup
+// of 4 waves 112; as 16 waves 103).  A team of more than 8 waves is a workgroup, one a compute unit (4096 rows of 7168: 104 us, with twice
+// as many workgroups 118).
+static RowTeams norm_grad_teams(const semmoe_config* cfg) {
+  RowTeams g(cfg->dtype == SEMMOE_BF16, cfg->d, 1024);
+  g.teams = g.tr > 256 ? 1 : 512 / g.tr;
+  return g;
+}
 
 static size_t norm_groups(const semmoe_config* cfg) {
-  const int rows = cdiv(cfg->T, norm_grad_teams(cfg).teams);
-  return rows < kNormGradGroups ? rows : kNormGradGroups;
+  const RowTeams g = norm_grad_teams(cfg);
+  const int rows = cdiv(cfg->T, g.teams), most = g.tr > 512 ? kNormGradGroups / 2 : kNormGradGroups;
+  return rows < most ? rows : most;
 }
 
 }  // namespace semmoe
