@@ -94,6 +94,8 @@ int32_t semmoe_workspace_bytes(const semmoe_config* cfg, size_t* bytes_out /*hos
  *     (the default for middling groups with tiles for the whole chip);
  *     20, 21, 22: four waves on a 256 x 256 tile with loads placed between the MFMAs; K must be a multiple of the
  *     K slice (32 for 20 and 21, 64 for 22) and hold at least a ring of slices (128); other K run as 16).
+ *     8-bit products follow the two knobs with 0, 16, 22, 26, 28, 30 to 35 and 38 to 40 (K counted in pairs of integers; 22, 28 and 33 take
+ *     any K); other ids leave the choice to the library.
  *     In fp32 (the router's GEMM follows SEMMOE_TUNE_GATEUP_TILE) 30, 31, 32 are the same shapes, 36 is 32 weight rows x 16
  *     tokens and 37 that with 64-bit addresses (the default for weight panels of 2 GiB); other ids leave the choice to
  *     the library

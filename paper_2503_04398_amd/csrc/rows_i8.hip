@@ -4,6 +4,7 @@
 // Both stream: a row is read once into registers, its largest magnitude found, and written as a byte a number.  A number's error is
 // at most half a step, max |x| / 254, beside which the roundings of the factor and the product (2^-24 each) are nothing but for a
 // number on the border of two steps, such as half of the largest one, which may go either way.
+// Measured: 8192 rows of 7168 bf16 34 to 36 us, 5.0 to 5.2 TB/s; the moves of 8192 rows of 2048 to 8 places each 25.5 us, 5.9 TB/s.
 #include "rows.hpp"
 
 namespace semmoe {
