@@ -382,7 +382,7 @@ extern "C" int32_t semmoe_block_norm(const semmoe_config* cfg, void* stream, con
     if (!aligned16(p)) return SEMMOE_EINVAL;
   if (cfg->T == 0) return SEMMOE_OK;
   const bool bf = cfg->dtype == SEMMOE_BF16;
-  const RowTeams g(bf, cfg->d, bf ? 512 : 1024);
+  const RowTeams g(bf, cfg->d);
   NormArgs a{};
   a.n_rows = cfg->T; a.d = cfg->d; a.tr = g.tr;
   a.res_scale = n->res_scale; a.eps_post = n->eps_post; a.eps_pre = n->eps_pre;

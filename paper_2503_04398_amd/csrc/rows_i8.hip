@@ -74,7 +74,7 @@ int32_t launch_quantize_rows(bool bf16, const void* X, int64_t ldx, int n_rows, 
   // A wave a row where four pieces a thread hold it: no barrier (20865 rows of 768: 13.7 -> 11.2 us, 8192 of 2048: 12.3 -> 11.8; few
   // rows: no difference).
   const bool short_rows = n_cols <= (bf16 ? 2048 : 1024);
-  const RowTeams g(bf16, n_cols, short_rows ? 64 : bf16 ? 512 : 1024);
+  const RowTeams g = short_rows ? RowTeams(bf16, n_cols, 64) : RowTeams(bf16, n_cols);
   const long long groups = cdiv(n_rows, g.teams), most = (long long)dev.num_cu * 8;
   const int grid = int(groups < most ? groups : most);
 #define SEMMOE_QUANTIZE(BF_, NP_)                                                                                             \
