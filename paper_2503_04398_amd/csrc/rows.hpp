@@ -91,7 +91,8 @@ struct RowTeams {
     teams = tr >= 256 ? 1 : 256 / tr;
   }
   // 512 threads where four pieces each hold the row: several such teams a compute unit are at different steps (norms of 20297 rows of
-  // 3632 in fp32 228 us, 276 with up to 1024 threads; of 16384 rows of 7168 in bf16 195 and 244)
+  // 3632 in fp32 228 us, 276 with up to 1024 threads; of 16384 rows of 7168 in bf16 195 and 244;
+  // 20297 rows of 3632 in fp32 to 8 bits 72 and 88).  1024 beyond it: 4096 rows of 32768 in bf16 to 8 bits 88 us, read twice 102.
   RowTeams(bool bf16, int n_cols) : RowTeams(bf16, n_cols, n_cols / (bf16 ? 8 : 4) <= 2048 ? 512 : 1024) {}
 };
 

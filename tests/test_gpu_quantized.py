@@ -56,7 +56,7 @@ def _within(got, want, bound, what):
 # ---- rows in 8 bits
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("n,cols", [(1, 8), (3, 64), (5, 504), (130, 512), (33, 520), (7, 2048), (9, 4096), (4, 4104), (3, 8200), (2, 16384),
-                                    (2, 16392), (3, 40000), (5000, 24)])
+                                    (2, 16392), (3, 40000), (5000, 24), (9, 3632), (3, 24584), (2, 32768), (2, 32776)])
 def test_quantize_rows(n, cols, dtype):
     r = np.random.default_rng(n + cols)
     X = _rand(r, (n, cols), dtype) * torch.from_numpy(2.0 ** r.integers(-20, 20, (n, 1))).to(_act(dtype))
