@@ -218,24 +218,28 @@ __global__ __launch_bounds__(1024, 4) void block_norm_grad_kernel(const NormArgs
     const float rh = 1.0f / sqrtf(s[0] * inv_d + a.eps_pre), ch = s[1] * rh * inv_d;
     const float ry = a.w_post ? 1.0f / sqrtf(s[2] * inv_d + a.eps_post) : 1.0f;
     float dh[NP][N], e[1] = {0.0f};
+    // A team without a row adds nothing to the sums: its zeros times the root's reciprocal, infinite where eps is 0, or times an infinite
+    // weight would be NaN.
+    if (have) {
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
+      for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int x = 0; x < N; ++x) {
-        float u = v.d[p][x];
-        if (a.dX) {
-          const float xn = v.h[p][x] * rh;
-          u += rh * (v.x[p][x] * wq[p][x] - xn * ch);
-          sq[p][x] = fmaf(v.x[p][x], xn, sq[p][x]);
+        for (int x = 0; x < N; ++x) {
+          float u = v.d[p][x];
+          if (a.dX) {
+            const float xn = v.h[p][x] * rh;
+            u += rh * (v.x[p][x] * wq[p][x] - xn * ch);
+            sq[p][x] = fmaf(v.x[p][x], xn, sq[p][x]);
+          }
+          dh[p][x] = u;
+          const float yn = v.y[p][x] * ry, b = a.gate ? u * g[p][x] : u;
+          if (a.w_post) {
+            e[0] = fmaf(b * wp[p][x], yn, e[0]);
+            sp[p][x] = fmaf(b, yn, sp[p][x]);
+          }
+          if constexpr (!GATES) sg[p][x] = fmaf(u, a.w_post ? yn * wp[p][x] : yn, sg[p][x]);
         }
-        dh[p][x] = u;
-        const float yn = v.y[p][x] * ry, b = a.gate ? u * g[p][x] : u;
-        if (a.w_post) {
-          e[0] = fmaf(b * wp[p][x], yn, e[0]);
-          sp[p][x] = fmaf(b, yn, sp[p][x]);
-        }
-        if constexpr (!GATES) sg[p][x] = fmaf(u, a.w_post ? yn * wp[p][x] : yn, sg[p][x]);
-      }
+    }
     if (a.w_post) team_join(e, part + 48, tw, add_f);
     else if (tw > 1) __syncthreads();  // `part` has been read
 #pragma unroll

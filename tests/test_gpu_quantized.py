@@ -565,6 +565,49 @@ def test_block_norm_grad_in_place_and_of_wider_tensors(dtype):
         assert torch.equal(outs[n], got[n]), n
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("gate", ["rows", "one", None])
+@pytest.mark.parametrize("T,d", [(1, 64), (7, 512), (777, 512), (5, 1000), (2, 1024), (301, 136), (3, 2048)])
+def test_norms_without_eps(T, d, gate, dtype, monkeypatch):
+    """eps 0, and fewer rows than the teams of the last workgroup: no row there is may be divided by zero, and none that isn't counts"""
+    monkeypatch.setitem(PAR, "eps_post", 0.0)
+    monkeypatch.setitem(PAR, "eps_pre", 0.0)
+    r = np.random.default_rng(T + d)
+    c, g = _grad_case(r, T, d, dtype, gate=gate)
+    m, outs = _m(T=T, d=d, dtype=dtype), _outs(c, T, d, dtype)
+    _grad(m, c, g, **outs)
+    want = _norm_grad_bounds(c, g, gate == "rows", dtype)
+    for n in outs:
+        _within(outs[n], *want[n], n)
+    c["R"] = _rand(r, (T, d), dtype, 3.0).to(DEV)
+    H, X = torch.empty_like(c["R"]), torch.empty_like(c["R"])
+    m.block_norm(c["R"], H, Y=c["Y"], X=X, w_post=c["w_post"], w_pre=c["w_pre"], gate=c["gate"], **PAR)
+    c = {n: c[n] for n in ("R", "Y", "w_post", "gate", "w_pre")}
+    b = _norm_bounds(c, dtype)
+    _within(H, *b["H"], "H")
+    _within(X, *b["X"], "X")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,d", [(7, 512), (2, 1000), (301, 136)])
+def test_infinite_weights_are_not_multiplied_with_rows_that_are_not_there(T, d, dtype):
+    """a channel whose gate or weight is infinite and whose products are positive has an infinite gradient, as the formula says"""
+    c, g = _grad_case(np.random.default_rng(T + d), T, d, dtype, gate="one", without=("w_pre",))
+    g["dX"] = None
+    for t in (g["dH"], c["Y"]):
+        t[:, 5] = t[:, 5].abs() + 0.5
+    m = _m(T=T, d=d, dtype=dtype)
+    clean = _outs(c, T, d, dtype)
+    _grad(m, c, g, **clean)
+    for infinite, result in (("gate", "dw_post"), ("w_post", "dgate")):
+        c2, out = {**c, infinite: c[infinite].clone()}, torch.empty_like(clean[result])
+        c2[infinite][5] = float("inf")
+        _grad(m, c2, g, **{result: out})
+        assert out[5] == float("inf")
+        out[5] = clean[result][5]
+        assert torch.equal(out, clean[result])
+
+
 def test_norms_of_rows_that_are_no_numbers():
     T, d = 40, 512
     r = np.random.default_rng(5)
