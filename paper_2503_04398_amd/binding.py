@@ -807,12 +807,12 @@ class SemMoE:
     # -- the norms around a block
     def _norm_call(self, call, T, d, par, gate, vectors, rows):
         """(config, shape) of a call on the norms: made and checked once for shapes, distances of rows and par (res_scale, eps_post,
-        eps_pre), which every layer of a step repeats.  vectors are w_post and w_pre with the gradients of such; rows the tensors [T,d]
-        by the name of their distance.  A gate of one dimension is all rows' (its gradient then is one row, too)."""
+        eps_pre), which every layer of a step repeats.  vectors are w_post and w_pre with the gradients of such, and a gate of one
+        dimension with its gradient, which are all rows'; rows the tensors [T,d] by the name of their distance."""
         s = _CNormShape(*par, int(gate is not None and gate.dim() == 2))
         for t in vectors:
-            if t is not None and tuple(t.shape) != (d,):
-                raise SemMoEError("%s: a norm's weights and a gate of all rows have %d numbers" % (call, d), -2)
+            if t is not None and (tuple(t.shape) != (d,) or not t.is_contiguous()):
+                raise SemMoEError("%s: a norm's weights, a gate of all rows and their gradients are %d numbers behind one another" % (call, d), -2)
         for name, t in rows:
             if t is not None:
                 if tuple(t.shape) != (T, d):
@@ -875,7 +875,7 @@ class SemMoE:
         def make():
             if dgate is not None and (gate is None or dgate.shape != gate.shape):
                 raise SemMoEError("block_norm_grad: dgate has gate's shape", -2)
-            c, s = self._norm_call("block_norm_grad", T, d, par, gate, (w_post, w_pre, dw_post, dw_pre, gate if of_all else None), (
+            c, s = self._norm_call("block_norm_grad", T, d, par, gate, (w_post, w_pre, dw_post, dw_pre, *((gate, dgate) if of_all else ())), (
                 ("ld_dh", dH), ("ld_dx", dX), ("ld_h", H), ("ld_y", Y), ("ld_dr", dR), ("ld_dy", dY),
                 ("ld_gate", None if of_all else gate), ("ld_dgate", None if of_all else dgate)))
             need = C.c_size_t(0)

@@ -197,3 +197,23 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     refused(-1, m.block_norm_grad, rows, rows, Y=rows, dH=rows, dY=rows)
     with pytest.raises(ValueError):
         m.block_norm(rows, rows.clone(), Y=vec.expand(4, 64))  # rows on one another
+
+
+def test_the_binding_refuses_vectors_that_are_not_packed():
+    """a column, every second number, one number for all: each would be read or written as if its numbers lay behind one another"""
+    import torch
+    m = S.SemMoE(S.Config(T=4, d=64, E=4, k=2, F=32, D=1, cap=4), allocate_workspace=False)
+    new = lambda *shape: torch.zeros(*shape, dtype=torch.bfloat16)  # noqa: E731
+    rows, vec = new(4, 64), new(64)
+    for odd in (new(64, 64)[:, 0], new(128)[::2], new(1).expand(64)):
+        assert odd.shape == vec.shape
+        for name in ("w_post", "w_pre", "gate"):
+            with pytest.raises(S.SemMoEError, match="behind one another") as e:
+                m.block_norm(rows, new(4, 64), Y=rows, X=new(4, 64), **{"w_pre": vec, name: odd})
+            assert e.value.status == ESHAPE
+        for name in ("w_post", "w_pre", "gate", "dw_post", "dw_pre", "dgate"):
+            kw = {**dict(w_post=vec, w_pre=vec, gate=vec, dw_post=new(64), dw_pre=new(64), dgate=new(64)), name: odd}
+            with pytest.raises(S.SemMoEError, match="behind one another") as e:
+                m.block_norm_grad(rows, new(4, 64), Y=rows, dH=rows, dX=rows, **kw)
+            assert e.value.status == ESHAPE
+    assert not m._norm_calls  # what has been refused is not taken for checked
