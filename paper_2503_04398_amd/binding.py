@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import operator
 import os
+import struct
 import threading
 from dataclasses import dataclass
 from typing import Optional
@@ -36,6 +37,7 @@ class _CConfig(C.Structure):
                 ("cap", C.c_int32), ("num_classes", C.c_int32)]
 
 
+_three_numbers = struct.Struct("3d")
 _config_values = operator.attrgetter(*(name for name, _ in _CConfig._fields_))
 
 
@@ -806,10 +808,10 @@ class SemMoE:
 
     # -- the norms around a block
     def _norm_call(self, call, T, d, par, gate, vectors, rows):
-        """(config, shape) of a call on the norms: made and checked once for shapes, distances of rows and par (res_scale, eps_post,
-        eps_pre), which every layer of a step repeats.  vectors are w_post and w_pre with the gradients of such, and a gate of one
+        """(config, shape) of a call on the norms: made and checked once for shapes, distances of rows and par (the bytes of
+        res_scale, eps_post, eps_pre), which every layer of a step repeats.  vectors are w_post and w_pre with the gradients of such, and a gate of one
         dimension with its gradient, which are all rows'; rows the tensors [T,d] by the name of their distance."""
-        s = _CNormShape(*par, int(gate is not None and gate.dim() == 2))
+        s = _CNormShape(*_three_numbers.unpack(par), int(gate is not None and gate.dim() == 2))
         for t in vectors:
             if t is not None and (tuple(t.shape) != (d,) or not t.is_contiguous()):
                 raise SemMoEError("%s: a norm's weights, a gate of all rows and their gradients are %d numbers behind one another" % (call, d), -2)
@@ -834,7 +836,7 @@ class SemMoE:
         gate: [d] or [T,d].  H and X may lie in the place of R or Y."""
         T, d = (Y if R is None else R).shape
         tensors = (R, Y, w_post, gate, w_pre, H, X)
-        par = (res_scale, eps_post, eps_pre)
+        par = _three_numbers.pack(res_scale, eps_post, eps_pre)  # their values now, and their signs
         key = (_config_values(self.cfg), par, *[None if t is None else (t.shape, t.stride()) for t in tensors])
 
         def make():
@@ -868,7 +870,7 @@ class SemMoE:
         the place of one of dH, dX, H and Y, not in each other's."""
         T, d = (dX if dH is None else dH).shape
         tensors = (dH, dX, H, Y, w_post, gate, w_pre, dR, dY, dgate, dw_post, dw_pre)
-        par = (res_scale, eps_post, eps_pre)
+        par = _three_numbers.pack(res_scale, eps_post, eps_pre)  # their values now, and their signs
         key = (_config_values(self.cfg), par, *[None if t is None else (t.shape, t.stride()) for t in tensors])
         of_all = gate is not None and gate.dim() == 1
 

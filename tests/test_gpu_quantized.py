@@ -608,6 +608,17 @@ def test_infinite_weights_are_not_multiplied_with_rows_that_are_not_there(T, d, 
         assert torch.equal(out, clean[result])
 
 
+def test_a_residual_scale_that_is_learned():
+    """one tensor, another value in each step"""
+    c, g = _grad_case(np.random.default_rng(8), 9, 64, "fp32")
+    m, scale, H, dR = _m(T=9, d=64, dtype="fp32"), torch.tensor(1.0, device=DEV), torch.empty_like(g["H"]), torch.empty_like(g["H"])
+    for v in (1.0, 0.5, -2.0):
+        scale.fill_(v)
+        m.block_norm(g["H"], H, res_scale=scale)
+        m.block_norm_grad(g["H"], dR, dH=g["dH"], res_scale=scale)
+        assert torch.equal(H, v * g["H"]) and torch.equal(dR, v * g["dH"])
+
+
 def test_norms_of_rows_that_are_no_numbers():
     T, d = 40, 512
     r = np.random.default_rng(5)

@@ -217,3 +217,17 @@ def test_the_binding_refuses_vectors_that_are_not_packed():
                 m.block_norm_grad(rows, new(4, 64), Y=rows, dH=rows, dX=rows, **kw)
             assert e.value.status == ESHAPE
     assert not m._norm_calls  # what has been refused is not taken for checked
+
+
+def test_the_binding_keeps_values_and_not_what_held_them():
+    """a residual scale that is learned is one tensor with another value in each step; -0 is another scale than 0"""
+    import torch
+    m = S.SemMoE(S.Config(T=4, d=64, E=4, k=2, F=32, D=1, cap=4), allocate_workspace=False)
+    rows, scale, eps = torch.zeros(4, 64, dtype=torch.bfloat16), torch.tensor(0.0), torch.tensor(0.5)
+    for s, e in ((0.0, 0.5), (0.75, 0.5), (-0.0, 0.5), (0.75, 0.25)):
+        scale.fill_(s), eps.fill_(e)
+        for call, kw in ((m.block_norm, {}), (m.block_norm_grad, dict(dH=rows))):
+            with pytest.raises(S.SemMoEError):  # the rows lie on the host; what the library would be given has been made before
+                call(rows, rows.clone(), Y=rows, res_scale=scale, eps_post=eps, eps_pre=eps, **kw)
+            made = list(m._norm_calls.values())[-1][1]
+            assert (str(made.res_scale), made.eps_post, made.eps_pre) == (str(s), e, e)
