@@ -93,7 +93,18 @@ __device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
   return kI8<MODE> ? cvt_pk_bf16(lo, hi) : pack_bf16x2(lo, hi);
 }
 
-__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+__device__ __forceinline__ float silu_mul_fast(float g, float u) {
+  // silu(g) * u with one exp2 and one reciprocal
+  return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * g)) * u;
+}
+
+// 8-bit operands: one form in every kernel.  Their sums are exact, so that a row's bits follow neither from the tile that it falls to
+// nor from the other rows of the batch; with two forms h would now and then round to another bf16 number.
+template <int MODE>
+__device__ __forceinline__ float silu_mul(float g, float u) {
+  if constexpr (kI8<MODE>) return silu_mul_fast(g, u);
+  else return g / (1.0f + __expf(-g)) * u;
+}
 
 // fp32 sums between two products: blocks of 32 rows, in a block the rows of four consecutive features behind one another
 // ([rows / 32][N / 4][32][4]).  A lane's four of an accumulator are 16 bytes, the next lanes' rows follow, where the sums are
@@ -337,10 +348,10 @@ __device__ __forceinline__ void store_tile_via_lds(f32x16_t (&acc)[TF][TT], unsi
 #pragma unroll
           for (int g4 = 0; g4 < 4; ++g4) {
             const int chunk = (wf * (TF / 2) + i / 2) * 4 + g4;
-            const float h0 = silu_mul(acc[i][j][g4 * 4 + 0], acc[i + 1][j][g4 * 4 + 0]);
-            const float h1 = silu_mul(acc[i][j][g4 * 4 + 1], acc[i + 1][j][g4 * 4 + 1]);
-            const float h2 = silu_mul(acc[i][j][g4 * 4 + 2], acc[i + 1][j][g4 * 4 + 2]);
-            const float h3 = silu_mul(acc[i][j][g4 * 4 + 3], acc[i + 1][j][g4 * 4 + 3]);
+            const float h0 = silu_mul<MODE>(acc[i][j][g4 * 4 + 0], acc[i + 1][j][g4 * 4 + 0]);
+            const float h1 = silu_mul<MODE>(acc[i][j][g4 * 4 + 1], acc[i + 1][j][g4 * 4 + 1]);
+            const float h2 = silu_mul<MODE>(acc[i][j][g4 * 4 + 2], acc[i + 1][j][g4 * 4 + 2]);
+            const float h3 = silu_mul<MODE>(acc[i][j][g4 * 4 + 3], acc[i + 1][j][g4 * 4 + 3]);
             *reinterpret_cast<uint2*>(rowp + ((chunk ^ (t & MASK)) * 16)) =
                 make_uint2(pack_out<MODE>(h0, h1), pack_out<MODE>(h2, h3));
           }

@@ -247,7 +247,7 @@ __device__ __forceinline__ void gemm_stream_body(const GemmArgs& a, unsigned cha
           const f32x4_t s1 = *reinterpret_cast<const f32x4_t*>(ws + a.N);
           const f32x4_t gt = total_of(2 * p, j), up = total_of(2 * p + 1, j);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = silu_mul(scaled_sum(gt[e], xs, s0[e]), scaled_sum(up[e], xs, s1[e]));
+          for (int e = 0; e < 4; ++e) v[e] = silu_mul<MODE>(scaled_sum(gt[e], xs, s0[e]), scaled_sum(up[e], xs, s1[e]));
         } else {
           const f32x4_t sum = total_of(p, j);
 #pragma unroll
@@ -256,7 +256,7 @@ __device__ __forceinline__ void gemm_stream_body(const GemmArgs& a, unsigned cha
       } else if constexpr (MODE == kModeSwiglu) {
         const f32x4_t gt = total_of(2 * p, j), up = total_of(2 * p + 1, j);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = F32 ? gt[e] / (1.0f + expf(-gt[e])) * up[e] : silu_mul(gt[e], up[e]);
+        for (int e = 0; e < 4; ++e) v[e] = F32 ? gt[e] / (1.0f + expf(-gt[e])) * up[e] : silu_mul<MODE>(gt[e], up[e]);
       } else {
         v = total_of(p, j);
       }

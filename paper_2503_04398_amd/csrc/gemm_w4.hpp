@@ -63,11 +63,6 @@ __device__ __forceinline__ void lds_dma16_imm(const void* sbase, uint32_t voff, 
                : "memory", "m0", "scc");
 }
 
-__device__ __forceinline__ float silu_mul_fast(float g, float u) {
-  // silu(g) * u with one exp2 and one reciprocal
-  return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * g)) * u;
-}
-
 // 16 bytes of global memory at a uniform base: named so, for behind scalar_ptr the compiler would not know and use flat stores
 typedef __attribute__((address_space(1))) i32x4_t* global_i32x4_ptr;
 __device__ __forceinline__ global_i32x4_ptr global_i32x4(const unsigned char* base, uint32_t off) {

@@ -188,6 +188,42 @@ def test_tiles_and_pieces_in_every_form_of_launch(tile, ring, grid, cut, d, F):
             m.set_tuning(key, -1)
 
 
+@pytest.mark.parametrize("d,F", [(256, 2048), (400, 272), (2048, 512)])
+def test_every_tile_shape_gives_the_same_bits(d, F):
+    """sums of integers do not depend on their order, and every tile makes h of them by the same operations; so many numbers that
+    some lie within an fp32 rounding of a border between two of bf16"""
+    r, rows = np.random.default_rng(d), [n * 4 for n in RAGGED] + [1520, 129]
+    E, P = len(rows), sum(rows)
+    m = _m(T=P, d=d, E=E, k=1, F=F)
+    off = torch.tensor([0, *np.cumsum(rows)], dtype=torch.int32, device=DEV)
+    of = torch.arange(E, dtype=torch.int32, device=DEV)
+    (q, s), (w_gu, s_gu), (w_dn, s_dn) = _quantized(r, P, d), _quantized(r, E * 2 * F, d, 0.2), _quantized(r, E * d, F, 0.05)
+    out = {}
+    try:
+        for tile in [-1, *SHAPES]:
+            m.set_tuning(0, tile)
+            m.set_tuning(1, tile)
+            Y = torch.empty(P, d, dtype=torch.bfloat16, device=DEV)
+            m.expert_ffn_i8(-1, q, s, off, of, w_gu, s_gu, w_dn, s_dn, Y)
+            out[tile] = Y
+    finally:
+        m.set_tuning(0, -1)
+        m.set_tuning(1, -1)
+    assert [tile for tile, Y in out.items() if not torch.equal(Y, out[-1])] == []
+
+
+def test_a_row_of_the_ffn_in_8_bits_is_the_same_in_any_batch():
+    r = np.random.default_rng(11)
+    n, d, F = 6000, 528, 3600
+    (q, s), (w_gu, s_gu), (w_dn, s_dn) = _quantized(r, n, d), _quantized(r, 2 * F, d, 0.2), _quantized(r, d, F, 0.05)
+    whole = torch.empty(n, d, dtype=torch.bfloat16, device=DEV)
+    _m(T=n, d=d, F=F).shared_ffn_i8(q, s, n, w_gu, s_gu, w_dn, s_dn, whole)
+    for lo, rows in ((0, 1), (7, 16), (100, 100), (250, 600), (2900, 100), (3000, 2000)):
+        Y = torch.empty(rows, d, dtype=torch.bfloat16, device=DEV)
+        _m(T=rows, d=d, F=F).shared_ffn_i8(q[lo:lo + rows], s[lo:lo + rows], rows, w_gu, s_gu, w_dn, s_dn, Y)
+        assert torch.equal(Y, whole[lo:lo + rows]), (lo, rows)
+
+
 @pytest.mark.parametrize("T,d_out", [(40, 512), (300, 2048), (700, 4096)])
 def test_linear_i8_of_rows_far_apart(T, d_out):
     """rows of a tile that 32-bit offsets do not reach"""
