@@ -506,7 +506,7 @@ static int32_t launch_bf16_tile(int id, const GemmArgs& a, int max_rows, int bpc
 //     0.98 to 0.99; K 4096 0.95 to 1.01 from one on.  Where it is not taken K 4096, and K 2048 with a tile a compute unit or
 //     more, keep 64 x 64 streamed: 0.94 and 0.96 of the 128 x 64 tiles.
 //     384 experts and more leave no room in its LDS for their table (512 experts, d 1024, F 512, 300 rows: 776 us as
-//     256 x 256 tiles, 1134 as 128 x 64).
+//     256 x 256 tiles, 1134 as 128 x 64), nor do 287 and more beside the scales of 8-bit operands.
 // Rows that are no whole 128 bytes: neighbouring slices share cache lines, and from about ten rows on the staged tiles
 // read them at the better rate (10 rows of d 2832: 191 against 208).
 // One set of weights (the shared expert) on few rows has so few tiles that a compute unit gets one, and its speed is what
@@ -524,13 +524,13 @@ static int32_t launch_bf16_tile(int id, const GemmArgs& a, int max_rows, int bpc
 // it: 45 83 179 as 256 x 128 tiles, 66 112 236 as 256 x 256, 37 105 234 as pieces.  256 x 256 tiles are ahead of 256 x 128
 // from three fifths of the compute units on (170 to 190 of them: 2 to 4 %; 130 to 150: 2 % behind); 2514 rows of d 6968,
 // F 1312, gate/up without whole slices: 248 us for the FFN with pieces, 331 with 256 x 256 tiles on less than half of the chip.
-// tails: the tiles with a running load stream take any K (8-bit operands; rows that are no whole 128 bytes go to the staged tiles all the
+// i8, 8-bit operands: the tiles with a running load stream take any K (rows that are no whole 128 bytes go to the staged tiles all the
 // same: 128 experts of 16 rows, d = F = 2880 in 8 bits, 662 us with 64 x 64 streamed, 630 so)
-static int default_tile(const GemmArgs& a, int max_rows, int est_rows_per_group, int w_rows, bool tails = false) {
+static int default_tile(const GemmArgs& a, int max_rows, int est_rows_per_group, int w_rows, bool i8 = false) {
   const int est = est_rows_per_group, t256 = cdiv(w_rows, 256);
   const long long cus = num_cu();
   const bool aligned = a.K % 64 == 0;
-  const bool whole_slices = (tails || aligned) && cdiv(a.K, 64) >= 3;  // what the tiles with a running load stream need
+  const bool whole_slices = (i8 || aligned) && cdiv(a.K, 64) >= 3;  // what the tiles with a running load stream need
   const int big_tile = (long long)(max_rows / 256 + a.nq) * t256 * 2 >= cus ? 22 : 28;
   if (!a.offsets) {
     auto tiles = [&](int w, int t) { return (long long)cdiv(w_rows, w) * cdiv(est, t); };
@@ -550,7 +550,8 @@ static int default_tile(const GemmArgs& a, int max_rows, int est_rows_per_group,
     if (ring > 2 * cus && a.K < 1536) return a.K >= 640 ? 35 : 26;
     return a.K >= 960 ? 34 : 26;
   }
-  const bool w4_room = W4Cfg<kModeStore, 64, 3, 2, 2>::lds_bytes(a.nq) <= size_t(max_lds());
+  const size_t w4_lds = i8 ? W4Cfg<kModeStoreI8, 64, 3, 2, 2>::lds_bytes(a.nq) : W4Cfg<kModeStore, 64, 3, 2, 2>::lds_bytes(a.nq);
+  const bool w4_room = w4_lds <= size_t(max_lds());
   if (est < 40) {
     const long long mid = (long long)a.nq * w_rows / 256;  // 256 x 128 tiles, one per group along the tokens
     const bool pow2 = a.K >= 2048 && (a.K & (a.K - 1)) == 0;

@@ -337,6 +337,12 @@ def test_expert_ffn_i8(rows, d, F):
     _experts(rows, d, F, seed=1)
 
 
+@pytest.mark.parametrize("groups,rows,d,F", [(286, 100, 272, 272), (287, 100, 272, 272), (383, 100, 272, 80), (287, 200, 1280, 64), (512, 40, 400, 32)])
+def test_expert_ffn_i8_of_many_groups(groups, rows, d, F):
+    """as many groups as LDS holds beside a tile, and more"""
+    _experts([rows] * groups, d, F, seed=3)
+
+
 @pytest.mark.parametrize("rank", [0, 1, 3])
 def test_expert_ffn_i8_of_one_rank(rank):
     _experts(RAGGED, 256, 320, D=4, rank=rank, seed=2)
