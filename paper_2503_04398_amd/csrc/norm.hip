@@ -395,18 +395,27 @@ extern "C" int32_t semmoe_block_norm(const semmoe_config* cfg, void* stream, con
   const int64_t d = cfg->d;
   a.ld_r = n->ld_r ? n->ld_r : d; a.ld_y = n->ld_y ? n->ld_y : d; a.ld_h = n->ld_h ? n->ld_h : d; a.ld_x = n->ld_x ? n->ld_x : d;
   a.ld_gate = n->gate_rows ? (n->ld_gate ? n->ld_gate : d) : 0;
-  const dim3 grid(cdiv(cfg->T, g.teams)), block(g.tr * g.teams);
+  const dim3 block(g.tr * g.teams);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (bf) {
-    if (g.np == 1) hipLaunchKernelGGL((block_norm_kernel<true, 1>), grid, block, 0, s, a);
-    else if (g.np == 2) hipLaunchKernelGGL((block_norm_kernel<true, 2>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((block_norm_kernel<true, 4>), grid, block, 0, s, a);
-  } else {
-    if (g.np == 1) hipLaunchKernelGGL((block_norm_kernel<false, 1>), grid, block, 0, s, a);
-    else if (g.np == 2) hipLaunchKernelGGL((block_norm_kernel<false, 2>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((block_norm_kernel<false, 4>), grid, block, 0, s, a);
+  const int per = rows_a_launch(g.teams, block.x);
+  for (int row = 0; row < cfg->T; row += per) {
+    const dim3 grid(cdiv(a.n_rows < per ? a.n_rows : per, g.teams));
+    if (bf) {
+      if (g.np == 1) hipLaunchKernelGGL((block_norm_kernel<true, 1>), grid, block, 0, s, a);
+      else if (g.np == 2) hipLaunchKernelGGL((block_norm_kernel<true, 2>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((block_norm_kernel<true, 4>), grid, block, 0, s, a);
+    } else {
+      if (g.np == 1) hipLaunchKernelGGL((block_norm_kernel<false, 1>), grid, block, 0, s, a);
+      else if (g.np == 2) hipLaunchKernelGGL((block_norm_kernel<false, 2>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((block_norm_kernel<false, 4>), grid, block, 0, s, a);
+    }
+    SEMMOE_LAUNCH_CHECK();
+    a.n_rows -= per;
+    auto rest = [&](const void* p, int64_t ld) { return p ? static_cast<const char*>(p) + size_t(per) * ld * (bf ? 2 : 4) : nullptr; };
+    a.R = rest(a.R, a.ld_r); a.Y = rest(a.Y, a.ld_y); a.gate = rest(a.gate, a.ld_gate);
+    a.H = const_cast<char*>(rest(a.H, a.ld_h)); a.X = const_cast<char*>(rest(a.X, a.ld_x));
+    if (a.Xq) { a.Xq += size_t(per) * a.d; a.x_scale += per; }
   }
-  SEMMOE_LAUNCH_CHECK();
   return SEMMOE_OK;
 }
 

@@ -96,6 +96,10 @@ struct RowTeams {
   RowTeams(bool bf16, int n_cols) : RowTeams(bf16, n_cols, n_cols / (bf16 ? 8 : 4) <= 2048 ? 512 : 1024) {}
 };
 
+// Rows that one launch takes where every `teams` rows are a workgroup of `threads`: a grid has fewer than 2^32 threads.  More rows are
+// more launches (narrow rows from 2^25 on).
+inline int rows_a_launch(int teams, int threads) { return int((1u << 31) / unsigned(threads)) * teams; }
+
 // Rows of `n_cols` activations in 8 bits, see semmoe_quantize_rows.  row_range (device, nullable): only the rows from row_range[0] up
 // to row_range[n_range] exist, n_rows is then the most there can be.
 int32_t launch_quantize_rows(bool bf16, const void* X, int64_t ldx, int n_rows, int n_cols, const int32_t* row_range, int n_range,

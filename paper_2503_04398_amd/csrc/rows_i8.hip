@@ -149,15 +149,21 @@ extern "C" int32_t semmoe_dispatch_rows_i8(const semmoe_config* cfg, void* strea
   if (!aligned16(Xq) || !aligned16(Xq_perm)) return SEMMOE_EINVAL;
   if (cfg->T == 0) return SEMMOE_OK;
   const int pieces = cfg->d / 16, threads = row_walk_threads(pieces), P = cfg->T * cfg->k;
+  const row_u32x4_t* X = static_cast<const row_u32x4_t*>(Xq);
+  const int per = rows_a_launch(1, threads);
 #define SEMMOE_ROWS_I8(KU_)                                                                                                    \
-  hipLaunchKernelGGL(dispatch_rows_i8_kernel<KU_>, dim3(cfg->T), dim3(threads), 0, static_cast<hipStream_t>(stream), cfg->k, \
-                     pieces, P, static_cast<const row_u32x4_t*>(Xq), x_scale, slot_of_pair, static_cast<row_u32x4_t*>(Xq_perm), \
-                     x_scale_perm)
-  if (cfg->k <= 2) SEMMOE_ROWS_I8(2);
-  else if (cfg->k <= 4) SEMMOE_ROWS_I8(4);
-  else if (cfg->k <= 8) SEMMOE_ROWS_I8(8);
-  else SEMMOE_ROWS_I8(16);
+  hipLaunchKernelGGL(dispatch_rows_i8_kernel<KU_>, dim3(left < per ? left : per), dim3(threads), 0, static_cast<hipStream_t>(stream), \
+                     cfg->k, pieces, P, X, x_scale, slot_of_pair, static_cast<row_u32x4_t*>(Xq_perm), x_scale_perm)
+  for (int left = cfg->T; left > 0; left -= per) {
+    if (cfg->k <= 2) SEMMOE_ROWS_I8(2);
+    else if (cfg->k <= 4) SEMMOE_ROWS_I8(4);
+    else if (cfg->k <= 8) SEMMOE_ROWS_I8(8);
+    else SEMMOE_ROWS_I8(16);
+    SEMMOE_LAUNCH_CHECK();
+    X += size_t(per) * pieces;
+    x_scale += per;
+    slot_of_pair += size_t(per) * cfg->k;
+  }
 #undef SEMMOE_ROWS_I8
-  SEMMOE_LAUNCH_CHECK();
   return SEMMOE_OK;
 }

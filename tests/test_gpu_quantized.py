@@ -842,3 +842,34 @@ def test_offsets_past_32_bits():
     dR = torch.empty_like(H2)
     m.block_norm_grad(H2, dR, Y=X2, dH=X2, w_post=v)
     assert torch.equal(H[-tail:], dR)
+
+
+def test_more_rows_than_one_launch_takes():
+    """narrow rows whose teams have more threads together than a grid may have: as calls on parts of them, and by the values"""
+    T, d = (1 << 26) + 77, 8
+    g = torch.Generator(device=DEV).manual_seed(1)
+    R = torch.empty(T, d, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    gate, w = torch.empty_like(R).normal_(generator=g), torch.full((d,), 1.5, dtype=torch.bfloat16, device=DEV)
+    X, q, s = torch.full_like(R, 7.0), torch.full((T, d), 77, dtype=torch.int8, device=DEV), torch.full((T,), 7.0, device=DEV)
+    m, part = _m(T=T, d=d), 1 << 24
+    H = torch.full_like(R, 7.0)
+    m.block_norm(R, H, Y=R, X=X, Xq=q, x_scale=s, w_pre=w, gate=gate, **PAR)
+    for lo in range(0, T, part):
+        a = slice(lo, min(lo + part, T))
+        H2, X2, q2, s2 = torch.empty_like(R[a]), torch.empty_like(R[a]), torch.empty_like(q[a]), torch.empty_like(s[a])
+        m.block_norm(R[a], H2, Y=R[a], X=X2, Xq=q2, x_scale=s2, w_pre=w, gate=gate[a], **PAR)
+        assert torch.equal(H[a], H2) and torch.equal(X[a], X2) and torch.equal(q[a], q2) and torch.equal(s[a], s2), lo
+    c = dict(R=R[-99:], Y=R[-99:], w_post=None, gate=gate[-99:], w_pre=w)
+    b = _norm_bounds(c, "bf16")
+    _within(H[-99:], *b["H"], "H")
+    _within(X[-99:], *b["X"], "X")
+
+
+def test_more_rows_to_move_than_one_launch_takes():
+    T, d = (1 << 26) + 77, 16
+    q = torch.randint(-128, 128, (T, d), dtype=torch.int8, device=DEV)
+    s = torch.rand(T, device=DEV)
+    slots = torch.arange(T - 1, -1, -1, dtype=torch.int32, device=DEV)
+    out, scale = torch.zeros_like(q), torch.zeros_like(s)
+    _m(T=T, d=d).dispatch_rows_i8(q, s, slots, out, scale)
+    assert torch.equal(out, q.flip(0)) and torch.equal(scale, s.flip(0))
