@@ -873,3 +873,137 @@ def test_more_rows_to_move_than_one_launch_takes():
     out, scale = torch.zeros_like(q), torch.zeros_like(s)
     _m(T=T, d=d).dispatch_rows_i8(q, s, slots, out, scale)
     assert torch.equal(out, q.flip(0)) and torch.equal(scale, s.flip(0))
+
+
+# Rows beyond what the workgroups of the gradient take at once, by the threads of a row: several rows a team, with the next one
+# requested ahead or two and four pieces a thread, one team a workgroup and many
+MANY_ROWS = [(2600, 1032), (1100, 2048), (1500, 3632), (1050, 4096), (700, 4104), (600, 7168), (600, 8200), (300, 12296), (300, 16384)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("gate", ["rows", "one", None])
+@pytest.mark.parametrize("T,d", MANY_ROWS)
+def test_block_norm_grad_of_several_rows_a_team(T, d, gate, dtype):
+    c, g = _grad_case(np.random.default_rng(T + d), T, d, dtype, gate=gate)
+    m, outs = _m(T=T, d=d, dtype=dtype), _outs(c, T, d, dtype)
+    _grad(m, c, g, **outs)
+    for n, (want, bound) in _norm_grad_bounds(c, g, gate == "rows", dtype).items():
+        if n in outs:
+            _within(outs[n], want, bound, n)
+    # in the place of the inputs: a team's next rows are read before its present ones are written, and no others are
+    places = [("dH", "Y", "H"), ("H", "dX", "Y"), ("dX", "H", "dH"), ("Y", "dH", "dX")]
+    for rows in places:
+        c2, g2 = {**c, "Y": c["Y"].clone()}, {n: t.clone() for n, t in g.items()}
+        at = {**c2, **g2}
+        got = {**_outs(c, T, d, dtype), "dR": at[rows[0]], "dY": at[rows[1]]}
+        if gate == "rows":
+            got["dgate"] = at[rows[2]]
+        _grad(m, c2, g2, **got)
+        for n in outs:
+            assert torch.equal(outs[n], got[n]), (rows, n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("without", [("w_post",), ("w_post", "gate"), ("Y", "w_post", "gate"), ("dX", "H", "w_pre"), ("dH",)])
+@pytest.mark.parametrize("T,d", [(2600, 1032), (1050, 4096), (600, 8200), (300, 16384)])
+def test_block_norm_grad_of_several_rows_a_team_without(T, d, without, dtype):
+    """without w_post a row's second sum, and the barrier that goes with it, falls away"""
+    c, g = _grad_case(np.random.default_rng(T), T, d, dtype, gate="one", without=without)
+    want = _norm_grad_bounds(c, {n: None if n in without and n != "H" else t for n, t in g.items()}, False, dtype)
+    for n in without:
+        if n in g:
+            g[n] = None
+    outs = _outs(c, T, d, dtype)
+    _grad(_m(T=T, d=d, dtype=dtype), c, g, **outs)
+    for n in outs:
+        _within(outs[n], *want[n], n)
+
+
+@pytest.mark.parametrize("gate", ["rows", "one"])
+def test_norm_gradient_past_32_bits(gate):
+    """numbers past 2^31 of the first one: the last rows as a call of their own gives them, sums over rows as those of parts"""
+    T, d, tail = 300007, 7168, 5
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    new = lambda *shape: torch.empty(*shape, dtype=torch.bfloat16, device=DEV).normal_(generator=gen)  # noqa: E731
+    g, c = {n: new(T, d) for n in ("dH", "dX", "H")}, dict(Y=new(T, d), w_post=1 + new(d), w_pre=1 + new(d))
+    c["gate"] = new(T, d) if gate == "rows" else new(d)
+    outs = _outs(c, T, d, "bf16")
+    _grad(_m(T=T, d=d), c, g, **outs)
+    end = lambda t: t[-tail:].contiguous() if t.shape[0] == T else t  # noqa: E731
+    c2, g2 = {n: end(t) for n, t in c.items()}, {n: end(t) for n, t in g.items()}
+    last = _outs(c2, tail, d, "bf16")
+    _grad(_m(T=tail, d=d), c2, g2, **last)
+    rows = ("dR", "dY", "dgate") if gate == "rows" else ("dR", "dY")
+    for n in rows:
+        assert torch.equal(outs[n][-tail:], last[n]), n
+    for n, (want, bound) in _norm_grad_bounds(c2, g2, gate == "rows", "bf16").items():
+        _within(last[n], want, bound, n)
+    # Sums over rows, in 64 bits by parts.  A term is off by ADDS + 12 roundings of the row's own sums and the products, as in
+    # _norm_grad_bounds; its error through dH' is at most as much of |dX w_pre| rh (1 + 2 |xn| mean|xn|), which is taken below; a
+    # column's sum passes T / 256 additions in a workgroup and 256 + 40 behind it.
+    want = {n: torch.zeros(d, dtype=torch.float64, device=DEV) for n in outs if n not in rows}
+    bound = {n: torch.zeros_like(t) for n, t in want.items()}
+    E = E32 * (ADDS + 12 + T // 256 + 296)
+    for lo in range(0, T, 20000):
+        a = slice(lo, lo + 20000)
+        dH, dX, H, Y = (t[a].double() for t in (g["dH"], g["dX"], g["H"], c["Y"]))
+        gt, wp, wq = (c["gate"][a] if gate == "rows" else c["gate"]).double(), c["w_post"].double(), c["w_pre"].double()
+        rh = 1 / (H.square().mean(1, keepdim=True) + PAR["eps_pre"]).sqrt()
+        yn = Y / (Y.square().mean(1, keepdim=True) + PAR["eps_post"]).sqrt()
+        xn, aw = H * rh, dX * wq
+        u = dH + rh * (aw - xn * (aw * xn).mean(1, keepdim=True))
+        size = u.abs() + dH.abs() + rh * (aw.abs() + 2 * xn.abs() * (aw * xn).abs().mean(1, keepdim=True))
+        for n, term, most in (("dw_pre", dX * xn, (dX * xn).abs()), ("dw_post", u * gt * yn, size * (gt * yn).abs()),
+                              ("dgate", u * yn * wp, size * (yn * wp).abs())):
+            if n in want:
+                want[n] += term.sum(0)
+                bound[n] += E * most.sum(0)
+    for n in want:
+        _within(outs[n], want[n], _np(bound[n] + R["bf16"] * want[n].abs()), n)
+
+
+@pytest.mark.parametrize("T", [3, 40, 300])
+@pytest.mark.parametrize("d_out", [33000, 66000])
+def test_linear_i8_of_weights_past_32_bits(T, d_out):
+    """weights beyond 2 and 4 GiB: the first and the last channels as a product of their own gives them"""
+    d_in = 65552
+    w = torch.randint(-128, 128, (d_out, d_in), dtype=torch.int8, device=DEV)
+    q, s, ws = torch.randint(-128, 128, (T, d_in), dtype=torch.int8, device=DEV), torch.rand(T, device=DEV), torch.rand(d_out, device=DEV)
+    m, Y = _m(), torch.full((T + 1, d_out), 7.0, dtype=torch.bfloat16, device=DEV)
+    m.linear_i8(q, s, w, ws, Y[:T])
+    for at in (slice(0, 64), slice(d_out // 2 - 40, d_out // 2 + 40), slice(d_out - 64, d_out)):
+        part = w[at].contiguous()
+        Z = torch.empty(T, part.shape[0], dtype=torch.bfloat16, device=DEV)
+        m.linear_i8(q, s, part, ws[at].clone(), Z)
+        assert torch.equal(Y[:T, at], Z)
+        want = (q.double() @ part.double().t()) * s.double()[:, None] * ws[at].double()
+        _within(Z, want, _np((R["bf16"] + 3 * E32) * want.abs() + TINY), "Z")
+    assert (Y[T] == 7.0).all()
+
+
+def test_expert_ffn_i8_of_an_expert_past_32_bits():
+    """an expert's gate and up rows beyond 2 GiB, the second expert's past 4"""
+    r = np.random.default_rng(12)
+    d, F, rows = 65552, 16400, [0, 9, 3]
+    P, E = sum(rows), 3
+    m = _m(T=P, d=d, E=E, k=1, F=F)
+    w_gu, w_dn = (torch.randint(-128, 128, s, dtype=torch.int8, device=DEV) for s in ((2, 2 * F, d), (2, d, F)))
+    s_gu, s_dn = torch.rand(2, 2 * F, device=DEV) * 2e-7 + 1e-7, torch.rand(2, d, device=DEV) * 1e-5
+    q, s = torch.randint(-128, 128, (P, d), dtype=torch.int8, device=DEV), torch.rand(P, device=DEV) + 0.5
+    off, of = torch.tensor([0, *np.cumsum(rows)], dtype=torch.int32, device=DEV), torch.tensor([0, 1, 0], dtype=torch.int32, device=DEV)
+    Y = torch.full((P, d), 7.0, dtype=torch.bfloat16, device=DEV)
+    m.expert_ffn_i8(-1, q, s, off, of, w_gu, s_gu, w_dn, s_dn, Y)
+    for e, lo, hi in ((1, 0, 9), (0, 9, 12)):
+        gu = (q[lo:hi].double() @ w_gu[e].double().t()) * s[lo:hi].double()[:, None] * s_gu[e].double()
+        gate = gu[:, :F]
+        h = gate * torch.sigmoid(gate) * gu[:, F:]
+        eps = (12 + 4 * gate.abs()) * 2.0 ** -23
+        near, below, above = (t.to(torch.bfloat16).float().cpu().numpy() for t in (h, h * (1 - eps), h * (1 + eps)))
+        (hq, hs), (lq, ls), (uq, us) = (Q.quantize_rows(t) for t in (near, below, above))
+        step = hs.astype(np.float64)[:, None]
+        D = step * np.maximum(np.abs(uq.astype(float) - hq), np.abs(lq.astype(float) - hq))
+        D = np.where((ls != us)[:, None], 2.0 ** -7 * np.abs(near) + 1.01 * step, D)
+        W = w_dn[e].double() * s_dn[e].double()[:, None]
+        want = (torch.from_numpy(hq).to(DEV).double() @ W.t()) * torch.from_numpy(step).to(DEV)
+        spread = torch.from_numpy(D).to(DEV) @ W.abs().t()
+        _within(Y[lo:hi], want, _np((R["bf16"] + 4 * E32) * want.abs() + (1 + R["bf16"]) * spread + TINY), "expert %d" % e)
