@@ -639,7 +639,8 @@ int32_t semmoe_shared_ffn_i8(const semmoe_config* cfg, void* stream, const void*
  *   H = res_scale * R + gate * n                   (gate NULL: 1; R or Y NULL: without that term);
  *   X = H * rsqrt(mean(H^2) + eps_pre) * w_pre.
  * gate has one number for each channel (gate_rows = 0: gate[d]) or for each number of a row (gate_rows != 0: gate[T,d]).
- * ld*: distances of rows in elements, 0 = packed, multiples of 8, at least d; pointers lie on 16 bytes.  d <= SEMMOE_MAX_NORM_D.
+ * ld*: distances of rows in elements, 0 = packed, multiples of 8, at least d; pointers lie on 16 bytes.  d <= SEMMOE_MAX_NORM_D,
+ * T < 2^30.  With an eps of 0 a row of zeros has no norm (NaN, as the formula says), and nor has its share of the sums over rows.
  * cfg: T (rows), d and dtype are used.
  */
 typedef struct semmoe_norm_shape {

@@ -5,9 +5,9 @@
 // h lies in memory as bf16 between its product and its 8-bit form, as expert_ffn's does, since its largest magnitude is known only when
 // the row is whole.  That rounding raises the error of the 8-bit form from 1.904e-2 of a row's norm to 1.911e-2 (silu(g) u of normal
 // numbers, F 768; 2.243e-2 to 2.249e-2 at F 2048); fp32 would double the bytes of the pass.
-// What bounds them: weights' bytes where rows are few (128 experts of 8 rows, d 2048, F 768: 604 MB in 120 us, 5.0 TB/s), the matrix pipes'
-// power and LDS where they are many (8192 rows 7168 -> 4096: 201 us, 2.4 POP/s), a tile's epilogue where K is short (20865 rows 768 -> 2048:
-// 66 us, 1.0 POP/s).
+// What bounds them: weights' bytes where rows are few (128 experts of 8 rows, d 2048, F 768: 604 MB in 71 + 46 us, 5.2 TB/s), the matrix
+// pipes where they are many (8192 rows 7168 -> 4096: 207 us, 2.3 POP/s, busy in 58 % of the cycles at 1.9 GHz), a tile's epilogue where K is
+// short (20865 rows 768 -> 2048: 64 us, 1.0 POP/s).
 #include "gemm_core.hpp"
 #include "rows.hpp"
 

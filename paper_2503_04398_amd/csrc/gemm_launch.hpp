@@ -525,7 +525,9 @@ static int32_t launch_bf16_tile(int id, const GemmArgs& a, int max_rows, int bpc
 // from three fifths of the compute units on (170 to 190 of them: 2 to 4 %; 130 to 150: 2 % behind); 2514 rows of d 6968,
 // F 1312, gate/up without whole slices: 248 us for the FFN with pieces, 331 with 256 x 256 tiles on less than half of the chip.
 // i8, 8-bit operands: the tiles with a running load stream take any K (rows that are no whole 128 bytes go to the staged tiles all the
-// same: 128 experts of 16 rows, d = F = 2880 in 8 bits, 662 us with 64 x 64 streamed, 630 so)
+// same.  FFNs in 8 bits, us as 128 x 64 staged tiles and as 64 x 64 streamed: d = F = 2880, 128 experts of 10, 16 and 30 rows 609 617, 633 670 and
+// 685 845, 64, 32, 16 and 8 of 16 rows 334 354, 176 191, 103 109 and 67 69; d 2064, 128 of 16, F 784, 177 183, 256 of 12, F 528, 226 247; d = F = 1680,
+// 64 of 12 147 152; d 4112, F 1552, 16 of 30 110 114; the other way round d 4112, F 1552, 32 of 20 177 174 and d 7184, F 2064, 16 of 12 198 185)
 static int default_tile(const GemmArgs& a, int max_rows, int est_rows_per_group, int w_rows, bool i8 = false) {
   const int est = est_rows_per_group, t256 = cdiv(w_rows, 256);
   const long long cus = num_cu();

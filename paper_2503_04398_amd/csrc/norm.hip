@@ -4,8 +4,9 @@
 // dgate = dH n, dw_post = sum over rows of dH gate Y ry, dw_pre = sum of dX H rh.
 //
 // Both stream: each tensor is read or written once, a row stays in registers between its two norms.  Statistics and sums are fp32.
-// Measured, bf16: 16384 rows of 7168 194 us, 4.85 TB/s as a copy; the gradient of 8192 rows of 4096 88 + 7 us, 4.6 TB/s with its partial
-// sums.
+// Measured, bf16: 16384 rows of 7168 194 us, 4.85 TB/s as a copy; the gradient of 8192 rows of 4096 89 + 6 us, 4.7 TB/s with its partial
+// sums, of 4096 rows of 7168 100 + 5.  fp32 gradient: 8192 rows of 4096 179 + 5 us, 4096 of 7168 148 + 5.  Past 8192 registers are
+// spilled: 17 of four pieces a thread in bf16 (13401 rows of 8208 222 us where 178 are a copy), and below at the gradient.
 #include <initializer_list>
 
 #include "rows.hpp"
@@ -125,7 +126,8 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const NormArgs a) {
 constexpr int kNormGradGroups = 512;  // workgroups of the backward pass at most: the rows of partial sums
 
 // NP 1: the rows that come next are requested before this one's sums are joined; with NP 2 there are no registers for that.  GATES: a
-// gate for each row.
+// gate for each row.  Of 128 registers bf16 rows past 8192 spill 10 with GATES and 41 without (2048 rows of 14336: 192 us, a copy 71), fp32
+// ones 191 and 238 (545 and 509 us, a copy 190 and 142).
 template <bool BF16, int NP, bool GATES>
 __global__ __launch_bounds__(1024, 4) void block_norm_grad_kernel(const NormArgs a) {
   using E = Piece<BF16>;
@@ -356,8 +358,8 @@ static int32_t check_norm(const semmoe_config* cfg, const semmoe_norm_shape* n, 
 }
 
 // The backward pass' kernel holds 128 registers a thread: 16 waves a compute unit.  Workgroups of 8 waves, two a compute unit, as many
-// teams in each as fit: their sums meet in LDS, and the rows of partial sums are fewer (16384 rows of 2048: 93 us, one team a workgroup
-// of 4 waves 112; as 16 waves 103).  A team of more than 8 waves is a workgroup, one a compute unit (4096 rows of 7168: 104 us, with twice
+// teams in each as fit: their sums meet in LDS, and the rows of partial sums are fewer (16384 rows of 2048: 94 us, one team a workgroup
+// of 4 waves 112; as 16 waves 103).  A team of more than 8 waves is a workgroup, one a compute unit (4096 rows of 7168: 105 us, with twice
 // as many workgroups 118).
 static RowTeams norm_grad_teams(const semmoe_config* cfg) {
   RowTeams g(cfg->dtype == SEMMOE_BF16, cfg->d, 1024);

@@ -91,8 +91,11 @@ struct RowTeams {
     teams = tr >= 256 ? 1 : 256 / tr;
   }
   // 512 threads where four pieces each hold the row: several such teams a compute unit are at different steps (norms of 20297 rows of
-  // 3632 in fp32 228 us, 276 with up to 1024 threads; of 16384 rows of 7168 in bf16 195 and 244;
-  // 20297 rows of 3632 in fp32 to 8 bits 72 and 88).  1024 beyond it: 4096 rows of 32768 in bf16 to 8 bits 88 us, read twice 102.
+  // 3632 in fp32 228 us, 276 with up to 1024 threads; of 16384 rows of 7168 in bf16 194 and 244;
+  // 20297 rows of 3632 in fp32 to 8 bits 72 and 88).  Four pieces a thread, norms of 1.1e8 numbers in bf16, widths 8208, 10240, 12288, 14336
+  // and 16384: 222, 195, 190, 185 and 176 us, as 1024 threads of two 248, 221, 204, 215 and 209; of 5.5e7 in fp32, widths 4104, 5120, 6144, 7168 and
+  // 8192: 178, 163, 160, 158 and 151, as 1024 threads of two 164, 157, 153, 165 and 153; to 8 bits within 5 % of one another, 7 % at 4104.
+  // 1024 beyond it: 4096 rows of 32768 in bf16 to 8 bits 88 us, read twice 102.
   RowTeams(bool bf16, int n_cols) : RowTeams(bf16, n_cols, n_cols / (bf16 ? 8 : 4) <= 2048 ? 512 : 1024) {}
 };
 
