@@ -93,17 +93,15 @@ __device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
   return kI8<MODE> ? cvt_pk_bf16(lo, hi) : pack_bf16x2(lo, hi);
 }
 
-__device__ __forceinline__ float silu_mul_fast(float g, float u) {
-  // silu(g) * u with one exp2 and one reciprocal
-  return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * g)) * u;
-}
-
-// 8-bit operands: one form in every kernel.  Their sums are exact, so that a row's bits follow neither from the tile that it falls to
-// nor from the other rows of the batch; with two forms h would now and then round to another bf16 number.
+// 8-bit operands: one form in every kernel, with one exp2 and one reciprocal.  Their sums are exact, so that a row's bits follow neither
+// from the tile that it falls to nor from the other rows of the batch; with two forms h would now and then round to another bf16 number.
+// The reciprocal is taken of a quarter of 1 + exp(-g): that of the whole, a subnormal number below g = -87.3, would be given as 0.
 template <int MODE>
 __device__ __forceinline__ float silu_mul(float g, float u) {
-  if constexpr (kI8<MODE>) return silu_mul_fast(g, u);
-  else return g / (1.0f + __expf(-g)) * u;
+  if constexpr (kI8<MODE>)
+    return 0.25f * g * __builtin_amdgcn_rcpf(fmaf(0.25f, __builtin_amdgcn_exp2f(-1.44269504088896340736f * g), 0.25f)) * u;
+  else
+    return g / (1.0f + __expf(-g)) * u;
 }
 
 // fp32 sums between two products: blocks of 32 rows, in a block the rows of four consecutive features behind one another

@@ -63,6 +63,11 @@ __device__ __forceinline__ void lds_dma16_imm(const void* sbase, uint32_t voff, 
                : "memory", "m0", "scc");
 }
 
+__device__ __forceinline__ float silu_mul_fast(float g, float u) {
+  // silu(g) * u with one exp2 and one reciprocal
+  return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * g)) * u;
+}
+
 // 16 bytes of global memory at a uniform base: named so, for behind scalar_ptr the compiler would not know and use flat stores
 typedef __attribute__((address_space(1))) i32x4_t* global_i32x4_ptr;
 __device__ __forceinline__ global_i32x4_ptr global_i32x4(const unsigned char* base, uint32_t off) {
@@ -516,7 +521,7 @@ __device__ __forceinline__ int gemm_bf16_w4_body(const GemmArgs& a, unsigned cha
               for (int e = 0; e < 4; ++e) {
                 y[e] = scaled_sum(acc[M * (NB * h + b)][j][g4 * 4 + e], x_scale[j], ws[b][g4][e]);
                 if constexpr (kPaired<MODE>)
-                  y[e] = silu_mul_fast(y[e], scaled_sum(acc[M * (NB * h + b) + 1][j][g4 * 4 + e], x_scale[j], us[b][g4][e]));
+                  y[e] = silu_mul<MODE>(y[e], scaled_sum(acc[M * (NB * h + b) + 1][j][g4 * 4 + e], x_scale[j], us[b][g4][e]));
               }
               *reinterpret_cast<uint2*>(put + (b * 4 + g4) * 16) = make_uint2(cvt_pk_bf16(y[0], y[1]), cvt_pk_bf16(y[2], y[3]));
             }

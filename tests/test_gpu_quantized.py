@@ -368,6 +368,26 @@ def test_large_gate_values():
     _ffn_check(_np(Y), *(t.cpu().numpy() for t in (q, s, w_gu, s_gu, w_dn, s_dn)), "Y")
 
 
+@pytest.mark.parametrize("tile", [-1, 0, 16, 22, 26, 28, 32, 33, 35])
+def test_gates_whose_sigmoid_lies_below_the_normal_numbers(tile):
+    """sigmoid(g) between 2^-128 and 2^-126 beside large ups: small, and not nothing"""
+    r = np.random.default_rng(13)
+    n, d, F = 600, 384, 400
+    m, q, w_gu = _m(T=n, d=d, F=F), np.zeros((n, d), np.int8), np.zeros((2 * F, d), np.int8)
+    q[:, 0], w_gu[:F, 0], w_gu[F:, 0] = 127, -1, 1
+    s = r.uniform(0.999, 1.001, n).astype(np.float32)
+    s_gu = np.concatenate([np.linspace(87.45, 88.55, F) / 127, np.full(F, 2.0 ** 110 / 127)]).astype(np.float32)
+    (w_dn, s_dn) = (t.cpu().numpy() for t in _quantized(r, d, F, 0.05))
+    Y = torch.empty(n, d, dtype=torch.bfloat16, device=DEV)
+    try:
+        m.set_tuning(0, tile)
+        m.shared_ffn_i8(*(torch.from_numpy(t).to(DEV) for t in (q, s)), n, *(torch.from_numpy(t).to(DEV) for t in (w_gu, s_gu, w_dn, s_dn)), Y)
+    finally:
+        m.set_tuning(0, -1)
+    _ffn_check(_np(Y), q, s, w_gu, s_gu, w_dn, s_dn, "Y")
+    assert (_np(Y) != 0).mean() > 0.9
+
+
 def test_a_row_that_is_no_number_stays_alone_in_the_ffn():
     r = np.random.default_rng(4)
     n, d, F = 40, 256, 128
